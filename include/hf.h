@@ -309,6 +309,103 @@ hf_status hf_selftest_wait_limit(hf_ctx* ctx, void* stream);
 /* Number of kernels the library has launched since the context was created. */
 hf_status hf_launch_count(hf_ctx* ctx, int64_t* launches);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * The rest of a denoiser block around the attention: layer norm, rotary positions with several axes, the gated
+ * feed-forward, each with its backward pass.  (No counterpart in the paper, which takes them from the pretrained model.)
+ *
+ * These calls need no context.  They run on the CURRENT device, enqueue work on `stream` and return; scratch is the caller's (`workspace`,
+ * whose size the *_workspace calls give; 16-byte aligned; it may be used again as soon as the call's work is done in stream order), so calls
+ * on different streams with different workspaces are independent.  They may be captured into a graph once one call of the kind has been
+ * made on the device.  Strides are in elements.  Sums, means and products are formed in float32 whatever the type; a result is rounded
+ * once.  A call of no rows launches nothing, or clears the parameters' gradients.  Gradients are summed in a fixed order: a call repeated
+ * gives the same bits.  A bounded wait that runs out, or a position outside its table, is reported by hf_layers_status. */
+enum { HF_BF16 = 0, HF_F16 = 1, HF_F32 = 2 };            /* element types */
+
+/* Layer norm over the last axis: mean and rstd = 1 / sqrt(var + eps) of each row, xhat = (x - mean) rstd,
+ *   y = xhat (weight_offset + weight_g) + bias_g,   g = row / rows_per_group (0 for every row when rows_per_group is 0).
+ * weight, bias: one row of `width` parameters for each group, param_stride elements apart.  rows_per_group > 0 with weight_offset 1 is
+ * the modulated norm of a denoiser (a scale and a shift per latent frame, slices of one modulation tensor). */
+typedef struct {
+    int type;                    /* of x, y, dy, dx: HF_BF16 | HF_F16 | HF_F32                                        */
+    int param_type;              /* of weight and bias: `type` or HF_F32                                              */
+    int width;                   /* D, 1 .. 16384                                                                     */
+    int64_t rows;
+    int64_t x_stride, y_stride, dx_stride;     /* between rows of x, of y or dy, of dx; each >= width                 */
+    int64_t rows_per_group;      /* 0: one group                                                                      */
+    int64_t param_stride;        /* >= width; not read with one group                                                 */
+    float weight_offset;         /* added to weight; not used without weight                                          */
+    float eps;                   /* >= 0                                                                              */
+} hf_norm_shape;
+
+/* weight, bias, mean, rstd may be NULL (no factor, no shift; not written).  mean, rstd float [rows].  y may be x.  Pointers are aligned to
+ * their element; rows whose starts are all 16-byte aligned and whose width is a multiple of 16 bytes are read and written in 16-byte pieces. */
+hf_status hf_layer_norm(const hf_norm_shape* shape, const void* x, const void* weight, const void* bias, void* y, float* mean,
+                        float* rstd, void* stream);
+
+/* With gh = dy (weight_offset + weight_g):
+ *   dx = rstd (gh - mean(gh) - xhat mean(gh xhat)),  dweight_g = sum of dy xhat over the group's rows,  dbias_g = sum of dy.
+ * mean, rstd: what the forward returned.  dweight, dbias float [groups, width], contiguous, written, not added to.  dx, and dweight and
+ * dbias, may be NULL (not formed).  dx may be dy or x. */
+hf_status hf_layer_norm_workspace(const hf_norm_shape* shape, size_t* bytes);
+hf_status hf_layer_norm_backward(const hf_norm_shape* shape, const void* dy, const void* x, const float* mean, const float* rstd,
+                                 const void* weight, void* dx, float* dweight, float* dbias, void* workspace, void* stream);
+
+/* Rotary positions with several axes (time, height, width of a video's tokens): the first pairs[0] feature pairs of a head turn by the
+ * token's position on axis 0, the next pairs[1] by its position on axis 1, and so on; features behind them are copied.
+ * (x0, x1) -> (x0 c - x1 s, x0 s + x1 c); with `inverse` the other way round, which is the backward pass.
+ *   cos_tab, sin_tab  device float: axis a's table [extent[a], pairs[a]] behind axis a - 1's
+ *   pos               device int32 [batch, tokens, axes], or [tokens, axes] for all batches (pos_batch 0).  A position outside [0, extent[a]) is
+ *                     taken as 0 and sets flag 2 of the status word.
+ * One launch takes up to three tensors of [batch, tokens, heads, head_dim] elements, features contiguous, other axes with strides of
+ * their own: q, k and v between the rows of a fused projection and head-major tensors, in either direction.  A tensor with rotate 0 is copied. */
+enum { HF_PAIRS_ADJACENT = 0, HF_PAIRS_HALVES = 1 };     /* pair p = features (2p, 2p+1) | (p, P + p), P = sum of pairs */
+typedef struct {
+    int type;
+    int batch, tokens, head_dim;                         /* head_dim even, 2 .. 1024                                  */
+    int axes;                                            /* 1 .. 4                                                    */
+    int pairs[4], extent[4];                             /* sum of pairs <= head_dim / 2                              */
+    int pairing;                                         /* HF_PAIRS_ADJACENT | HF_PAIRS_HALVES                       */
+    int inverse;
+    int64_t pos_batch;                                   /* int32 between the positions of two batches; 0: shared     */
+} hf_rope_shape;
+typedef struct {
+    const void* x;                                       /* read                                                      */
+    void* y;                                             /* written; may be x with the same strides                   */
+    int64_t x_batch, x_token, x_head;                    /* strides of x                                              */
+    int64_t y_batch, y_token, y_head;
+    int heads;
+    int rotate;                                          /* 0: copied                                                 */
+} hf_rope_tensor;
+hf_status hf_rope_axes(const hf_rope_shape* shape, const hf_rope_tensor* tensors, int n_tensors, const float* cos_tab,
+                       const float* sin_tab, const int32_t* pos, void* stream);
+
+/* Gated feed-forward:  g = x Wg^T,  u = x Wu^T,  h = act(g) u,  y = h Wd^T.   act: silu(g) = g / (1 + e^-g), or the tanh form of gelu.
+ *   x [rows, width], Wg, Wu [hidden, width], Wd [out_width, hidden], y [rows, out_width]: bf16 or f16, weights contiguous.
+ *   gate, up [rows, hidden] contiguous: g and u for the backward pass, rounded to the type, or both NULL.
+ * h is rounded to the type between the two products (the tensor cores take 16-bit operands), from g and u in float32.
+ * width, hidden, out_width: multiples of 8; strides too; pointers 16-byte aligned. */
+enum { HF_ACT_SILU = 0, HF_ACT_GELU_TANH = 1 };
+typedef struct {
+    int type;                    /* HF_BF16 | HF_F16 */
+    int act;
+    int64_t rows;                /* up to 2^24       */
+    int width, hidden, out_width;                        /* up to 2^17 */
+    int64_t x_stride, y_stride;                          /* between rows of x, of y or dy */
+} hf_ff_shape;
+hf_status hf_gated_ff_workspace(const hf_ff_shape* shape, int backward, size_t* bytes);
+hf_status hf_gated_ff(const hf_ff_shape* shape, const void* x, const void* w_gate, const void* w_up, const void* w_down, void* y,
+                      void* gate, void* up, void* workspace, void* stream);
+/* dh = dy Wd,  dg = dh u act'(g),  du = dh act(g),   dx = dg Wg + du Wu,  dWg = dg^T x,  dWu = du^T x,  dWd = dy^T h  (h from g and u again;
+ * dg, du and h rounded to the type).  gate, up: what the forward returned.  dx [rows, width], dWg, dWu, dWd: the type, contiguous, written.
+ * dx, and the three weights' gradients together, may be NULL (not formed). */
+hf_status hf_gated_ff_backward(const hf_ff_shape* shape, const void* dy, const void* x, const void* w_gate, const void* w_up,
+                               const void* w_down, const void* gate, const void* up, void* dx, void* dw_gate, void* dw_up,
+                               void* dw_down, void* workspace, void* stream);
+
+/* Synchronises the current device and reports the status word of the calls without a context, as hf_get_device_status does for a
+ * context's: flag 1 a bounded wait ran out (HF_ERR_DEVICE_TIMEOUT), flag 2 a position outside its table (HF_ERR_INVALID_ARG).  Clears it. */
+hf_status hf_layers_status(int* flags, int* detail);
+
 const char* hf_status_string(hf_status s);
 const char* hf_last_error(void);   /* text of the last failure on this thread ("" if none) */
 

@@ -19,6 +19,9 @@ HF_PHI_ELU1 = 0
 HF_MERGE_IDENTITY, HF_MERGE_PER_HEAD, HF_MERGE_FULL_WIDTH = 0, 1, 2
 HF_SWA_AUTO, HF_SWA_MMA, HF_SWA_TCGEN05, HF_SWA_TCGEN05_PINGPONG = 0, 1, 2, 3
 HF_Z_SUM, HF_Z_FRAME_MEAN = 0, 1
+HF_BF16, HF_F16, HF_F32 = 0, 1, 2
+HF_PAIRS_ADJACENT, HF_PAIRS_HALVES = 0, 1
+HF_ACT_SILU, HF_ACT_GELU_TANH = 0, 1
 (HF_Q_CACHED_CHUNKS, HF_Q_KEY_BLOCKS, HF_Q_KEPT_BLOCKS, HF_Q_ABSORBED_TOKENS, HF_Q_QUERY_BLOCKS,
  HF_Q_MASK_WORDS, HF_Q_SWA_KERNEL, HF_Q_SINK_CHUNKS) = range(8)
 
@@ -29,6 +32,8 @@ EXPORTS = [
     "hf_kv_append_host", "hf_get_state", "hf_query", "hf_get_device_status", "hf_launch_count",
     "hf_status_string", "hf_last_error", "hf_state_absorb_noalloc", "hf_set_rope", "hf_state_export", "hf_state_import",
     "hf_sparse_swa_merged", "hf_slow_path_units", "hf_selftest_wait_limit", "hf_kv_append_layers", "hf_state_absorb_layers", "hf_set_temporal_rope", "hf_sparse_swa_backward_dq", "hf_sparse_swa_backward_dkv", "hf_linear_attn_backward_dq",
+    "hf_layer_norm", "hf_layer_norm_workspace", "hf_layer_norm_backward", "hf_rope_axes", "hf_gated_ff_workspace", "hf_gated_ff",
+    "hf_gated_ff_backward", "hf_layers_status",
 ]
 
 
@@ -37,6 +42,27 @@ class hf_config(C.Structure):
                 ("tokens_per_frame", C.c_int), ("chunk_frames", C.c_int), ("window_frames", C.c_int),
                 ("block", C.c_int), ("topk", C.c_int), ("keep_permille", C.c_int), ("layers", C.c_int),
                 ("phi", C.c_int), ("eps", C.c_float), ("merge", C.c_int), ("swa_kernel", C.c_int), ("z_mode", C.c_int), ("sink_frames", C.c_int)]
+
+
+class hf_norm_shape(C.Structure):
+    _fields_ = [("type", C.c_int), ("param_type", C.c_int), ("width", C.c_int), ("rows", C.c_int64), ("x_stride", C.c_int64),
+                ("y_stride", C.c_int64), ("dx_stride", C.c_int64), ("rows_per_group", C.c_int64), ("param_stride", C.c_int64),
+                ("weight_offset", C.c_float), ("eps", C.c_float)]
+
+
+class hf_rope_shape(C.Structure):
+    _fields_ = [("type", C.c_int), ("batch", C.c_int), ("tokens", C.c_int), ("head_dim", C.c_int), ("axes", C.c_int),
+                ("pairs", C.c_int * 4), ("extent", C.c_int * 4), ("pairing", C.c_int), ("inverse", C.c_int), ("pos_batch", C.c_int64)]
+
+
+class hf_rope_tensor(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("y", C.c_void_p), ("x_batch", C.c_int64), ("x_token", C.c_int64), ("x_head", C.c_int64),
+                ("y_batch", C.c_int64), ("y_token", C.c_int64), ("y_head", C.c_int64), ("heads", C.c_int), ("rotate", C.c_int)]
+
+
+class hf_ff_shape(C.Structure):
+    _fields_ = [("type", C.c_int), ("act", C.c_int), ("rows", C.c_int64), ("width", C.c_int), ("hidden", C.c_int),
+                ("out_width", C.c_int), ("x_stride", C.c_int64), ("y_stride", C.c_int64)]
 
 
 class HFError(RuntimeError):
@@ -88,6 +114,14 @@ def lib() -> C.CDLL:
     L.hf_slow_path_units.argtypes = [vp, C.POINTER(C.c_int64)]
     L.hf_selftest_wait_limit.argtypes = [vp, vp]
     L.hf_state_absorb_noalloc.argtypes = [vp, vp, ip, ip, ip, vp, vp, vp]
+    L.hf_layer_norm.argtypes = [C.POINTER(hf_norm_shape)] + [vp] * 7
+    L.hf_layer_norm_workspace.argtypes = [C.POINTER(hf_norm_shape), C.POINTER(C.c_size_t)]
+    L.hf_layer_norm_backward.argtypes = [C.POINTER(hf_norm_shape)] + [vp] * 10
+    L.hf_rope_axes.argtypes = [C.POINTER(hf_rope_shape), C.POINTER(hf_rope_tensor), ip, vp, vp, vp, vp]
+    L.hf_gated_ff_workspace.argtypes = [C.POINTER(hf_ff_shape), ip, C.POINTER(C.c_size_t)]
+    L.hf_gated_ff.argtypes = [C.POINTER(hf_ff_shape)] + [vp] * 9
+    L.hf_gated_ff_backward.argtypes = [C.POINTER(hf_ff_shape)] + [vp] * 13
+    L.hf_layers_status.argtypes = [C.POINTER(ip), C.POINTER(ip)]
     L.hf_status_string.argtypes = [ip]
     L.hf_status_string.restype = C.c_char_p
     L.hf_last_error.argtypes = []
@@ -260,6 +294,49 @@ def hf_state_absorb_noalloc(k_ev, v_ev, S, z):
     n = k_ev.shape[-2]
     bh = k_ev.numel() // (n * d)
     _check(lib().hf_state_absorb_noalloc(_ptr(k_ev), _ptr(v_ev), bh, n, d, _ptr(S), _ptr(z), _stream()))
+
+
+# -- calls without a context, one to one; tensors as in include/hf.h (layers.py allocates, checks and fills the shapes in)
+def hf_layer_norm(shape, x, weight, bias, y, mean, rstd):
+    _check(lib().hf_layer_norm(C.byref(shape), _ptr(x), _ptr(weight), _ptr(bias), _ptr(y), _ptr(mean), _ptr(rstd), _stream()))
+
+
+def hf_layer_norm_workspace(shape) -> int:
+    n = C.c_size_t()
+    _check(lib().hf_layer_norm_workspace(C.byref(shape), C.byref(n)))
+    return n.value
+
+
+def hf_layer_norm_backward(shape, dy, x, mean, rstd, weight, dx, dweight, dbias, workspace):
+    _check(lib().hf_layer_norm_backward(C.byref(shape), _ptr(dy), _ptr(x), _ptr(mean), _ptr(rstd), _ptr(weight), _ptr(dx), _ptr(dweight),
+                                        _ptr(dbias), _ptr(workspace), _stream()))
+
+
+def hf_rope_axes(shape, tensors, n_tensors, cos_tab, sin_tab, pos):
+    """tensors: a ctypes array of hf_rope_tensor."""
+    _check(lib().hf_rope_axes(C.byref(shape), tensors, n_tensors, _ptr(cos_tab), _ptr(sin_tab), _ptr(pos), _stream()))
+
+
+def hf_gated_ff_workspace(shape, backward) -> int:
+    n = C.c_size_t()
+    _check(lib().hf_gated_ff_workspace(C.byref(shape), backward, C.byref(n)))
+    return n.value
+
+
+def hf_gated_ff(shape, x, w_gate, w_up, w_down, y, gate, up, workspace):
+    _check(lib().hf_gated_ff(C.byref(shape), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(y), _ptr(gate), _ptr(up),
+                             _ptr(workspace), _stream()))
+
+
+def hf_gated_ff_backward(shape, dy, x, w_gate, w_up, w_down, gate, up, dx, dw_gate, dw_up, dw_down, workspace):
+    _check(lib().hf_gated_ff_backward(C.byref(shape), _ptr(dy), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(gate), _ptr(up),
+                                      _ptr(dx), _ptr(dw_gate), _ptr(dw_up), _ptr(dw_down), _ptr(workspace), _stream()))
+
+
+def hf_layers_status():
+    f, d = C.c_int(), C.c_int()
+    _check(lib().hf_layers_status(C.byref(f), C.byref(d)))
+    return f.value, d.value
 
 
 def bits_to_cuda(bits, device="cuda"):

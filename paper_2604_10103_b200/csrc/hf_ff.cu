@@ -1,0 +1,197 @@
+// Gated feed-forward: host side and the kernels' instantiations.
+#include "hf_layers.h"
+#include <type_traits>
+#include "k_ff_gemm.cuh"
+
+#include <cstring>
+
+using namespace hf_layers;
+
+namespace {
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// Map of a matrix [rows, cols] of 16-bit elements with `stride` between rows; box of box_cols (64: 128-byte swizzle; 32: 64-byte) x box_rows.
+hf_status matrix_map(const Device* d, CUtensorMap* m, int type, const void* base, long long rows, long long cols, long long stride,
+                     int box_cols, int box_rows) {
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)(rows > 1 ? stride : (cols + 7) / 8 * 8) * 2};
+    const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
+    const cuuint32_t es[2] = {1, 1};
+    const CUresult r = reinterpret_cast<EncodeTiledFn>(d->encode_tiled)(
+        m, type == HF_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void*>(base), dims, strides, box, es,
+        CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(HF_ERR_CUDA, "cuTensorMapEncodeTiled failed with %d", (int)r);
+    return HF_OK;
+}
+
+struct Matrix { const void* p; long long rows, cols, stride; };
+
+// One launch being put together: operands, outputs, tiles.
+struct Launch {
+    const Device* d;
+    int type;
+    FfGemmParams p;
+    Launch(const Device* dev, int t, int act) : d(dev), type(t) {
+        memset(&p, 0, sizeof(p));
+        p.segments = 1; p.act = act; p.dev_status = dev->status;
+    }
+    // Contraction-contiguous (K-major) operand of `tile` rows; row-contiguous (MN-major) operand.
+    hf_status k_major(CUtensorMap* m, const Matrix& x, int tile) { return matrix_map(d, m, type, x.p, x.rows, x.cols, x.stride, 64, tile); }
+    hf_status mn_major(CUtensorMap* m, const Matrix& x) { return matrix_map(d, m, type, x.p, x.rows, x.cols, x.stride, 64, 64); }
+    hf_status output(int i, const Matrix& x) { return matrix_map(d, &p.out[i], type, x.p, x.rows, x.cols, x.stride, 32, 32); }
+    void product(long long rows, int cols, long long contraction, int bn_out) {
+        const int i = p.products++;
+        p.rows[i] = (int)rows; p.cols[i] = cols; p.kb[i] = (int)((contraction + 63) / 64);
+        const long long tiles = (rows + FfGemm::BM - 1) / FfGemm::BM * ((cols + bn_out - 1) / bn_out);
+        p.tile0[i + 1] = p.tile0[i] + (int)tiles;
+    }
+    template <typename T, int EPI, bool A_MN, bool B_MN>
+    hf_status run_t(cudaStream_t st) {
+        p.stages = FfGemm::stages_for(p.bn);
+        const int smem = FfGemm::smem_bytes(p.bn, p.stages), tiles = p.tile0[p.products];
+        HFL_CUDA(cudaFuncSetAttribute(k_ff_gemm<T, EPI, A_MN, B_MN>, cudaFuncAttributeMaxDynamicSharedMemorySize, FfGemm::SMEM_MAX));
+        k_ff_gemm<T, EPI, A_MN, B_MN><<<tiles < d->sm_count ? tiles : d->sm_count, FfGemm::THREADS, smem, st>>>(p);
+        HFL_CUDA(cudaGetLastError());
+        return HF_OK;
+    }
+    template <int EPI, bool A_MN, bool B_MN>
+    hf_status run(cudaStream_t st) {
+        return type == HF_BF16 ? run_t<bf16, EPI, A_MN, B_MN>(st) : run_t<__half, EPI, A_MN, B_MN>(st);
+    }
+};
+
+hf_status ff_check(const hf_ff_shape* g) {
+    if (g == nullptr) return fail(HF_ERR_INVALID_ARG, "shape is null");
+    if (g->type != HF_BF16 && g->type != HF_F16) return fail(HF_ERR_UNSUPPORTED, "type %d: bf16 and f16 are taken", g->type);
+    if (g->act != HF_ACT_SILU && g->act != HF_ACT_GELU_TANH) return fail(HF_ERR_UNSUPPORTED, "act %d unknown", g->act);
+    if (g->rows < 0 || g->rows > (1 << 24)) return fail(HF_ERR_SHAPE, "rows %lld outside [0, 2^24]", (long long)g->rows);
+    const int w[3] = {g->width, g->hidden, g->out_width};
+    for (int v : w)
+        if (v < 8 || v % 8 || v > (1 << 17)) return fail(HF_ERR_SHAPE, "width, hidden and out_width are multiples of 8 up to 2^17: got %d", v);
+    if (g->rows > 1) {
+        if (g->x_stride < g->width || g->y_stride < g->out_width) return fail(HF_ERR_SHAPE, "row strides must be at least the width");
+        if (g->x_stride % 8 || g->y_stride % 8) return fail(HF_ERR_SHAPE, "row strides must be multiples of 8");
+        if (g->x_stride > (1LL << 36) || g->y_stride > (1LL << 36)) return fail(HF_ERR_SHAPE, "row strides too large");
+    }
+    return HF_OK;
+}
+hf_status ff_pointer(const void* p, const char* name) {
+    if (p == nullptr) return fail(HF_ERR_INVALID_ARG, "%s is null", name);
+    if (!aligned(p, 16)) return fail(HF_ERR_INVALID_ARG, "%s is not 16-byte aligned", name);
+    return HF_OK;
+}
+size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
+
+}  // namespace
+
+extern "C" {
+
+hf_status hf_gated_ff_workspace(const hf_ff_shape* g, int backward, size_t* bytes) {
+    HFL_TRY(ff_check(g));
+    if (!bytes) return fail(HF_ERR_INVALID_ARG, "bytes is null");
+    const size_t h = round_up((size_t)g->rows * g->hidden * 2);
+    *bytes = backward ? 3 * h : h;          // h; dg, du, h
+    return HF_OK;
+}
+
+hf_status hf_gated_ff(const hf_ff_shape* g, const void* x, const void* w_gate, const void* w_up, const void* w_down, void* y, void* gate,
+                      void* up, void* workspace, void* stream) {
+    HFL_TRY(ff_check(g));
+    if (g->rows == 0) return HF_OK;
+    HFL_TRY(ff_pointer(x, "x")); HFL_TRY(ff_pointer(w_gate, "w_gate")); HFL_TRY(ff_pointer(w_up, "w_up")); HFL_TRY(ff_pointer(w_down, "w_down"));
+    HFL_TRY(ff_pointer(y, "y")); HFL_TRY(ff_pointer(workspace, "workspace"));
+    if ((gate == nullptr) != (up == nullptr)) return fail(HF_ERR_INVALID_ARG, "gate and up are saved together or not at all");
+    if (gate) { HFL_TRY(ff_pointer(gate, "gate")); HFL_TRY(ff_pointer(up, "up")); }
+    const Device* d;
+    HFL_TRY(current_device(&d));
+    const cudaStream_t st = (cudaStream_t)stream;
+    const long long M = g->rows, K = g->width, N = g->hidden, O = g->out_width;
+    const Matrix h = {workspace, M, N, N};
+    {
+        Launch l(d, g->type, g->act);
+        const int hn = 128;
+        l.p.bn = 2 * hn;
+        HFL_TRY(l.k_major(&l.p.a[0], {x, M, K, g->x_stride}, FfGemm::BM));
+        HFL_TRY(l.k_major(&l.p.b[0], {w_gate, N, K, K}, hn));
+        HFL_TRY(l.k_major(&l.p.b[1], {w_up, N, K, K}, hn));
+        HFL_TRY(l.output(0, h));
+        if (gate) {
+            HFL_TRY(l.output(1, {gate, M, N, N}));
+            HFL_TRY(l.output(2, {up, M, N, N}));
+            l.p.save = 1;
+        }
+        l.product(M, N, K, hn);
+        HFL_TRY((l.run<FF_GATED, false, false>(st)));
+    }
+    Launch l(d, g->type, g->act);
+    l.p.bn = 256;
+    HFL_TRY(l.k_major(&l.p.a[0], h, FfGemm::BM));
+    HFL_TRY(l.k_major(&l.p.b[0], {w_down, O, N, N}, l.p.bn));
+    HFL_TRY(l.output(0, {y, M, O, g->y_stride}));
+    l.product(M, O, N, l.p.bn);
+    return l.run<FF_STORE, false, false>(st);
+}
+
+hf_status hf_gated_ff_backward(const hf_ff_shape* g, const void* dy, const void* x, const void* w_gate, const void* w_up, const void* w_down,
+                               const void* gate, const void* up, void* dx, void* dw_gate, void* dw_up, void* dw_down, void* workspace,
+                               void* stream) {
+    HFL_TRY(ff_check(g));
+    const int n_dw = (dw_gate != nullptr) + (dw_up != nullptr) + (dw_down != nullptr);
+    if (n_dw != 0 && n_dw != 3) return fail(HF_ERR_INVALID_ARG, "the weights' gradients are formed together or not at all");
+    const cudaStream_t st = (cudaStream_t)stream;
+    const long long M = g->rows, K = g->width, N = g->hidden, O = g->out_width;
+    if (n_dw) { HFL_TRY(ff_pointer(dw_gate, "dw_gate")); HFL_TRY(ff_pointer(dw_up, "dw_up")); HFL_TRY(ff_pointer(dw_down, "dw_down")); }
+    if (M == 0) {
+        if (n_dw) {
+            HFL_CUDA(cudaMemsetAsync(dw_gate, 0, (size_t)N * K * 2, st));
+            HFL_CUDA(cudaMemsetAsync(dw_up, 0, (size_t)N * K * 2, st));
+            HFL_CUDA(cudaMemsetAsync(dw_down, 0, (size_t)O * N * 2, st));
+        }
+        return HF_OK;
+    }
+    if (!dx && !n_dw) return HF_OK;
+    HFL_TRY(ff_pointer(dy, "dy")); HFL_TRY(ff_pointer(x, "x")); HFL_TRY(ff_pointer(w_gate, "w_gate")); HFL_TRY(ff_pointer(w_up, "w_up"));
+    HFL_TRY(ff_pointer(w_down, "w_down")); HFL_TRY(ff_pointer(gate, "gate")); HFL_TRY(ff_pointer(up, "up")); HFL_TRY(ff_pointer(workspace, "workspace"));
+    if (dx) HFL_TRY(ff_pointer(dx, "dx"));
+    const Device* d;
+    HFL_TRY(current_device(&d));
+    const size_t part = round_up((size_t)M * N * 2);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    const Matrix mdy = {dy, M, O, g->y_stride}, mx = {x, M, K, g->x_stride}, dg = {ws, M, N, N}, du = {ws + part, M, N, N}, h = {ws + 2 * part, M, N, N};
+    {
+        Launch l(d, g->type, g->act);
+        l.p.bn = 256;
+        l.p.gate = gate; l.p.up = up;
+        HFL_TRY(l.k_major(&l.p.a[0], mdy, FfGemm::BM));
+        HFL_TRY(l.mn_major(&l.p.b[0], {w_down, O, N, N}));
+        HFL_TRY(l.output(0, dg)); HFL_TRY(l.output(1, du)); HFL_TRY(l.output(2, h));
+        l.product(M, (int)N, O, l.p.bn);
+        HFL_TRY((l.run<FF_DHIDDEN, false, true>(st)));
+    }
+    if (dx) {
+        Launch l(d, g->type, g->act);
+        l.p.bn = 256;
+        HFL_TRY(l.k_major(&l.p.a[0], dg, FfGemm::BM)); HFL_TRY(l.k_major(&l.p.a[1], du, FfGemm::BM));
+        HFL_TRY(l.mn_major(&l.p.b[0], {w_gate, N, K, K})); HFL_TRY(l.mn_major(&l.p.b[1], {w_up, N, K, K}));
+        HFL_TRY(l.output(0, {dx, M, K, K}));
+        l.product(M, (int)K, N, l.p.bn);
+        l.p.segments = 2; l.p.kb[1] = l.p.kb[0];
+        HFL_TRY((l.run<FF_STORE, false, true>(st)));
+    }
+    if (n_dw) {
+        Launch l(d, g->type, g->act);
+        l.p.bn = 256;
+        HFL_TRY(l.mn_major(&l.p.a[0], dg)); HFL_TRY(l.mn_major(&l.p.a[1], du)); HFL_TRY(l.mn_major(&l.p.a[2], mdy));
+        HFL_TRY(l.mn_major(&l.p.b[0], mx)); l.p.b[1] = l.p.b[0]; HFL_TRY(l.mn_major(&l.p.b[2], h));
+        HFL_TRY(l.output(0, {dw_gate, N, K, K})); HFL_TRY(l.output(1, {dw_up, N, K, K})); HFL_TRY(l.output(2, {dw_down, O, N, N}));
+        l.product(N, (int)K, M, l.p.bn); l.product(N, (int)K, M, l.p.bn); l.product(O, (int)N, M, l.p.bn);
+        HFL_TRY((l.run<FF_STORE, true, true>(st)));
+    }
+    return HF_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,118 @@
+// Rotary positions with several axes.  Feature pair p of a token turns by the angle of its axis a(p) at the token's position on that
+// axis, read from tables: (x0, x1) -> (x0 c - x1 s, x0 s + x1 c) (inverse: s -> -s, the transposed rotation, which is the backward pass).
+// Products and sums in float32, one rounding at the end.  Up to three tensors of [batch, tokens, heads, head_dim] with strides of their
+// own go through one launch (q, k, v between a projection's rows and head-major tensors); one that is not rotated is copied.
+// Memory bounds it: a thread keeps the angles of its features of a token in registers and walks heads with them.
+#pragma once
+#include "k_vec.cuh"
+
+struct RopeTensor {
+    const void* x; void* y;
+    long long xb, xt, xh, yb, yt, yh;       // elements between batches, tokens, heads
+    int heads, rotate;
+};
+struct RopeParams {
+    RopeTensor t[3];
+    const float* cos_tab; const float* sin_tab;
+    const int* pos;
+    long long pos_batch;                    // ints between batches (0: shared)
+    int first[4], pairs[4], extent[4], tab[4];      // per axis: first pair, pairs, rows of the table, first entry of the table
+    int axes, n_pairs;                      // n_pairs: rotated pairs; features behind them are copied
+    int batch, tokens, units;               // units: threads of a token
+    int n_tensors, head_dim, slices, total_heads;
+    int inverse;
+    int* dev_status;
+};
+
+// HALVES: pair p = features (p, n_pairs + p), otherwise (2p, 2p + 1).  A thread owns 2 V features of a token: V pairs, or 2 V features
+// behind the rotated ones, in two pieces of V (neighbours unless HALVES).  WIDE: every piece of every tensor starts on a boundary of its
+// own size (at most 16 bytes); otherwise V is 1 and elements are accessed one by one.
+template <typename T, int V, bool HALVES, bool WIDE>
+__global__ void __launch_bounds__(256)
+k_rope_axes(const RopeParams p) {
+    constexpr int HB = 4;
+    const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
+    const long long bt = id / p.units;
+    if (bt >= (long long)p.batch * p.tokens) return;
+    const int u = (int)(id - bt * p.units), b = (int)(bt / p.tokens), tok = (int)(bt - (long long)b * p.tokens);
+    // features f0 .. f0 + V - 1 and f1 .. f1 + V - 1
+    const int pair0 = u * V;
+    const bool turned = pair0 < p.n_pairs;                          // (HALVES: n_pairs is a multiple of V)
+    const int f0 = HALVES && turned ? pair0 : 2 * pair0;
+    const int f1 = HALVES && turned ? p.n_pairs + pair0 : f0 + V;
+    float c[V], s[V];
+    bool on[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const int pr = pair0 + j;
+        on[j] = pr < p.n_pairs;
+        c[j] = 1.f; s[j] = 0.f;
+        if (on[j]) {
+            int a = 0;
+            while (a + 1 < p.axes && pr >= p.first[a + 1]) ++a;
+            int at = p.pos[b * p.pos_batch + (long long)tok * p.axes + a];
+            if ((unsigned)at >= (unsigned)p.extent[a]) {            // outside the table: no address is formed from it
+                atomicOr(p.dev_status, HF_DEV_BAD_INDEX_FLAG);
+                atomicExch(p.dev_status + 1, tok);
+                at = 0;
+            }
+            const int e = p.tab[a] + at * p.pairs[a] + pr - p.first[a];
+            c[j] = p.cos_tab[e];
+            s[j] = p.inverse ? -p.sin_tab[e] : p.sin_tab[e];
+        }
+    }
+    // this slice's part of all tensors' heads, one after the other
+    int h = (int)((long long)p.total_heads * blockIdx.y / p.slices);
+    const int h_end = (int)((long long)p.total_heads * (blockIdx.y + 1) / p.slices);
+    int n = 0, base = 0;
+    while (n < p.n_tensors && h < h_end) {
+        const RopeTensor& t = p.t[n];
+        if (h >= base + t.heads) { base += t.heads; ++n; continue; }
+        const int stop = min(h_end, base + t.heads);
+        const T* x = static_cast<const T*>(t.x) + b * t.xb + tok * t.xt + (h - base) * t.xh;
+        T* y = static_cast<T*>(t.y) + b * t.yb + tok * t.yt + (h - base) * t.yh;
+        const bool rot = t.rotate != 0;
+        // HB heads' loads are in flight together (x and y may be the same tensor, so the order of the code is the order of the accesses)
+        for (; h < stop; h += HB, x += HB * t.xh, y += HB * t.yh) {
+            Vec<T, V, WIDE> lo[HB], hi[HB];
+#pragma unroll
+            for (int k = 0; k < HB; ++k)
+                if (h + k < stop) {
+                    if constexpr (HALVES || !WIDE) {
+                        lo[k] = *reinterpret_cast<const Vec<T, V, WIDE>*>(x + k * t.xh + f0);
+                        hi[k] = *reinterpret_cast<const Vec<T, V, WIDE>*>(x + k * t.xh + f1);
+                    } else {
+                        const Vec<T, 2 * V> v = *reinterpret_cast<const Vec<T, 2 * V>*>(x + k * t.xh + f0);
+#pragma unroll
+                        for (int j = 0; j < V; ++j) { lo[k].v[j] = v.v[j]; hi[k].v[j] = v.v[V + j]; }
+                    }
+                }
+#pragma unroll
+            for (int k = 0; k < HB; ++k)
+                if (h + k < stop) {
+                    if (rot) {
+#pragma unroll
+                        for (int j = 0; j < V; ++j)
+                            if (on[j]) {            // (an infinity behind the rotated pairs is copied, not multiplied by a zero sine)
+                                // neighbours: pair j is elements (2j, 2j + 1) of the 2 V
+                                T& e0 = HALVES ? lo[k].v[j] : (2 * j < V ? lo[k].v[2 * j % V] : hi[k].v[2 * j % V]);
+                                T& e1 = HALVES ? hi[k].v[j] : (2 * j + 1 < V ? lo[k].v[(2 * j + 1) % V] : hi[k].v[(2 * j + 1) % V]);
+                                const float x0 = to_float(e0), x1 = to_float(e1);
+                                e0 = from_float<T>(x0 * c[j] - x1 * s[j]);
+                                e1 = from_float<T>(x0 * s[j] + x1 * c[j]);
+                            }
+                    }
+                    if constexpr (HALVES || !WIDE) {
+                        *reinterpret_cast<Vec<T, V, WIDE>*>(y + k * t.yh + f0) = lo[k];
+                        *reinterpret_cast<Vec<T, V, WIDE>*>(y + k * t.yh + f1) = hi[k];
+                    } else {
+                        Vec<T, 2 * V> v;
+#pragma unroll
+                        for (int j = 0; j < V; ++j) { v.v[j] = lo[k].v[j]; v.v[V + j] = hi[k].v[j]; }
+                        *reinterpret_cast<Vec<T, 2 * V>*>(y + k * t.yh + f0) = v;
+                    }
+                }
+        }
+        h = stop;
+    }
+}

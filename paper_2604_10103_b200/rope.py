@@ -33,3 +33,11 @@ def chunk_positions(last_frame: int, t0: int, chunk_frames: int, height: int, wi
     ts = relative_temporal_indices(last_frame, t0, chunk_frames)
     t, y, x = np.meshgrid(np.asarray(ts), np.arange(height), np.arange(width), indexing="ij")
     return np.stack([t.ravel(), y.ravel(), x.ravel()], axis=1)
+
+
+def axis_tables(extents, pairs_per_axis, base: float = 10000.0):
+    """Tables of `layers.split_heads_rope` / `hf_rope_axes`: for each axis the angles position * base ** (-j / pairs) of its pairs at the
+    positions 0 .. extent - 1, one axis after the other.  Returns float32 (cos, sin), flat, formed in float64."""
+    th = [np.arange(e, dtype=np.float64)[:, None] * base ** (-np.arange(n, dtype=np.float64) / n)[None, :] for e, n in zip(extents, pairs_per_axis)]
+    th = np.concatenate([t.ravel() for t in th])
+    return np.cos(th).astype(np.float32), np.sin(th).astype(np.float32)
