@@ -114,13 +114,14 @@ def lib() -> C.CDLL:
     L.hf_slow_path_units.argtypes = [vp, C.POINTER(C.c_int64)]
     L.hf_selftest_wait_limit.argtypes = [vp, vp]
     L.hf_state_absorb_noalloc.argtypes = [vp, vp, ip, ip, ip, vp, vp, vp]
-    L.hf_layer_norm.argtypes = [C.POINTER(hf_norm_shape)] + [vp] * 7
-    L.hf_layer_norm_workspace.argtypes = [C.POINTER(hf_norm_shape), C.POINTER(C.c_size_t)]
-    L.hf_layer_norm_backward.argtypes = [C.POINTER(hf_norm_shape)] + [vp] * 10
-    L.hf_rope_axes.argtypes = [C.POINTER(hf_rope_shape), C.POINTER(hf_rope_tensor), ip, vp, vp, vp, vp]
-    L.hf_gated_ff_workspace.argtypes = [C.POINTER(hf_ff_shape), ip, C.POINTER(C.c_size_t)]
-    L.hf_gated_ff.argtypes = [C.POINTER(hf_ff_shape)] + [vp] * 9
-    L.hf_gated_ff_backward.argtypes = [C.POINTER(hf_ff_shape)] + [vp] * 13
+    # (shapes as the structures' bytes, or by reference: one struct.pack costs a fifth of a Structure with its fields)
+    L.hf_layer_norm.argtypes = [vp] * 8
+    L.hf_layer_norm_workspace.argtypes = [vp, C.POINTER(C.c_size_t)]
+    L.hf_layer_norm_backward.argtypes = [vp] * 11
+    L.hf_rope_axes.argtypes = [vp, vp, ip, vp, vp, vp, vp]
+    L.hf_gated_ff_workspace.argtypes = [vp, ip, C.POINTER(C.c_size_t)]
+    L.hf_gated_ff.argtypes = [vp] * 10
+    L.hf_gated_ff_backward.argtypes = [vp] * 14
     L.hf_layers_status.argtypes = [C.POINTER(ip), C.POINTER(ip)]
     L.hf_status_string.argtypes = [ip]
     L.hf_status_string.restype = C.c_char_p
@@ -296,41 +297,47 @@ def hf_state_absorb_noalloc(k_ev, v_ev, S, z):
     _check(lib().hf_state_absorb_noalloc(_ptr(k_ev), _ptr(v_ev), bh, n, d, _ptr(S), _ptr(z), _stream()))
 
 
-# -- calls without a context, one to one; tensors as in include/hf.h (layers.py allocates, checks and fills the shapes in)
+# -- calls without a context, one to one; tensors as in include/hf.h (layers.py allocates, checks and fills the shapes in).
+# shape: an hf_norm_shape / hf_rope_shape / hf_ff_shape by C.byref, or its bytes.
+def _call(fn, *args):
+    status = fn(*args, _stream())
+    if status != HF_OK:
+        raise HFError(status, lib().hf_last_error().decode())
+
+
 def hf_layer_norm(shape, x, weight, bias, y, mean, rstd):
-    _check(lib().hf_layer_norm(C.byref(shape), _ptr(x), _ptr(weight), _ptr(bias), _ptr(y), _ptr(mean), _ptr(rstd), _stream()))
+    _call(lib().hf_layer_norm, shape, _ptr(x), _ptr(weight), _ptr(bias), _ptr(y), _ptr(mean), _ptr(rstd))
 
 
 def hf_layer_norm_workspace(shape) -> int:
     n = C.c_size_t()
-    _check(lib().hf_layer_norm_workspace(C.byref(shape), C.byref(n)))
+    _check(lib().hf_layer_norm_workspace(shape, C.byref(n)))
     return n.value
 
 
 def hf_layer_norm_backward(shape, dy, x, mean, rstd, weight, dx, dweight, dbias, workspace):
-    _check(lib().hf_layer_norm_backward(C.byref(shape), _ptr(dy), _ptr(x), _ptr(mean), _ptr(rstd), _ptr(weight), _ptr(dx), _ptr(dweight),
-                                        _ptr(dbias), _ptr(workspace), _stream()))
+    _call(lib().hf_layer_norm_backward, shape, _ptr(dy), _ptr(x), _ptr(mean), _ptr(rstd), _ptr(weight), _ptr(dx), _ptr(dweight), _ptr(dbias),
+          _ptr(workspace))
 
 
 def hf_rope_axes(shape, tensors, n_tensors, cos_tab, sin_tab, pos):
-    """tensors: a ctypes array of hf_rope_tensor."""
-    _check(lib().hf_rope_axes(C.byref(shape), tensors, n_tensors, _ptr(cos_tab), _ptr(sin_tab), _ptr(pos), _stream()))
+    """tensors: a ctypes array of hf_rope_tensor, or its bytes."""
+    _call(lib().hf_rope_axes, shape, tensors, n_tensors, _ptr(cos_tab), _ptr(sin_tab), _ptr(pos))
 
 
 def hf_gated_ff_workspace(shape, backward) -> int:
     n = C.c_size_t()
-    _check(lib().hf_gated_ff_workspace(C.byref(shape), backward, C.byref(n)))
+    _check(lib().hf_gated_ff_workspace(shape, backward, C.byref(n)))
     return n.value
 
 
 def hf_gated_ff(shape, x, w_gate, w_up, w_down, y, gate, up, workspace):
-    _check(lib().hf_gated_ff(C.byref(shape), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(y), _ptr(gate), _ptr(up),
-                             _ptr(workspace), _stream()))
+    _call(lib().hf_gated_ff, shape, _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(y), _ptr(gate), _ptr(up), _ptr(workspace))
 
 
 def hf_gated_ff_backward(shape, dy, x, w_gate, w_up, w_down, gate, up, dx, dw_gate, dw_up, dw_down, workspace):
-    _check(lib().hf_gated_ff_backward(C.byref(shape), _ptr(dy), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(gate), _ptr(up),
-                                      _ptr(dx), _ptr(dw_gate), _ptr(dw_up), _ptr(dw_down), _ptr(workspace), _stream()))
+    _call(lib().hf_gated_ff_backward, shape, _ptr(dy), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(gate), _ptr(up), _ptr(dx),
+          _ptr(dw_gate), _ptr(dw_up), _ptr(dw_down), _ptr(workspace))
 
 
 def hf_layers_status():

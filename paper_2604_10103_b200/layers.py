@@ -1,10 +1,14 @@
 """The operators of a denoiser block around the hybrid attention, on torch CUDA tensors: layer norm, rotary positions with several axes,
 gated feed-forward, forward and backward.  Each is one call of the library (include/hf.h) on the current stream; outputs and workspaces
 come from torch's allocator.  There is no fallback: a tensor the library does not take raises.
+
+The short calls are bound by the host, so the way to the library is kept short: the shapes are packed as the bytes of the C structures,
+and tensors are asked for nothing twice.
 """
 from __future__ import annotations
 
-import ctypes as C
+import functools
+import struct
 
 import torch
 
@@ -13,207 +17,282 @@ from . import binding as hf
 _TYPES = {torch.bfloat16: hf.HF_BF16, torch.float16: hf.HF_F16, torch.float32: hf.HF_F32}
 _PAIRINGS = {"adjacent": hf.HF_PAIRS_ADJACENT, "halves": hf.HF_PAIRS_HALVES}
 _ACTS = {"silu": hf.HF_ACT_SILU, "gelu_tanh": hf.HF_ACT_GELU_TANH}
+_NORM = struct.Struct("@3i6q2f").pack                       # hf_norm_shape
+_ROPE = struct.Struct("@5i4i4i2iq").pack                    # hf_rope_shape
+_ROPE_TENSOR = struct.Struct("@2P6q2i").pack                # hf_rope_tensor
+_FF = struct.Struct("@2iq3i2q").pack                        # hf_ff_shape
+_F32 = torch.float32
+_empty = torch.empty
 
 
-def _want(ok: bool, text: str):
-    if not ok:
-        raise ValueError(text)
+def _device() -> int:
+    # torch's raw getter, which has no public name, spares a microsecond a call
+    try:
+        return torch._C._cuda_getDevice()
+    except AttributeError:
+        return torch.cuda.current_device()
 
 
-def _cuda(name, t, shape=None, dtype=None):
+def _fail(text: str):
+    raise ValueError(text)
+
+
+def _here(name, t, dev):
+    if t.get_device() != dev:
+        _fail(f"{name} is on {t.device}, not on the current CUDA device")
+
+
+def _current(t) -> int:
     if not t.is_cuda:
-        raise ValueError(f"{name} is not on a CUDA device")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, not on the current device")
-    if dtype is not None and t.dtype != dtype:
-        raise ValueError(f"{name} is {t.dtype}, not {dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+        _fail(f"a tensor on {t.device}: CUDA tensors are taken")
+    return _device()
 
 
-def _type(name, t):
-    if t.dtype not in _TYPES:
-        raise ValueError(f"{name}: {t.dtype} is not taken")
-    return _TYPES[t.dtype]
+def _like(name, t, dev, shape, dtype):
+    """t on the device, of that shape and type."""
+    if t.get_device() != dev or t.dtype != dtype or t.shape != shape:
+        _here(name, t, dev)
+        _fail(f"{name} is {t.dtype} {tuple(t.shape)}: {dtype} {tuple(shape)} is taken")
+
+
+def _dense(name, t, dev, shape, dtype):
+    _like(name, t, dev, shape, dtype)
+    if not t.is_contiguous():
+        _fail(f"{name} has to be contiguous")
 
 
 def _rows(name, t):
     """t as rows of its last axis: (rows, width, elements between rows).  Raises where the rows have no common stride."""
-    width = t.shape[-1]
-    if t.dim() == 2:
-        if width > 1 and t.stride(1) != 1:
-            raise ValueError(f"{name}: the last axis has to be contiguous")
-        return t.shape[0], width, t.stride(0) if t.shape[0] > 1 else max(width, 1)
-    if t.dim() == 1:
-        return _rows(name, t[None])
-    try:
-        v = t.view(-1, width) if t.numel() else t.reshape(-1, width) if width else t.new_empty(0, 0)
-    except RuntimeError:
-        raise ValueError(f"{name}: the leading axes have no common stride") from None
-    return _rows(name, v)
+    shape = t.shape
+    n = len(shape)
+    if n == 0:
+        _fail(f"{name} has no axes")
+    width = shape[-1]
+    if n != 2:
+        rows = t.numel() // width if width else 0
+        if t.is_contiguous():
+            return rows, width, width
+        try:
+            t = t.view(rows, width)
+        except RuntimeError:
+            _fail(f"{name}: the leading axes have no common stride")
+    rows = t.shape[0]
+    stride, one = t.stride()
+    if one != 1 and width > 1:
+        _fail(f"{name}: the last axis has to be contiguous")
+    return rows, width, stride if rows > 1 else width
 
 
 # ------------------------------------------------------------------------------------------------ layer norm
-def _norm_shape(x, weight, bias, eps, weight_offset, rows_per_group):
-    rows, width, stride = _rows("x", x)
-    _want(width >= 1, "x has rows of no elements")
-    _cuda("x", x)
-    s = hf.hf_norm_shape(type=_type("x", x), width=width, rows=rows, x_stride=stride, y_stride=width, dx_stride=width,
-                         rows_per_group=rows_per_group, param_stride=width, weight_offset=weight_offset, eps=eps)
-    s.param_type = s.type
-    groups = -(-rows // rows_per_group) if rows_per_group > 0 else 1
+def _norm_params(weight, bias, dev, dtype, width, groups):
+    """Type and row stride of weight and bias."""
+    ptype, pstride = dtype, width
     for name, p in (("weight", weight), ("bias", bias)):
         if p is None:
             continue
-        _cuda(name, p)
-        _want(p.dtype in (x.dtype, torch.float32), f"{name} is {p.dtype}: x's type or float32 is taken")
-        n, w, ps = _rows(name, p)
-        _want(w == width and n == groups, f"{name} has shape {tuple(p.shape)}: {groups} rows of {width} are taken")
-        s.param_type = _TYPES[p.dtype]
-        s.param_stride = ps
-    if weight is not None and bias is not None:
-        _want(weight.dtype == bias.dtype, "weight and bias have different types")
-        _want(groups == 1 or _rows("weight", weight)[2] == _rows("bias", bias)[2], "weight and bias have different strides")
-    return s, groups
+        _here(name, p, dev)
+        n, w, stride = _rows(name, p)
+        if w != width or n != groups:
+            _fail(f"{name} has shape {tuple(p.shape)}: {groups} rows of {width} are taken")
+        if p.dtype != dtype and p.dtype != _F32:
+            _fail(f"{name} is {p.dtype}: x's type or float32 is taken")
+        if p is bias and weight is not None and (p.dtype != ptype or stride != pstride):
+            _fail("weight and bias differ in their type or their stride")
+        ptype, pstride = p.dtype, stride
+    return _TYPES[ptype], pstride
+
+
+def _norm_type(x, width):
+    if x.dtype not in _TYPES:
+        _fail(f"x is {x.dtype}: bfloat16, float16 and float32 are taken")
+    if width < 1:
+        _fail("x has rows of no elements")
+    return _TYPES[x.dtype]
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-6, weight_offset=0.0, rows_per_group=0):
     """y = (x - mean) * rstd * (weight_offset + weight) + bias over the last axis; returns (y, mean, rstd), the last two float32 [rows].
     x: bf16, f16 or f32 [..., width], rows with one common stride.  weight, bias: [width] or [1, width]; with rows_per_group > 0
     [groups, width], row r of x taking row r // rows_per_group (slices of a modulation tensor are fine); x's type or float32; or None."""
-    s, _ = _norm_shape(x, weight, bias, eps, weight_offset, rows_per_group)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    mean = torch.empty(s.rows, dtype=torch.float32, device=x.device)
-    rstd = torch.empty(s.rows, dtype=torch.float32, device=x.device)
-    hf.hf_layer_norm(s, x, weight, bias, y, mean, rstd)
+    dev = _current(x)
+    _here("x", x, dev)
+    rows, width, stride = _rows("x", x)
+    t = _norm_type(x, width)
+    pt, ps = _norm_params(weight, bias, dev, x.dtype, width, -(-rows // rows_per_group) if rows_per_group > 0 else 1)
+    y = _empty(x.shape, dtype=x.dtype, device=x.device)
+    stats = _empty((2, rows), dtype=_F32, device=x.device)
+    mean, rstd = stats.unbind(0)
+    hf.hf_layer_norm(_NORM(t, pt, width, rows, stride, width, width, rows_per_group, ps, weight_offset, eps), x, weight, bias, y, mean, rstd)
     return y, mean, rstd
+
+
+@functools.lru_cache(maxsize=256)
+def _norm_workspace(dev, shape):
+    return hf.hf_layer_norm_workspace(shape)
 
 
 def layer_norm_backward(dy, x, mean, rstd, weight=None, weight_offset=0.0, rows_per_group=0):
     """Gradients of `layer_norm`: (dx in x's type, dweight, dbias float32 [groups, width]).  mean, rstd: as the forward returned them."""
-    s, groups = _norm_shape(x, weight, None, 0.0, weight_offset, rows_per_group)
-    _cuda("dy", dy, x.shape, x.dtype)
-    _cuda("mean", mean, (s.rows,), torch.float32)
-    _cuda("rstd", rstd, (s.rows,), torch.float32)
-    _want(mean.is_contiguous() and rstd.is_contiguous(), "mean and rstd have to be contiguous")
-    s.y_stride = _rows("dy", dy)[2]
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    d_params = torch.empty((2, groups, s.width), dtype=torch.float32, device=x.device)
-    dw, db = d_params.unbind(0)
-    ws = torch.empty(hf.hf_layer_norm_workspace(s), dtype=torch.uint8, device=x.device)
-    hf.hf_layer_norm_backward(s, dy, x, mean, rstd, weight, dx, dw, db, ws)
+    dev = _current(x)
+    _here("x", x, dev)
+    rows, width, stride = _rows("x", x)
+    t = _norm_type(x, width)
+    groups = -(-rows // rows_per_group) if rows_per_group > 0 else 1
+    pt, ps = _norm_params(weight, None, dev, x.dtype, width, groups)
+    _like("dy", dy, dev, x.shape, x.dtype)
+    _dense("mean", mean, dev, (rows,), _F32)
+    _dense("rstd", rstd, dev, (rows,), _F32)
+    dx = _empty(x.shape, dtype=x.dtype, device=x.device)
+    dw, db = _empty((2, groups, width), dtype=_F32, device=x.device).unbind(0)
+    shape = _NORM(t, pt, width, rows, stride, _rows("dy", dy)[2], width, rows_per_group, ps, weight_offset, 0.0)
+    ws = _empty(_norm_workspace(dev, shape), dtype=torch.uint8, device=x.device)
+    hf.hf_layer_norm_backward(shape, dy, x, mean, rstd, weight, dx, dw, db, ws)
     return dx, dw, db
 
 
 # ------------------------------------------------------------------------------------------------ rotary positions
-def _rope(tensors, pos, tables, pairing, inverse):
-    """tensors: (x, y, rotate) with x, y [batch, tokens, heads, head_dim] of any strides, features contiguous."""
+def _rope(x, B, T, d, tensors, n, pos, tables, pairing, inverse, dev):
+    """tensors: the bytes of n hf_rope_tensor."""
     cos, sin, extents, pairs = tables
-    x = tensors[0][0]
-    B, T, _, d = x.shape
     axes = len(pairs)
-    _want(1 <= axes <= 4 and len(extents) == axes, "one to four axes, an extent and a number of pairs for each")
-    _want(pairing in _PAIRINGS, f"pairing {pairing!r} unknown")
-    n = sum(e * p for e, p in zip(extents, pairs))
-    for name, t in (("cos", cos), ("sin", sin)):
-        _cuda(name, t, (n,), torch.float32)
-        _want(t.is_contiguous(), f"{name} has to be contiguous")
-    _cuda("pos", pos, None, torch.int32)
-    _want(tuple(pos.shape) in ((T, axes), (1, T, axes), (B, T, axes)) and pos.is_contiguous(),
-          f"pos has shape {tuple(pos.shape)}: contiguous [{T}, {axes}] or [{B}, {T}, {axes}] is taken")
-    s = hf.hf_rope_shape(type=_type("x", x), batch=B, tokens=T, head_dim=d, axes=axes, pairing=_PAIRINGS[pairing], inverse=inverse,
-                         pos_batch=T * axes if pos.dim() == 3 and pos.shape[0] == B and B > 1 else 0)
-    s.pairs[:axes] = pairs
-    s.extent[:axes] = extents
-    arr = (hf.hf_rope_tensor * len(tensors))()
-    for a, (x, y, rotate) in zip(arr, tensors):
-        xs, ys = x.stride(), y.stride()
-        _want((xs[3] == 1 and ys[3] == 1) or d == 1, "the features of a head have to be contiguous")
-        a.x, a.y, a.heads, a.rotate = x.data_ptr(), y.data_ptr(), x.shape[2], rotate
-        a.x_batch, a.x_token, a.x_head = xs[0], xs[1], xs[2]
-        a.y_batch, a.y_token, a.y_head = ys[0], ys[1], ys[2]
-    hf.hf_rope_axes(s, arr, len(tensors), cos, sin, pos)
+    if not (1 <= axes <= 4 and len(extents) == axes):
+        _fail("one to four axes, an extent and a number of pairs for each")
+    if pairing not in _PAIRINGS:
+        _fail(f"pairing {pairing!r} unknown")
+    if x.dtype not in _TYPES:
+        _fail(f"{x.dtype}: bfloat16, float16 and float32 are taken")
+    entries = (sum(map(int.__mul__, extents, pairs)),)
+    _dense("cos", cos, dev, entries, _F32)
+    _dense("sin", sin, dev, entries, _F32)
+    shape = pos.shape
+    if shape != (T, axes) and shape != (1, T, axes) and shape != (B, T, axes):
+        _fail(f"pos has shape {tuple(shape)}: [{T}, {axes}] or [{B}, {T}, {axes}] is taken")
+    _dense("pos", pos, dev, shape, torch.int32)
+    rest = (0,) * (4 - axes)
+    hf.hf_rope_axes(_ROPE(_TYPES[x.dtype], B, T, d, axes, *pairs, *rest, *extents, *rest, _PAIRINGS[pairing], inverse,
+                          T * axes if B > 1 and len(shape) == 3 and shape[0] == B else 0), tensors, n, cos, sin, pos)
 
 
 def rope_axes(x, pos, tables, out=None, pairing="adjacent", inverse=False):
     """x [batch, tokens, heads, head_dim] (any strides, features contiguous) turned by its tokens' positions.  pos: int32 [tokens, axes]
     or [batch, tokens, axes]; tables: (cos, sin, extents, pairs per axis) as `rope.axis_tables` forms cos and sin, on the device.
     out: a tensor of x's shape and type with strides of its own, or x itself; None: a new one.  inverse: the backward pass."""
-    _want(x.dim() == 4, "x is [batch, tokens, heads, head_dim]")
-    _cuda("x", x)
+    dev = _current(x)
+    _here("x", x, dev)
+    if x.dim() != 4:
+        _fail("x is [batch, tokens, heads, head_dim]")
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = _empty(x.shape, dtype=x.dtype, device=x.device)
     else:
-        _cuda("out", out, x.shape, x.dtype)
-    _rope([(x, out, 1)], pos, tables, pairing, inverse)
+        _like("out", out, dev, x.shape, x.dtype)
+    B, T, H, d = x.shape
+    xb, xt, xh, x1 = x.stride()
+    yb, yt, yh, y1 = out.stride()
+    if (x1 != 1 or y1 != 1) and d > 1:
+        _fail("the features of a head have to be contiguous")
+    _rope(x, B, T, d, _ROPE_TENSOR(x.data_ptr(), out.data_ptr(), xb, xt, xh, yb, yt, yh, H, 1), 1, pos, tables, pairing, inverse, dev)
     return out
 
 
 def split_heads_rope(qkv, heads, kv_heads, pos, tables, pairing="adjacent"):
     """Rows of a fused projection [batch, tokens, (heads + 2 kv_heads) * head_dim] (row stride free) -> q, k, v [batch, heads, tokens, head_dim]
     as the hybrid attention takes them, q and k turned by their positions, in one launch."""
-    _want(qkv.dim() == 3, "qkv is [batch, tokens, (heads + 2 kv_heads) * head_dim]")
+    dev = _current(qkv)
+    _here("qkv", qkv, dev)
+    if qkv.dim() != 3:
+        _fail("qkv is [batch, tokens, (heads + 2 kv_heads) * head_dim]")
     B, T, W = qkv.shape
-    _want(heads >= 1 and kv_heads >= 1 and W % (heads + 2 * kv_heads) == 0, f"{W} columns do not divide into {heads} + 2 x {kv_heads} heads")
-    _cuda("qkv", qkv)
-    _want(W == 1 or qkv.stride(2) == 1, "the last axis has to be contiguous")
+    if heads < 1 or kv_heads < 1 or W % (heads + 2 * kv_heads):
+        _fail(f"{W} columns do not divide into {heads} + 2 x {kv_heads} heads")
+    xb, xt, one = qkv.stride()
+    if one != 1 and W > 1:
+        _fail("qkv: the last axis has to be contiguous")
     d = W // (heads + 2 * kv_heads)
-    q = torch.empty((B, heads, T, d), dtype=qkv.dtype, device=qkv.device)
-    k = torch.empty((B, kv_heads, T, d), dtype=qkv.dtype, device=qkv.device)
-    v = torch.empty((B, kv_heads, T, d), dtype=qkv.dtype, device=qkv.device)
-    xq, xk, xv = qkv.unflatten(2, (heads + 2 * kv_heads, d)).split([heads, kv_heads, kv_heads], dim=2)
-    _rope([(xq, q.transpose(1, 2), 1), (xk, k.transpose(1, 2), 1), (xv, v.transpose(1, 2), 0)], pos, tables, pairing, 0)
+    dtype, device, e = qkv.dtype, qkv.device, qkv.element_size()
+    q = _empty((B, heads, T, d), dtype=dtype, device=device)
+    k = _empty((B, kv_heads, T, d), dtype=dtype, device=device)
+    v = _empty((B, kv_heads, T, d), dtype=dtype, device=device)
+    x, td = qkv.data_ptr(), T * d
+    _rope(qkv, B, T, d, _ROPE_TENSOR(x, q.data_ptr(), xb, xt, d, heads * td, d, td, heads, 1)
+          + _ROPE_TENSOR(x + heads * d * e, k.data_ptr(), xb, xt, d, kv_heads * td, d, td, kv_heads, 1)
+          + _ROPE_TENSOR(x + (heads + kv_heads) * d * e, v.data_ptr(), xb, xt, d, kv_heads * td, d, td, kv_heads, 0), 3, pos, tables, pairing, 0, dev)
     return q, k, v
 
 
 def split_heads_rope_backward(dq, dk, dv, pos, tables, pairing="adjacent"):
     """Gradient of `split_heads_rope` with respect to the rows: [batch, tokens, (heads + 2 kv_heads) * head_dim], contiguous."""
+    dev = _current(dq)
+    _here("dq", dq, dev)
+    if dq.dim() != 4 or dk.dim() != 4:
+        _fail("dq, dk, dv are [batch, heads, tokens, head_dim]")
     B, H, T, d = dq.shape
     KV = dk.shape[1]
-    for name, t, h in (("dq", dq, H), ("dk", dk, KV), ("dv", dv, KV)):
-        _cuda(name, t, (B, h, T, d), dq.dtype)
-    out = torch.empty((B, T, (H + 2 * KV) * d), dtype=dq.dtype, device=dq.device)
-    yq, yk, yv = out.view(B, T, H + 2 * KV, d).split([H, KV, KV], dim=2)
-    _rope([(dq.transpose(1, 2), yq, 1), (dk.transpose(1, 2), yk, 1), (dv.transpose(1, 2), yv, 0)], pos, tables, pairing, 1)
+    _like("dk", dk, dev, (B, KV, T, d), dq.dtype)
+    _like("dv", dv, dev, (B, KV, T, d), dq.dtype)
+    W, e = (H + 2 * KV) * d, dq.element_size()
+    out = _empty((B, T, W), dtype=dq.dtype, device=dq.device)
+    at, parts = out.data_ptr(), b""
+    for t, h, rotate in ((dq, H, 1), (dk, KV, 1), (dv, KV, 0)):
+        xb, xh, xt, one = t.stride()
+        if one != 1 and d > 1:
+            _fail("the features of a head have to be contiguous")
+        parts += _ROPE_TENSOR(t.data_ptr(), at, xb, xt, xh, T * W, W, d, h, rotate)
+        at += h * d * e
+    _rope(dq, B, T, d, parts, 3, pos, tables, pairing, 1, dev)
     return out
 
 
 # ------------------------------------------------------------------------------------------------ gated feed-forward
-def _ff_shape(x, w_gate, w_up, w_down, act):
+def _ff_operands(x, w_gate, w_up, w_down, act):
+    """(device, type, rows, width, hidden, out_width, row stride of x) of checked operands."""
+    dev = _current(x)
+    _here("x", x, dev)
     rows, width, stride = _rows("x", x)
-    _want(act in _ACTS, f"act {act!r} unknown")
-    _cuda("x", x)
-    hidden, out_width = w_gate.shape[0], w_down.shape[0]
-    for name, w, shape in (("w_gate", w_gate, (hidden, width)), ("w_up", w_up, (hidden, width)), ("w_down", w_down, (out_width, hidden))):
-        _cuda(name, w, shape, x.dtype)
-        _want(w.is_contiguous(), f"{name} has to be contiguous")
-    return hf.hf_ff_shape(type=_type("x", x), act=_ACTS[act], rows=rows, width=width, hidden=hidden, out_width=out_width, x_stride=stride,
-                          y_stride=out_width)
+    if act not in _ACTS:
+        _fail(f"act {act!r} unknown")
+    if w_gate.dim() != 2 or w_down.dim() != 2:
+        _fail("the weights are matrices")
+    dtype, hidden, out_width = x.dtype, w_gate.shape[0], w_down.shape[0]
+    if dtype not in _TYPES:
+        _fail(f"x is {dtype}: bfloat16 and float16 are taken")
+    _dense("w_gate", w_gate, dev, (hidden, width), dtype)
+    _dense("w_up", w_up, dev, (hidden, width), dtype)
+    _dense("w_down", w_down, dev, (out_width, hidden), dtype)
+    return dev, _TYPES[dtype], rows, width, hidden, out_width, stride
+
+
+@functools.lru_cache(maxsize=256)
+def _ff_workspace(dev, shape, backward):
+    return hf.hf_gated_ff_workspace(shape, backward)
 
 
 def gated_ff(x, w_gate, w_up, w_down, act="silu", save=False):
     """y = (act(x w_gate^T) * (x w_up^T)) w_down^T.  x bf16 or f16 [..., width], rows with one common stride; w_gate, w_up [hidden, width],
     w_down [out_width, hidden] contiguous; act "silu" or "gelu_tanh".  save: returns (y, gate, up), the last two [rows, hidden] for
     `gated_ff_backward`; otherwise y alone."""
-    s = _ff_shape(x, w_gate, w_up, w_down, act)
-    y = torch.empty(x.shape[:-1] + (s.out_width,), dtype=x.dtype, device=x.device)
-    gate = torch.empty((s.rows, s.hidden), dtype=x.dtype, device=x.device) if save else None
-    up = torch.empty((s.rows, s.hidden), dtype=x.dtype, device=x.device) if save else None
-    ws = torch.empty(hf.hf_gated_ff_workspace(s, 0), dtype=torch.uint8, device=x.device)
-    hf.hf_gated_ff(s, x, w_gate, w_up, w_down, y, gate, up, ws)
+    dev, t, rows, width, hidden, out_width, stride = _ff_operands(x, w_gate, w_up, w_down, act)
+    dtype, device = x.dtype, x.device
+    y = _empty(x.shape[:-1] + (out_width,), dtype=dtype, device=device)
+    gate = _empty((rows, hidden), dtype=dtype, device=device) if save else None
+    up = _empty((rows, hidden), dtype=dtype, device=device) if save else None
+    shape = _FF(t, _ACTS[act], rows, width, hidden, out_width, stride, out_width)
+    ws = _empty(_ff_workspace(dev, shape, 0), dtype=torch.uint8, device=device)
+    hf.hf_gated_ff(shape, x, w_gate, w_up, w_down, y, gate, up, ws)
     return (y, gate, up) if save else y
 
 
 def gated_ff_backward(dy, x, w_gate, w_up, w_down, gate, up, act="silu"):
     """Gradients of `gated_ff`: (dx, dw_gate, dw_up, dw_down) in x's type.  gate, up: as the forward returned them."""
-    s = _ff_shape(x, w_gate, w_up, w_down, act)
-    _cuda("dy", dy, tuple(x.shape[:-1]) + (s.out_width,), x.dtype)
-    for name, t in (("gate", gate), ("up", up)):
-        _cuda(name, t, (s.rows, s.hidden), x.dtype)
-        _want(t.is_contiguous(), f"{name} has to be contiguous")
-    s.y_stride = _rows("dy", dy)[2]
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    dwg, dwu, dwd = torch.empty_like(w_gate), torch.empty_like(w_up), torch.empty_like(w_down)
-    ws = torch.empty(hf.hf_gated_ff_workspace(s, 1), dtype=torch.uint8, device=x.device)
-    hf.hf_gated_ff_backward(s, dy, x, w_gate, w_up, w_down, gate, up, dx, dwg, dwu, dwd, ws)
+    dev, t, rows, width, hidden, out_width, stride = _ff_operands(x, w_gate, w_up, w_down, act)
+    dtype, device = x.dtype, x.device
+    _like("dy", dy, dev, x.shape[:-1] + (out_width,), dtype)
+    _dense("gate", gate, dev, (rows, hidden), dtype)
+    _dense("up", up, dev, (rows, hidden), dtype)
+    dx = _empty(x.shape, dtype=dtype, device=device)
+    dwg = _empty((hidden, width), dtype=dtype, device=device)
+    dwu = _empty((hidden, width), dtype=dtype, device=device)
+    dwd = _empty((out_width, hidden), dtype=dtype, device=device)
+    shape = _FF(t, _ACTS[act], rows, width, hidden, out_width, stride, _rows("dy", dy)[2])
+    ws = _empty(_ff_workspace(dev, shape, 1), dtype=torch.uint8, device=device)
+    hf.hf_gated_ff_backward(shape, dy, x, w_gate, w_up, w_down, gate, up, dx, dwg, dwu, dwd, ws)
     return dx, dwg, dwu, dwd

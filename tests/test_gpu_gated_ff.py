@@ -4,6 +4,8 @@ Bounds.  The forward rounds h once (U |h|) and y once; g and u carry a float32 s
 act and the product pass on with factors below 1.2 and |u|.  Element by element that is U |y| + (U + ...) sum |h| |Wd|, and in the 2-norm
 two independent roundings of relative size at most U / sqrt(3) each stay below U.  The backward pass rounds dg, du, h once and each
 result once: the same two roundings."""
+import ctypes as C
+
 import pytest
 import torch
 
@@ -196,9 +198,9 @@ def test_nothing_is_written_past_the_outputs():
             return torch.full((n + 512,), 7.0, dtype=BF, device="cuda")
         sizes = dict(y=M * O, gate=M * N, up=M * N, dx=M * K, dwg=N * K, dwu=N * K, dwd=O * N)
         b = {k: guarded(n) for k, n in sizes.items()}
-        ws = [torch.full((hf.hf_gated_ff_workspace(s, k) + 1024,), 99, dtype=torch.uint8, device="cuda") for k in (0, 1)]
-        hf.hf_gated_ff(s, x, wg, wu, wd, b["y"], b["gate"], b["up"], ws[0])
-        hf.hf_gated_ff_backward(s, dy, x, wg, wu, wd, b["gate"], b["up"], b["dx"], b["dwg"], b["dwu"], b["dwd"], ws[1])
+        ws = [torch.full((hf.hf_gated_ff_workspace(C.byref(s), k) + 1024,), 99, dtype=torch.uint8, device="cuda") for k in (0, 1)]
+        hf.hf_gated_ff(C.byref(s), x, wg, wu, wd, b["y"], b["gate"], b["up"], ws[0])
+        hf.hf_gated_ff_backward(C.byref(s), dy, x, wg, wu, wd, b["gate"], b["up"], b["dx"], b["dwg"], b["dwu"], b["dwd"], ws[1])
         torch.cuda.synchronize()
         for k, n in sizes.items():
             assert (b[k][n:] == 7.0).all(), k
@@ -207,8 +209,8 @@ def test_nothing_is_written_past_the_outputs():
         assert torch.equal(b["y"][:M * O].view(M, O), y) and torch.equal(b["up"][:M * N].view(M, N), up)
         # dx alone, and the weights' gradients alone
         dx = guarded(M * K)
-        hf.hf_gated_ff_backward(s, dy, x, wg, wu, wd, gate, up, dx, None, None, None, ws[1])
+        hf.hf_gated_ff_backward(C.byref(s), dy, x, wg, wu, wd, gate, up, dx, None, None, None, ws[1])
         assert torch.equal(dx, b["dx"])
         d3 = [guarded(n) for n in (N * K, N * K, O * N)]
-        hf.hf_gated_ff_backward(s, dy, x, wg, wu, wd, gate, up, None, *d3, ws[1])
+        hf.hf_gated_ff_backward(C.byref(s), dy, x, wg, wu, wd, gate, up, None, *d3, ws[1])
         assert all(torch.equal(p, b[k]) for p, k in zip(d3, ("dwg", "dwu", "dwd")))

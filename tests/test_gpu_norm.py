@@ -1,4 +1,6 @@
 """Layer norm and its gradients against the definition in 64 bits."""
+import ctypes as C
+
 import pytest
 import torch
 
@@ -195,15 +197,15 @@ def test_in_place():
     dx, dw, db = layers.layer_norm_backward(dy, x, mean, rstd, w)
     s = hf.hf_norm_shape(type=0, param_type=0, width=768, rows=50, x_stride=768, y_stride=768, dx_stride=768, rows_per_group=0, param_stride=768,
                          weight_offset=0.0, eps=1e-6)
-    ws = torch.empty(hf.hf_layer_norm_workspace(s), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(hf.hf_layer_norm_workspace(C.byref(s)), dtype=torch.uint8, device="cuda")
     g, gw, gb = dy.clone(), torch.empty_like(dw), torch.empty_like(db)
-    hf.hf_layer_norm_backward(s, g, x, mean, rstd, w, g, gw, gb, ws)          # dx over dy
+    hf.hf_layer_norm_backward(C.byref(s), g, x, mean, rstd, w, g, gw, gb, ws)          # dx over dy
     assert torch.equal(g, dx) and torch.equal(gw, dw) and torch.equal(gb, db)
     g = dy.clone()
-    hf.hf_layer_norm_backward(s, g, x, mean, rstd, w, None, gw, gb, ws)       # the parameters' gradients alone
+    hf.hf_layer_norm_backward(C.byref(s), g, x, mean, rstd, w, None, gw, gb, ws)       # the parameters' gradients alone
     assert torch.equal(gw, dw) and torch.equal(g, dy)
-    hf.hf_layer_norm_backward(s, dy, x, mean, rstd, w, g, None, None, None)   # dx alone
+    hf.hf_layer_norm_backward(C.byref(s), dy, x, mean, rstd, w, g, None, None, None)   # dx alone
     assert torch.equal(g, dx)
     z = x.clone()
-    hf.hf_layer_norm(s, z, w, b, z, None, None)
+    hf.hf_layer_norm(C.byref(s), z, w, b, z, None, None)
     assert torch.equal(z, y)
