@@ -65,8 +65,9 @@ bool stride_ok(long long s, int bytes) { return s * bytes % 16 == 0; }
 // ------------------------------------------------------------------------------------------------ layer norm
 struct NormPlan {
     bool wide;                  // 16-byte accesses
-    int groups, nv, tpr, teams, rb, group_blocks;
+    int groups, nv, tpr, teams, group_blocks, stages, smem;
 };
+constexpr int NORM_SMEM = 232448;       // shared memory of a multiprocessor's one thread block
 
 hf_status norm_check(const hf_norm_shape* g) {
     if (g == nullptr) return fail(HF_ERR_INVALID_ARG, "shape is null");
@@ -94,22 +95,37 @@ bool norm_wide(const hf_norm_shape* g, const void* const* rows, const long long*
     return !((w || b) && norm_groups(g) > 1 && !stride_ok(g->param_stride, pe));
 }
 
-// Backward: threads a row (at most 512, so that the sums over rows of V NV columns, x and dy of `rb` rows fit in registers), rows in
-// step, thread blocks.  The number of thread blocks depends on the shape alone, as the workspace does.
+// Backward: threads a row, teams of them, thread blocks.  With 16-byte pieces a team has as few warps as its columns' sums fit in (48 columns
+// a thread; 32760 rows of 1536 bf16: 59 us, with 24 columns and two warps a team 64, with 16 and three 69); element by element, where a
+// thread's loads are many and short, eight columns a thread while there are warps.  A thread block has up to twelve warps, fewer where
+// there are not two rows a team for every multiprocessor.  The number of thread blocks depends on the shape and its alignment alone, as
+// the workspace does.
 NormPlan norm_bwd_plan(const hf_norm_shape* g, bool wide, int sms) {
     NormPlan p;
-    const int V = wide ? 16 / element_bytes(g->type) : 1;
+    const int e = element_bytes(g->type), V = wide ? 16 / e : 1;
     p.wide = wide;
     p.groups = norm_groups(g);
-    p.nv = 1;
-    while ((g->width + V * p.nv - 1) / (V * p.nv) > 512) p.nv = !wide && p.nv == 8 ? 32 : (!wide && p.nv == 1 ? 4 : 2 * p.nv);
-    p.tpr = ((g->width + V * p.nv - 1) / (V * p.nv) + 31) / 32 * 32;
-    p.teams = p.tpr <= 128 ? 256 / p.tpr : 1;
-    p.rb = p.nv * V <= 8 ? 4 : (p.nv * V <= 16 ? 2 : 1);
+    int warps = (g->width + 32 * (wide ? 48 : 8) - 1) / (32 * (wide ? 48 : 8));
+    if (warps > 12) warps = 12;
+    p.tpr = 32 * warps;
+    p.nv = (g->width + V * p.tpr - 1) / (V * p.tpr);
+    // (the instantiations)
+    if (V == 8) p.nv = p.nv <= 1 ? 1 : (p.nv <= 2 ? 2 : (p.nv <= 4 ? 4 : 6));
+    else if (V == 4) p.nv = p.nv <= 2 ? 2 : (p.nv <= 4 ? 4 : (p.nv <= 8 ? 8 : 12));
+    else p.nv = p.nv <= 8 ? 8 : (p.nv <= 24 ? 24 : 48);
     const long long rows = g->rows_per_group ? (g->rows < g->rows_per_group ? g->rows : g->rows_per_group) : g->rows;
-    const long long most = (rows + p.teams * p.rb - 1) / (p.teams * p.rb);
-    long long n = (4LL * sms + p.groups - 1) / p.groups;
-    if (n > most) n = most;
+    long long n = (sms + p.groups - 1) / p.groups;
+    p.teams = 12 / warps;
+    const long long most = (rows + 2 * n - 1) / (2 * n);
+    if (p.teams > most) p.teams = most < 1 ? 1 : (int)most;
+    const int fixed = (g->width * 4 + 15) / 16 * 16 + p.teams * NORM_TEAM_BYTES, row = p.teams * 2 * g->width * e;
+    p.stages = wide ? (NORM_SMEM - fixed) / row : 0;
+    if (p.stages > 4) p.stages = 4;
+    if (p.stages < 2) p.stages = 0;             // (rows too long for rings)
+    p.smem = fixed + p.stages * row;
+    const int join = p.teams * 2 * V * p.nv * p.tpr * 4;
+    if (join > p.smem) p.smem = join;
+    if (n > (rows + p.teams - 1) / p.teams) n = (rows + p.teams - 1) / p.teams;
     p.group_blocks = n < 1 ? 1 : (int)n;
     return p;
 }
@@ -144,34 +160,37 @@ hf_status launch_norm_of(const NormParams& p, bool wide, cudaStream_t st) {
     return launch_norm<T, 1, 32, 512>(p, st);
 }
 
-template <typename T, int V, int NV>
+template <typename T, int V, int NV, bool RING>
 hf_status launch_norm_bwd(const NormParams& p, const NormPlan& n, cudaStream_t st) {
-    const int warps = n.tpr / 32;
-    size_t smem = (size_t)2 * n.teams * n.rb * warps * sizeof(float2);
-    const size_t join = (size_t)(n.teams - 1) * 2 * V * NV * n.tpr * sizeof(float);
-    if (join > smem) smem = join;
-    k_norm_bwd<T, V, NV><<<(unsigned)((long long)n.groups * n.group_blocks), dim3(n.tpr, n.teams), smem, st>>>(p);
+    if (n.smem > 48 * 1024) HFL_CUDA(cudaFuncSetAttribute(k_norm_bwd<T, V, NV, RING>, cudaFuncAttributeMaxDynamicSharedMemorySize, NORM_SMEM));
+    k_norm_bwd<T, V, NV, RING><<<(unsigned)((long long)n.groups * n.group_blocks), dim3(n.tpr, n.teams), n.smem, st>>>(p);
     HFL_CUDA(cudaGetLastError());
-    if (n.group_blocks > 1 && (p.dw || p.db)) {
-        k_norm_bwd_sum<<<dim3((p.width + 31) / 32, n.groups), dim3(32, 16), 0, st>>>(p.partials, n.group_blocks, p.width, p.dw, p.db);
-        HFL_CUDA(cudaGetLastError());
-    }
+    if (n.group_blocks > 1 && (p.dw || p.db))
+        HFL_TRY(launch_after(k_norm_bwd_sum, dim3((p.width + 31) / 32, 2 * n.groups), dim3(32, 32), 0, st, (const float*)p.partials, n.group_blocks,
+                             p.width, p.dw, p.db));
     return HF_OK;
+}
+template <typename T, bool RING>
+hf_status launch_norm_bwd_wide(const NormParams& p, const NormPlan& n, cudaStream_t st) {
+    if constexpr (sizeof(T) == 2) {
+        if (n.nv == 1) return launch_norm_bwd<T, 8, 1, RING>(p, n, st);
+        if (n.nv == 2) return launch_norm_bwd<T, 8, 2, RING>(p, n, st);
+        if (n.nv == 4) return launch_norm_bwd<T, 8, 4, RING>(p, n, st);
+        return launch_norm_bwd<T, 8, 6, RING>(p, n, st);
+    } else {
+        if (n.nv == 2) return launch_norm_bwd<T, 4, 2, RING>(p, n, st);
+        if (n.nv == 4) return launch_norm_bwd<T, 4, 4, RING>(p, n, st);
+        if (n.nv == 8) return launch_norm_bwd<T, 4, 8, RING>(p, n, st);
+        return launch_norm_bwd<T, 4, 12, RING>(p, n, st);
+    }
 }
 template <typename T>
 hf_status launch_norm_bwd_of(const NormParams& p, const NormPlan& n, cudaStream_t st) {
-    constexpr int V = 16 / sizeof(T);
-    if (n.wide) {
-        if (n.nv == 1) return launch_norm_bwd<T, V, 1>(p, n, st);
-        if (n.nv == 2) return launch_norm_bwd<T, V, 2>(p, n, st);
-        if (n.nv == 4) return launch_norm_bwd<T, V, 4>(p, n, st);
-        if constexpr (V == 4) return launch_norm_bwd<T, V, 8>(p, n, st);
-        return fail(HF_ERR_SHAPE, "width %d too large", p.width);
-    }
-    if (n.nv == 1) return launch_norm_bwd<T, 1, 1>(p, n, st);
-    if (n.nv == 4) return launch_norm_bwd<T, 1, 4>(p, n, st);
-    if (n.nv == 8) return launch_norm_bwd<T, 1, 8>(p, n, st);
-    return launch_norm_bwd<T, 1, 32>(p, n, st);
+    if (n.stages) return launch_norm_bwd_wide<T, true>(p, n, st);
+    if (n.wide) return launch_norm_bwd<T, 16 / sizeof(T), 48 * sizeof(T) / 16, false>(p, n, st);       // (only rows of over 9216 elements are too long for rings)
+    if (n.nv == 8) return launch_norm_bwd<T, 1, 8, false>(p, n, st);
+    if (n.nv == 24) return launch_norm_bwd<T, 1, 24, false>(p, n, st);
+    return launch_norm_bwd<T, 1, 48, false>(p, n, st);
 }
 
 // ------------------------------------------------------------------------------------------------ rotary positions
@@ -179,8 +198,9 @@ template <typename T, int V, bool HALVES, bool WIDE>
 hf_status launch_rope(RopeParams& p, int sms, cudaStream_t st) {
     p.units = p.head_dim / (2 * V);
     const long long threads = (long long)p.batch * p.tokens * p.units, blocks = (threads + 255) / 256;
-    // Heads are cut into slices until there are about eight thread blocks a multiprocessor, each with four heads at least.
-    int slices = (int)((8LL * sms + blocks - 1) / blocks);
+    // Heads are cut into slices while all thread blocks still run at once (four a multiprocessor), each with six heads at least: the angles
+    // are looked up once a slice.
+    int slices = (int)(4LL * sms / blocks);
     const int most = (p.total_heads + 3) / 4;
     p.slices = slices < 1 ? 1 : (slices > most ? most : slices);
     k_rope_axes<T, V, HALVES, WIDE><<<dim3((unsigned)blocks, p.slices), 256, 0, st>>>(p);
@@ -269,6 +289,7 @@ hf_status hf_layer_norm_backward(const hf_norm_shape* g, const void* dy, const v
     p.rows = g->rows; p.x_stride = g->x_stride; p.y_stride = g->y_stride; p.dx_stride = g->dx_stride;
     p.rows_per_group = g->rows_per_group; p.param_stride = g->param_stride;
     p.width = g->width; p.params_f32 = g->param_type == HF_F32; p.weight_offset = g->weight_offset; p.eps = g->eps; p.group_blocks = n.group_blocks;
+    p.stages = n.stages; p.dev_status = d->status;
     if (g->type == HF_BF16) return launch_norm_bwd_of<bf16>(p, n, st);
     if (g->type == HF_F16) return launch_norm_bwd_of<__half>(p, n, st);
     return launch_norm_bwd_of<float>(p, n, st);

@@ -19,6 +19,20 @@ hf_status current_device(const Device** out);
 inline int element_bytes(int type) { return type == HF_F32 ? 4 : 2; }
 inline bool aligned(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
+// Launch of a kernel that may start while the one before it in the stream still runs (it calls pdl_wait() before it touches what that
+// kernel wrote).
+template <typename... P, typename... A>
+hf_status launch_after(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cfg.attrs = &attr; cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
+    return e == cudaSuccess ? HF_OK : fail(HF_ERR_CUDA, "cudaLaunchKernelEx: %s", cudaGetErrorString(e));
+}
+
 }  // namespace hf_layers
 
 #define HFL_TRY(expr) do { hf_status s_ = (expr); if (s_ != HF_OK) return s_; } while (0)

@@ -6,6 +6,9 @@
 // differences from the mean, not a difference of two large sums.  Memory bounds all of it.
 #pragma once
 #include "k_vec.cuh"
+#include "tc5_common.cuh"
+
+constexpr int NORM_TEAM_BYTES = 64 + 2 * 12 * 8;          // backward, per team: up to 8 barriers, two buffers of sums of up to 12 warps
 
 struct NormParams {
     const void* x; void* y;                 // forward; backward: y = dx
@@ -19,19 +22,19 @@ struct NormParams {
     int params_f32;                         // w, b are float32, not of x's type
     float weight_offset, eps;
     int group_blocks;                       // backward: thread blocks per group
+    int stages;                             // ... sets of rows in the ring
+    int* dev_status;
 };
 
 // V parameters from column col of row g on.
 template <typename T, int V>
 __device__ __forceinline__ void norm_params(const void* base, bool f32, long long row_at, int col, float (&out)[V]) {
     if (f32) {
-        const Vec<float, V> p = *reinterpret_cast<const Vec<float, V>*>(static_cast<const float*>(base) + row_at + col);
-#pragma unroll
-        for (int j = 0; j < V; ++j) out[j] = p.v[j];
+        const Vec<float, V> p = load_vec<float, V>(static_cast<const float*>(base) + row_at + col);
+        to_floats(p, out);
     } else {
-        const Vec<T, V> p = *reinterpret_cast<const Vec<T, V>*>(static_cast<const T*>(base) + row_at + col);
-#pragma unroll
-        for (int j = 0; j < V; ++j) out[j] = to_float(p.v[j]);
+        const Vec<T, V> p = load_vec<T, V>(static_cast<const T*>(base) + row_at + col);
+        to_floats(p, out);
     }
 }
 
@@ -55,8 +58,9 @@ __device__ __forceinline__ float row_sum(float v, float* shared) {
 }
 
 // TPR threads share a row and hold V NV elements of it each.  TPR 32: eight rows a thread block of eight warps; otherwise one row.
+// The row stays packed (at most 64 registers a thread for the row lengths of models, so that 4736 rows are at work at a time).
 template <typename T, int V, int NV, int TPR>
-__global__ void __launch_bounds__(TPR == 32 ? 256 : TPR)
+__global__ void __launch_bounds__(TPR == 32 ? 256 : TPR, TPR == 32 ? 4 : (TPR == 128 && NV <= 4 ? 8 : 1))
 k_norm(const NormParams p) {
     __shared__ float s_sum[2][TPR / 32];
     const int t = TPR == 32 ? threadIdx.x & 31 : threadIdx.x;
@@ -68,25 +72,35 @@ k_norm(const NormParams p) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int col = (i * TPR + t) * V;
-        if (col < p.width) xv[i] = *reinterpret_cast<const Vec<T, V>*>(x + col);
+        if (col < p.width) xv[i] = load_vec<T, V>(x + col);
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i)
-        if ((i * TPR + t) * V < p.width)
+        if ((i * TPR + t) * V < p.width) {
+            float f[V];
+            to_floats(xv[i], f);
 #pragma unroll
-            for (int j = 0; j < V; ++j) s += to_float(xv[i].v[j]);
+            for (int j = 0; j < V; ++j) s += f[j];
+        }
     const float mean = row_sum<TPR>(s, s_sum[0]) / (float)p.width;
     s = 0.f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-        if ((i * TPR + t) * V < p.width)
+    for (int i = 0; i < NV; ++i) stay_packed(xv[i]);
 #pragma unroll
-            for (int j = 0; j < V; ++j) { const float c = to_float(xv[i].v[j]) - mean; s = fmaf(c, c, s); }
+    for (int i = 0; i < NV; ++i)
+        if ((i * TPR + t) * V < p.width) {
+            float f[V];
+            to_floats(xv[i], f);
+#pragma unroll
+            for (int j = 0; j < V; ++j) { const float c = f[j] - mean; s = fmaf(c, c, s); }
+        }
     const float rstd = 1.f / sqrtf(row_sum<TPR>(s, s_sum[1]) / (float)p.width + p.eps);
     if (t == 0) {
         if (p.mean) p.mean[row] = mean;
         if (p.rstd) p.rstd[row] = rstd;
     }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) stay_packed(xv[i]);
     const long long at = p.rows_per_group ? row / p.rows_per_group * p.param_stride : 0;
     T* y = static_cast<T*>(p.y) + row * p.y_stride;
 #pragma unroll
@@ -103,176 +117,193 @@ k_norm(const NormParams p) {
         }
         if (p.b) norm_params<T, V>(p.b, p.params_f32, at, col, b);
         Vec<T, V> o;
+        float f[V];
+        to_floats(xv[i], f);
 #pragma unroll
-        for (int j = 0; j < V; ++j) o.v[j] = from_float<T>(fmaf((to_float(xv[i].v[j]) - mean) * rstd, a[j], b[j]));
-        *reinterpret_cast<Vec<T, V>*>(y + col) = o;
+        for (int j = 0; j < V; ++j) f[j] = fmaf((f[j] - mean) * rstd, a[j], b[j]);
+        from_floats(o, f);
+        store_vec(y + col, o);
     }
 }
 
-// Rows that a thread holds at a time: their loads are in flight together, and they share one barrier.
-template <int NV, int V> __host__ __device__ constexpr int norm_bwd_rows() { return NV * V <= 8 ? 4 : (NV * V <= 16 ? 2 : 1); }
-
 // grid groups x thread blocks per group, block (tpr, teams): a team of tpr threads shares a row, each thread V NV columns of it, the same
-// ones in every row, so that the sums over rows stay in its registers; at the end the teams' sums are added in shared memory, in order,
-// and a thread block writes one partial of the group's dw and db (the only one: dw and db themselves).  The teams walk in step.
-template <typename T, int V, int NV>
-__global__ void __launch_bounds__(512)
+// ones in every row, so that the sums over rows stay in its registers (2 V NV of them, at most 96); at the end the teams' sums are added in
+// shared memory, in order, and a thread block writes one partial of the group's dw and db (the only one: dw and db themselves).  A row is
+// read twice, for its sums and for dx, from where it lies: RING (16-byte pieces): each team has a ring of `stages` rows of x and dy in
+// shared memory, filled by bulk copies, so memory's latency is hidden whatever the registers allow; otherwise from global memory, the
+// second time out of the caches.  A team of one warp (rows of up to 1536 16-bit elements) needs no barrier.
+template <typename T, int V, int NV, bool RING>
+__global__ void __launch_bounds__(384, 1)
 k_norm_bwd(const NormParams p) {
-    constexpr int RB = norm_bwd_rows<NV, V>();
-    extern __shared__ float s_dyn[];            // [2][teams][RB][warps of a team] float2, then (the same memory) [teams - 1][2][V NV tpr]
+    extern __shared__ __align__(16) uint8_t s_raw[];    // factors [width] | per team: barriers, sums | rings; at the end the teams' sums
     const int t = threadIdx.x, tpr = blockDim.x, team = threadIdx.y, teams = blockDim.y, warps = tpr >> 5;
     const int nb = p.group_blocks, slot = blockIdx.x % nb;
     const long long g = blockIdx.x / nb, g0 = p.rows_per_group ? g * p.rows_per_group : 0;
     const long long g1 = p.rows_per_group ? min(p.rows, g0 + p.rows_per_group) : p.rows;
-    const long long at = g * p.param_stride;
     const float inv = 1.f / (float)p.width;
-    float accw[NV][V], accb[NV][V], a[NV][V];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-#pragma unroll
-        for (int j = 0; j < V; ++j) { accw[i][j] = 0.f; accb[i][j] = 0.f; a[i][j] = 1.f; }
-        const int col = (i * tpr + t) * V;
-        if (p.w && col < p.width) {
-            norm_params<T, V>(p.w, p.params_f32, at, col, a[i]);
-#pragma unroll
-            for (int j = 0; j < V; ++j) a[i][j] += p.weight_offset;
-        }
+    const int factor_bytes = (p.width * 4 + 15) / 16 * 16;
+    float* s_a = reinterpret_cast<float*>(s_raw);
+    uint8_t* s_team = s_raw + factor_bytes + team * NORM_TEAM_BYTES;
+    float2* s_sum = reinterpret_cast<float2*>(s_team + 64);             // [2][warps of the team]
+    const uint32_t row_bytes = p.width * sizeof(T);
+    uint8_t* s_ring = s_raw + factor_bytes + teams * NORM_TEAM_BYTES + (size_t)team * p.stages * 2 * row_bytes;
+    const uint32_t bar = smem_u32(s_team), ring = smem_u32(s_ring);
+    const long long first = g0 + (long long)slot * teams, step = (long long)nb * teams;     // the thread block's rows, one for each team
+    // one thread of the team: the copies of a row into stage s
+    auto load = [&](long long row, int s) {
+        tc5::mbar_expect_tx(bar + 8 * s, 2 * row_bytes);
+        tc5::bulk_load(ring + 2 * s * row_bytes, static_cast<const T*>(p.x) + row * p.x_stride, row_bytes, bar + 8 * s);
+        tc5::bulk_load(ring + (2 * s + 1) * row_bytes, static_cast<const T*>(p.dy) + row * p.y_stride, row_bytes, bar + 8 * s);
+    };
+    if (RING && t == 0) {
+        for (int s = 0; s < p.stages; ++s) tc5::mbar_init(bar + 8 * s, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+        for (int s = 0; s < p.stages && first + team + s * step < g1; ++s) load(first + team + s * step, s);
     }
-    float2* s_sum = reinterpret_cast<float2*>(s_dyn);
-    int buf = 0;
-    for (long long r0 = g0 + (long long)slot * teams * RB; r0 < g1; r0 += (long long)nb * teams * RB, buf ^= 1) {
-        Vec<T, V> xv[RB][NV], dv[RB][NV];
-        float mean[RB], rstd[RB];
-        float2 s[RB];
+    // (V 8: the first and the second four of a thread's eight columns apart, so that neighbouring threads read neighbouring 16 bytes)
+    for (int c = team * tpr + t; c < p.width; c += teams * tpr) {
+        float a[1] = {1.f};
+        if (p.w) { norm_params<T, 1>(p.w, p.params_f32, g * p.param_stride, c, a); a[0] += p.weight_offset; }
+        s_a[V == 8 ? (c >> 2 & 1) * (p.width / 2) + (c >> 3) * 4 + (c & 3) : c] = a[0];
+    }
+    __syncthreads();
+    auto load_factors = [&](int col, float (&a)[V]) {
+        if constexpr (V == 8) {
+            const float4 lo = *reinterpret_cast<const float4*>(s_a + col / 2), hi = *reinterpret_cast<const float4*>(s_a + p.width / 2 + col / 2);
+            a[0] = lo.x; a[1] = lo.y; a[2] = lo.z; a[3] = lo.w; a[4] = hi.x; a[5] = hi.y; a[6] = hi.z; a[7] = hi.w;
+        } else
+            to_floats(load_vec<float, V>(s_a + col), a);
+    };
+    float accw[NV][V], accb[NV][V];
 #pragma unroll
-        for (int k = 0; k < RB; ++k) {
-            const long long row = r0 + k * teams + team;
-            const bool on = row < g1;
-            mean[k] = on ? p.mean[row] : 0.f;
-            rstd[k] = on ? p.rstd[row] : 0.f;
-            const T* x = static_cast<const T*>(p.x) + row * p.x_stride;
-            const T* dy = static_cast<const T*>(p.dy) + row * p.y_stride;
+    for (int i = 0; i < NV; ++i)
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int col = (i * tpr + t) * V;
-                if (on && col < p.width) {
-                    xv[k][i] = *reinterpret_cast<const Vec<T, V>*>(x + col);
-                    dv[k][i] = *reinterpret_cast<const Vec<T, V>*>(dy + col);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < V; ++j) { xv[k][i].v[j] = from_float<T>(0.f); dv[k][i].v[j] = from_float<T>(0.f); }
+        for (int j = 0; j < V; ++j) { accw[i][j] = 0.f; accb[i][j] = 0.f; }
+    float mean_next = 0.f, rstd_next = 0.f;             // one row ahead
+    if (first + team < g1) { mean_next = p.mean[first + team]; rstd_next = p.rstd[first + team]; }
+    int stage = 0, buf = 0;
+    uint32_t phase = 0;
+    long long before = -1;                              // the row before, whose stage is read no more once the team has met
+    int before_stage = 0;
+    for (long long r0 = first; r0 < g1; r0 += step, buf ^= 1) {         // (the teams walk in step)
+        const long long row = r0 + team;
+        const bool on = row < g1;
+        const float rstd = rstd_next, neg = -mean_next * rstd;          // xhat = x rstd + neg
+        if (row + step < g1) { mean_next = p.mean[row + step]; rstd_next = p.rstd[row + step]; }
+        const T* x = static_cast<const T*>(p.x) + row * p.x_stride;
+        const T* dy = static_cast<const T*>(p.dy) + row * p.y_stride;
+        if constexpr (RING) {
+            x = reinterpret_cast<const T*>(s_ring + 2 * stage * row_bytes);
+            dy = reinterpret_cast<const T*>(s_ring + (2 * stage + 1) * row_bytes);
+            // bounded like every wait: a row that never came would leave garbage, and the flag
+            if (on && !tc5::mbar_try_wait(bar + 8 * stage, phase)) {
+                const long long t0 = clock64();
+                while (!tc5::mbar_try_wait(bar + 8 * stage, phase) && clock64() - t0 < tc5::WAIT_LIMIT_CYCLES) {}
+                if (clock64() - t0 >= tc5::WAIT_LIMIT_CYCLES) {
+                    atomicOr(p.dev_status, HF_DEV_TIMEOUT_FLAG);
+                    atomicExch(p.dev_status + 1, 91);
                 }
             }
         }
+        float s1[V], s2[V];
 #pragma unroll
-        for (int k = 0; k < RB; ++k) {
-            s[k] = make_float2(0.f, 0.f);
+        for (int j = 0; j < V; ++j) { s1[j] = 0.f; s2[j] = 0.f; }
+        if (on) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float xh = (to_float(xv[k][i].v[j]) - mean[k]) * rstd[k], d = to_float(dv[k][i].v[j]), gh = d * a[i][j];
-                    accw[i][j] = fmaf(d, xh, accw[i][j]);
-                    accb[i][j] += d;
-                    s[k].x += gh;
-                    s[k].y = fmaf(gh, xh, s[k].y);
-                }
-            s[k].x = warp_sum(s[k].x);
-            s[k].y = warp_sum(s[k].y);
+            for (int i = 0; i < NV; ++i) {
+                const int col = (i * tpr + t) * V;
+                if (col >= p.width) continue;
+                float xf[V], d[V], gh[V], a[V];
+                to_floats(load_vec<T, V>(x + col), xf);
+                to_floats(load_vec<T, V>(dy + col), d);
+                load_factors(col, a);
+                vfma(xf, xf, rstd, neg);
+                vmul(gh, d, a);
+                vfma(accw[i], d, xf, accw[i]);
+                vadd(accb[i], d);
+                vadd(s1, gh);
+                vfma(s2, gh, xf, s2);
+            }
         }
+        float m1 = warp_sum(vsum(s1)), m2 = warp_sum(vsum(s2));
         if (tpr > 32) {
             // (two buffers in turn: a warp that writes one has passed the barrier behind which the others read the other)
-            float2* own = s_sum + (size_t)((buf * teams + team) * RB) * warps;
-            if ((t & 31) == 0)
-#pragma unroll
-                for (int k = 0; k < RB; ++k) own[k * warps + (t >> 5)] = s[k];
+            float2* own = s_sum + buf * warps;
+            if ((t & 31) == 0) own[t >> 5] = make_float2(m1, m2);
             __syncthreads();
-#pragma unroll
-            for (int k = 0; k < RB; ++k) {
-                s[k] = make_float2(0.f, 0.f);
-                for (int w = 0; w < warps; ++w) { const float2 o = own[k * warps + w]; s[k].x += o.x; s[k].y += o.y; }
-            }
+            m1 = 0.f; m2 = 0.f;
+            for (int w = 0; w < warps; ++w) { const float2 o = own[w]; m1 += o.x; m2 += o.y; }
         }
-        if (p.y == nullptr) continue;
+        if constexpr (RING) {                           // (behind the sums every thread of the team has left the row before)
+            if (t == 0 && before >= 0 && before + p.stages * step < g1) load(before + p.stages * step, before_stage);
+            before = row; before_stage = stage;
+            if (++stage == p.stages) { stage = 0; phase ^= 1; }
+        }
+        if (!on || p.y == nullptr) continue;
+        // dx = rstd gh - rstd m1 - xhat rstd m2
+        const float c1 = -m1 * inv * rstd, c2 = -m2 * inv * rstd;
+        T* dx = static_cast<T*>(p.y) + row * p.dx_stride;
 #pragma unroll
-        for (int k = 0; k < RB; ++k) {
-            const long long row = r0 + k * teams + team;
-            T* dx = static_cast<T*>(p.y) + row * p.dx_stride;
-            const float m1 = s[k].x * inv, m2 = s[k].y * inv;
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int col = (i * tpr + t) * V;
-                if (row >= g1 || col >= p.width) continue;
-                Vec<T, V> o;
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float xh = (to_float(xv[k][i].v[j]) - mean[k]) * rstd[k], gh = to_float(dv[k][i].v[j]) * a[i][j];
-                    o.v[j] = from_float<T>(rstd[k] * (gh - m1 - xh * m2));
-                }
-                *reinterpret_cast<Vec<T, V>*>(dx + col) = o;
-            }
+        for (int i = 0; i < NV; ++i) {
+            const int col = (i * tpr + t) * V;
+            if (col >= p.width) continue;
+            float xf[V], d[V], a[V];
+            to_floats(load_vec<T, V>(x + col), xf);
+            to_floats(load_vec<T, V>(dy + col), d);
+            load_factors(col, a);
+            vfma(xf, xf, rstd, neg);
+            vmul(d, d, a);
+            vfma(xf, xf, c2, c1);
+            vfma(xf, d, rstd, xf);
+            Vec<T, V> o;
+            from_floats(o, xf);
+            store_vec(dx + col, o);
         }
     }
     if (p.dw == nullptr && p.db == nullptr) return;
-    // the teams' sums, one after the other
+    // the teams' sums: all to shared memory, then added column by column
     const int cols = V * NV * tpr;
-    if (teams > 1) {
-        __syncthreads();
-        if (team > 0)
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    float* o = s_dyn + (size_t)(team - 1) * 2 * cols + (i * V + j) * tpr + t;
-                    o[0] = accw[i][j];
-                    o[cols] = accb[i][j];
-                }
-        __syncthreads();
-        if (team > 0) return;
-        for (int q = 0; q < teams - 1; ++q)
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float* o = s_dyn + (size_t)q * 2 * cols + (i * V + j) * tpr + t;
-                    accw[i][j] += o[0];
-                    accb[i][j] += o[cols];
-                }
-    }
-    const bool direct = nb == 1;
-    float* ow = direct ? p.dw + g * p.width : p.partials + (long long)blockIdx.x * 2 * p.width;
-    float* ob = direct ? p.db + g * p.width : ow + p.width;
+    float* s_join = reinterpret_cast<float*>(s_raw);
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const int col = (i * tpr + t) * V + j;
-            if (col >= p.width) continue;
-            if (p.dw || !direct) ow[col] = accw[i][j];
-            if (p.db || !direct) ob[col] = accb[i][j];
+            float* o = s_join + (size_t)team * 2 * cols + (i * V + j) * tpr + t;
+            o[0] = accw[i][j];
+            o[cols] = accb[i][j];
         }
+    __syncthreads();
+    const bool direct = nb == 1;
+    for (int e = team * tpr + t; e < 2 * cols; e += teams * tpr) {
+        const int which = e >= cols, at = e - which * cols, ij = at / tpr, tt = at - ij * tpr;
+        const int col = (ij / V * tpr + tt) * V + ij % V;
+        if (col >= p.width) continue;
+        float v = 0.f;
+        for (int q = 0; q < teams; ++q) v += s_join[(size_t)q * 2 * cols + e];
+        float* out = direct ? (which ? p.db : p.dw) : p.partials;
+        if (out) out[direct ? g * p.width + col : ((long long)blockIdx.x * 2 + which) * p.width + col] = v;
+    }
 }
 
-// dw, db [groups, width] from the partials [groups, n, 2, width], always in the same order: 16 threads a column, then their sums.
-__global__ void __launch_bounds__(512)
+// dw, db [groups, width] from the partials [groups, n, 2, width], always in the same order: 32 threads a column, then their sums.  blockIdx.y:
+// group x (dw or db).
+__global__ void __launch_bounds__(1024)
 k_norm_bwd_sum(const float* partials, int n, int width, float* dw, float* db) {
-    __shared__ float s[2][16][33];
-    const int col = blockIdx.x * 32 + threadIdx.x;
-    const float* src = partials + (size_t)blockIdx.y * n * 2 * width;
-    float a = 0.f, b = 0.f;
-    if (col < width)
-        for (int i = threadIdx.y; i < n; i += 16) {
-            a += src[(size_t)i * 2 * width + col];
-            b += src[(size_t)i * 2 * width + width + col];
-        }
-    s[0][threadIdx.y][threadIdx.x] = a;
-    s[1][threadIdx.y][threadIdx.x] = b;
-    __syncthreads();
-    if (threadIdx.y < 2 && col < width) {
-        float v = 0.f;
-#pragma unroll
-        for (int q = 0; q < 16; ++q) v += s[threadIdx.y][q][threadIdx.x];
-        float* out = threadIdx.y ? db : dw;
-        if (out) out[(size_t)blockIdx.y * width + col] = v;
+    __shared__ float s[32][33];
+    pdl_wait();
+    const int col = blockIdx.x * 32 + threadIdx.x, g = blockIdx.y >> 1, which = blockIdx.y & 1;
+    float* out = which ? db : dw;
+    if (out == nullptr) return;
+    const float* src = partials + ((size_t)g * n * 2 + which) * width + col;
+    float a = 0.f;
+    if (col < width) {
+#pragma unroll 4
+        for (int i = threadIdx.y; i < n; i += 32) a += src[(size_t)i * 2 * width];
     }
+    s[threadIdx.y][threadIdx.x] = a;
+    __syncthreads();
+    // warp y adds column y's 32 sums
+    const float v = warp_sum(s[threadIdx.x][threadIdx.y]);
+    if (threadIdx.x == 0 && blockIdx.x * 32 + threadIdx.y < width) out[(size_t)g * width + blockIdx.x * 32 + threadIdx.y] = v;
 }

@@ -79,37 +79,44 @@ k_rope_axes(const RopeParams p) {
             for (int k = 0; k < HB; ++k)
                 if (h + k < stop) {
                     if constexpr (HALVES || !WIDE) {
-                        lo[k] = *reinterpret_cast<const Vec<T, V, WIDE>*>(x + k * t.xh + f0);
-                        hi[k] = *reinterpret_cast<const Vec<T, V, WIDE>*>(x + k * t.xh + f1);
+                        lo[k] = load_vec<T, V, WIDE>(x + k * t.xh + f0);
+                        hi[k] = load_vec<T, V, WIDE>(x + k * t.xh + f1);
                     } else {
-                        const Vec<T, 2 * V> v = *reinterpret_cast<const Vec<T, 2 * V>*>(x + k * t.xh + f0);
-#pragma unroll
-                        for (int j = 0; j < V; ++j) { lo[k].v[j] = v.v[j]; hi[k].v[j] = v.v[V + j]; }
+                        const Vec<T, 2 * V> v = load_vec<T, 2 * V>(x + k * t.xh + f0);
+                        memcpy(&lo[k], &v, sizeof(lo[k]));
+                        memcpy(&hi[k], reinterpret_cast<const char*>(&v) + sizeof(lo[k]), sizeof(hi[k]));
                     }
                 }
 #pragma unroll
             for (int k = 0; k < HB; ++k)
                 if (h + k < stop) {
                     if (rot) {
+                        float e[2 * V], l[V], u2[V];
+                        to_floats(lo[k], l);
+                        to_floats(hi[k], u2);
+#pragma unroll
+                        for (int j = 0; j < V; ++j) { e[j] = l[j]; e[V + j] = u2[j]; }
 #pragma unroll
                         for (int j = 0; j < V; ++j)
                             if (on[j]) {            // (an infinity behind the rotated pairs is copied, not multiplied by a zero sine)
-                                // neighbours: pair j is elements (2j, 2j + 1) of the 2 V
-                                T& e0 = HALVES ? lo[k].v[j] : (2 * j < V ? lo[k].v[2 * j % V] : hi[k].v[2 * j % V]);
-                                T& e1 = HALVES ? hi[k].v[j] : (2 * j + 1 < V ? lo[k].v[(2 * j + 1) % V] : hi[k].v[(2 * j + 1) % V]);
-                                const float x0 = to_float(e0), x1 = to_float(e1);
-                                e0 = from_float<T>(x0 * c[j] - x1 * s[j]);
-                                e1 = from_float<T>(x0 * s[j] + x1 * c[j]);
+                                const int i0 = HALVES ? j : 2 * j, i1 = HALVES ? V + j : 2 * j + 1;     // neighbours: pair j is elements (2j, 2j + 1)
+                                const float x0 = e[i0], x1 = e[i1];
+                                e[i0] = x0 * c[j] - x1 * s[j];
+                                e[i1] = x0 * s[j] + x1 * c[j];
                             }
+#pragma unroll
+                        for (int j = 0; j < V; ++j) { l[j] = e[j]; u2[j] = e[V + j]; }
+                        from_floats(lo[k], l);
+                        from_floats(hi[k], u2);
                     }
                     if constexpr (HALVES || !WIDE) {
-                        *reinterpret_cast<Vec<T, V, WIDE>*>(y + k * t.yh + f0) = lo[k];
-                        *reinterpret_cast<Vec<T, V, WIDE>*>(y + k * t.yh + f1) = hi[k];
+                        store_vec(y + k * t.yh + f0, lo[k]);
+                        store_vec(y + k * t.yh + f1, hi[k]);
                     } else {
                         Vec<T, 2 * V> v;
-#pragma unroll
-                        for (int j = 0; j < V; ++j) { v.v[j] = lo[k].v[j]; v.v[V + j] = hi[k].v[j]; }
-                        *reinterpret_cast<Vec<T, 2 * V>*>(y + k * t.yh + f0) = v;
+                        memcpy(&v, &lo[k], sizeof(lo[k]));
+                        memcpy(reinterpret_cast<char*>(&v) + sizeof(lo[k]), &hi[k], sizeof(hi[k]));
+                        store_vec(y + k * t.yh + f0, v);
                     }
                 }
         }
