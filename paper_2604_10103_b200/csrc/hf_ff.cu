@@ -30,37 +30,78 @@ hf_status matrix_map(const Device* d, CUtensorMap* m, int type, const void* base
 
 struct Matrix { const void* p; long long rows, cols, stride; };
 
+// How a launch's products are cut: thread blocks a tile (cg), accumulator columns a tile (bn).
+struct Tiling { int cg, bn; };
+struct Size { long long rows, cols, contraction; };
+
+// The tiling of least estimated time: rounds of tiles over the device times a tile's cycles.  A block of 64 of the contraction costs the MMAs
+// 2 bn cycles, and shared memory, which takes each operand byte in and gives it out once, 2 x 128 (128 + bn / cg) bytes at 128 a cycle,
+// of which four fifths were seen to count, a little more with an MN-major B.  What was seen, us a call, of 4680 rows, width 1536, hidden
+// 4096, the other products of the call unchanged: y in tiles of one thread block x 256 columns 140.2, 192 139, 224 139; of two x 256 137,
+// 224 135, 192 141, 128 151; dx one x 256 335, one x 192 330, two x 256 321, two x 192 345; of 1560 rows g, u one x 256 63, two x 256 65; y
+// one x 160 60, two x 192 57, two x 128 68.  An MN-major B comes in boxes of 64 columns a thread block, and other widths were slower than
+// this says (dw two x 256 317, two x 224 334).  most_bn: columns for which the kernel still has four stages with one thread block a tile.
+Tiling ff_tiling(const Device* d, const Size* s, int n, int segments, bool gated, bool b_mn, int most_bn = 256) {
+    Tiling best = {1, 64};
+    double least = 1e300;
+    for (int cg = 1; cg <= 2; ++cg)
+        for (int bn = b_mn ? 64 * cg : 64; bn <= 256; bn += gated ? 64 : (b_mn ? 64 * cg : 32)) {
+            if (cg == 1 && bn > most_bn) break;
+            const int out = gated ? bn / 2 : bn, slots = cg == 1 ? d->sm_count : d->pairs;
+            long long tiles = 0;
+            double blocks = 0;
+            for (int i = 0; i < n; ++i) {
+                tiles += (s[i].rows + 128 * cg - 1) / (128 * cg) * ((s[i].cols + out - 1) / out);
+                if (blocks < (double)((s[i].contraction + 63) / 64)) blocks = (double)((s[i].contraction + 63) / 64);
+            }
+            const double mma = 2.0 * bn, memory = (b_mn ? 1.75 : 1.6) * (128 + bn / cg);
+            const double cost = (double)((tiles + slots - 1) / slots) * (blocks * segments * (mma > memory ? mma : memory) + 1500.0);
+            if (cost < least) { least = cost; best = {cg, bn}; }
+        }
+    return best;
+}
+
 // One launch being put together: operands, outputs, tiles.
 struct Launch {
     const Device* d;
     int type;
+    Tiling tiling;
     FfGemmParams p;
-    Launch(const Device* dev, int t, int act) : d(dev), type(t) {
+    Launch(const Device* dev, int t, int act, Tiling cut) : d(dev), type(t), tiling(cut) {
         memset(&p, 0, sizeof(p));
-        p.segments = 1; p.act = act; p.dev_status = dev->status;
+        p.segments = 1; p.act = act; p.dev_status = dev->status; p.bn = cut.bn;
     }
     // Contraction-contiguous (K-major) operand of `tile` rows; row-contiguous (MN-major) operand.
     hf_status k_major(CUtensorMap* m, const Matrix& x, int tile) { return matrix_map(d, m, type, x.p, x.rows, x.cols, x.stride, 64, tile); }
     hf_status mn_major(CUtensorMap* m, const Matrix& x) { return matrix_map(d, m, type, x.p, x.rows, x.cols, x.stride, 64, 64); }
-    hf_status output(int i, const Matrix& x) { return matrix_map(d, &p.out[i], type, x.p, x.rows, x.cols, x.stride, 32, 32); }
+    // What an epilogue reads or writes: boxes of 32 x 32.
+    hf_status box(CUtensorMap* m, const Matrix& x) { return matrix_map(d, m, type, x.p, x.rows, x.cols, x.stride, 32, 32); }
     void product(long long rows, int cols, long long contraction, int bn_out) {
-        const int i = p.products++;
+        const int i = p.products++, bm = 128 * tiling.cg;
         p.rows[i] = (int)rows; p.cols[i] = cols; p.kb[i] = (int)((contraction + 63) / 64);
-        const long long tiles = (rows + FfGemm::BM - 1) / FfGemm::BM * ((cols + bn_out - 1) / bn_out);
+        const long long tiles = (rows + bm - 1) / bm * ((cols + bn_out - 1) / bn_out);
         p.tile0[i + 1] = p.tile0[i] + (int)tiles;
     }
-    template <typename T, int EPI, bool A_MN, bool B_MN>
+    template <typename T, int EPI, bool A_MN, bool B_MN, int CG>
     hf_status run_t(cudaStream_t st) {
-        p.stages = FfGemm::stages_for(p.bn);
-        const int smem = FfGemm::smem_bytes(p.bn, p.stages), tiles = p.tile0[p.products];
-        HFL_CUDA(cudaFuncSetAttribute(k_ff_gemm<T, EPI, A_MN, B_MN>, cudaFuncAttributeMaxDynamicSharedMemorySize, FfGemm::SMEM_MAX));
-        k_ff_gemm<T, EPI, A_MN, B_MN><<<tiles < d->sm_count ? tiles : d->sm_count, FfGemm::THREADS, smem, st>>>(p);
-        HFL_CUDA(cudaGetLastError());
+        typedef FfGemm<EPI, CG> C;
+        p.stages = C::stages_for(p.bn);
+        auto kernel = k_ff_gemm<T, EPI, A_MN, B_MN, CG>;
+        HFL_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_MAX));
+        const int tiles = p.tile0[p.products], slots = CG == 1 ? d->sm_count : d->pairs;
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = CG; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+        cfg.gridDim = dim3(CG * (tiles < slots ? tiles : slots)); cfg.blockDim = dim3(C::THREADS);
+        cfg.dynamicSmemBytes = C::smem_bytes(p.bn, p.stages); cfg.stream = st; cfg.attrs = &attr; cfg.numAttrs = 1;
+        HFL_CUDA(cudaLaunchKernelEx(&cfg, kernel, p));
         return HF_OK;
     }
     template <int EPI, bool A_MN, bool B_MN>
     hf_status run(cudaStream_t st) {
-        return type == HF_BF16 ? run_t<bf16, EPI, A_MN, B_MN>(st) : run_t<__half, EPI, A_MN, B_MN>(st);
+        if (tiling.cg == 1) return type == HF_BF16 ? run_t<bf16, EPI, A_MN, B_MN, 1>(st) : run_t<__half, EPI, A_MN, B_MN, 1>(st);
+        return type == HF_BF16 ? run_t<bf16, EPI, A_MN, B_MN, 2>(st) : run_t<__half, EPI, A_MN, B_MN, 2>(st);
     }
 };
 
@@ -88,6 +129,23 @@ size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
 
 }  // namespace
 
+namespace hf_layers {
+// Pairs of multiprocessors that can hold a cluster of two thread blocks at a time (a persistent grid of more would run in two rounds).
+hf_status count_pairs(int* pairs) {
+    typedef FfGemm<FF_STORE, 2> C;
+    auto kernel = k_ff_gemm<bf16, FF_STORE, false, false, 2>;
+    HFL_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_MAX));
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 2; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+    cfg.gridDim = dim3(256); cfg.blockDim = dim3(C::THREADS); cfg.dynamicSmemBytes = C::SMEM_MAX; cfg.attrs = &attr; cfg.numAttrs = 1;
+    HFL_CUDA(cudaOccupancyMaxActiveClusters(pairs, kernel, &cfg));
+    if (*pairs < 1) return fail(HF_ERR_UNSUPPORTED, "the device holds no cluster of two thread blocks");
+    return HF_OK;
+}
+}  // namespace hf_layers
+
 extern "C" {
 
 hf_status hf_gated_ff_workspace(const hf_ff_shape* g, int backward, size_t* bytes) {
@@ -112,26 +170,26 @@ hf_status hf_gated_ff(const hf_ff_shape* g, const void* x, const void* w_gate, c
     const long long M = g->rows, K = g->width, N = g->hidden, O = g->out_width;
     const Matrix h = {workspace, M, N, N};
     {
-        Launch l(d, g->type, g->act);
-        const int hn = 128;
-        l.p.bn = 2 * hn;
-        HFL_TRY(l.k_major(&l.p.a[0], {x, M, K, g->x_stride}, FfGemm::BM));
+        const Size size = {M, N, K};
+        Launch l(d, g->type, g->act, ff_tiling(d, &size, 1, 1, true, false));
+        const int hn = l.p.bn / 2;
+        HFL_TRY(l.k_major(&l.p.a[0], {x, M, K, g->x_stride}, 128));
         HFL_TRY(l.k_major(&l.p.b[0], {w_gate, N, K, K}, hn));
         HFL_TRY(l.k_major(&l.p.b[1], {w_up, N, K, K}, hn));
-        HFL_TRY(l.output(0, h));
+        HFL_TRY(l.box(&l.p.out[0], h));
         if (gate) {
-            HFL_TRY(l.output(1, {gate, M, N, N}));
-            HFL_TRY(l.output(2, {up, M, N, N}));
+            HFL_TRY(l.box(&l.p.out[1], {gate, M, N, N}));
+            HFL_TRY(l.box(&l.p.out[2], {up, M, N, N}));
             l.p.save = 1;
         }
         l.product(M, N, K, hn);
         HFL_TRY((l.run<FF_GATED, false, false>(st)));
     }
-    Launch l(d, g->type, g->act);
-    l.p.bn = 256;
-    HFL_TRY(l.k_major(&l.p.a[0], h, FfGemm::BM));
-    HFL_TRY(l.k_major(&l.p.b[0], {w_down, O, N, N}, l.p.bn));
-    HFL_TRY(l.output(0, {y, M, O, g->y_stride}));
+    const Size size = {M, O, N};
+    Launch l(d, g->type, g->act, ff_tiling(d, &size, 1, 1, false, false));
+    HFL_TRY(l.k_major(&l.p.a[0], h, 128));
+    HFL_TRY(l.k_major(&l.p.b[0], {w_down, O, N, N}, l.p.bn / l.tiling.cg));
+    HFL_TRY(l.box(&l.p.out[0], {y, M, O, g->y_stride}));
     l.product(M, O, N, l.p.bn);
     return l.run<FF_STORE, false, false>(st);
 }
@@ -163,31 +221,31 @@ hf_status hf_gated_ff_backward(const hf_ff_shape* g, const void* dy, const void*
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     const Matrix mdy = {dy, M, O, g->y_stride}, mx = {x, M, K, g->x_stride}, dg = {ws, M, N, N}, du = {ws + part, M, N, N}, h = {ws + 2 * part, M, N, N};
     {
-        Launch l(d, g->type, g->act);
-        l.p.bn = 256;
-        l.p.gate = gate; l.p.up = up;
-        HFL_TRY(l.k_major(&l.p.a[0], mdy, FfGemm::BM));
+        const Size size = {M, N, O};
+        Launch l(d, g->type, g->act, ff_tiling(d, &size, 1, 1, false, true, 128));
+        HFL_TRY(l.box(&l.p.in[0], {gate, M, N, N})); HFL_TRY(l.box(&l.p.in[1], {up, M, N, N}));
+        HFL_TRY(l.k_major(&l.p.a[0], mdy, 128));
         HFL_TRY(l.mn_major(&l.p.b[0], {w_down, O, N, N}));
-        HFL_TRY(l.output(0, dg)); HFL_TRY(l.output(1, du)); HFL_TRY(l.output(2, h));
+        HFL_TRY(l.box(&l.p.out[0], dg)); HFL_TRY(l.box(&l.p.out[1], du)); HFL_TRY(l.box(&l.p.out[2], h));
         l.product(M, (int)N, O, l.p.bn);
         HFL_TRY((l.run<FF_DHIDDEN, false, true>(st)));
     }
     if (dx) {
-        Launch l(d, g->type, g->act);
-        l.p.bn = 256;
-        HFL_TRY(l.k_major(&l.p.a[0], dg, FfGemm::BM)); HFL_TRY(l.k_major(&l.p.a[1], du, FfGemm::BM));
+        const Size size = {M, K, N};
+        Launch l(d, g->type, g->act, ff_tiling(d, &size, 1, 2, false, true));
+        HFL_TRY(l.k_major(&l.p.a[0], dg, 128)); HFL_TRY(l.k_major(&l.p.a[1], du, 128));
         HFL_TRY(l.mn_major(&l.p.b[0], {w_gate, N, K, K})); HFL_TRY(l.mn_major(&l.p.b[1], {w_up, N, K, K}));
-        HFL_TRY(l.output(0, {dx, M, K, K}));
+        HFL_TRY(l.box(&l.p.out[0], {dx, M, K, K}));
         l.product(M, (int)K, N, l.p.bn);
         l.p.segments = 2; l.p.kb[1] = l.p.kb[0];
         HFL_TRY((l.run<FF_STORE, false, true>(st)));
     }
     if (n_dw) {
-        Launch l(d, g->type, g->act);
-        l.p.bn = 256;
+        const Size sizes[3] = {{N, K, M}, {N, K, M}, {O, N, M}};
+        Launch l(d, g->type, g->act, ff_tiling(d, sizes, 3, 1, false, true));
         HFL_TRY(l.mn_major(&l.p.a[0], dg)); HFL_TRY(l.mn_major(&l.p.a[1], du)); HFL_TRY(l.mn_major(&l.p.a[2], mdy));
         HFL_TRY(l.mn_major(&l.p.b[0], mx)); l.p.b[1] = l.p.b[0]; HFL_TRY(l.mn_major(&l.p.b[2], h));
-        HFL_TRY(l.output(0, {dw_gate, N, K, K})); HFL_TRY(l.output(1, {dw_up, N, K, K})); HFL_TRY(l.output(2, {dw_down, O, N, N}));
+        HFL_TRY(l.box(&l.p.out[0], {dw_gate, N, K, K})); HFL_TRY(l.box(&l.p.out[1], {dw_up, N, K, K})); HFL_TRY(l.box(&l.p.out[2], {dw_down, O, N, N}));
         l.product(N, (int)K, M, l.p.bn); l.product(N, (int)K, M, l.p.bn); l.product(O, (int)N, M, l.p.bn);
         HFL_TRY((l.run<FF_STORE, true, true>(st)));
     }

@@ -38,7 +38,7 @@ hf_status current_device(const Device** out) {
     if (!g_known[dev]) {
         std::lock_guard<std::mutex> lock(g_mutex);
         if (!g_known[dev]) {
-            Device d = {dev, 0, nullptr, nullptr};
+            Device d = {dev, 0, 0, nullptr, nullptr};
             int major = 0;
             HFL_CUDA(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev));
             if (major != 10) return fail(HF_ERR_UNSUPPORTED, "device of compute capability %d.x; this library is built for sm_100a only", major);
@@ -50,6 +50,7 @@ hf_status current_device(const Device** out) {
             e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &d.encode_tiled, cudaEnableDefault, &q);
             if (e != cudaSuccess || q != cudaDriverEntryPointSuccess || d.encode_tiled == nullptr)
                 return fail(HF_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+            HFL_TRY(count_pairs(&d.pairs));
             g_devices[dev] = d;
             g_known[dev] = true;
         }
