@@ -2,6 +2,7 @@
 #include "hf_layers.h"
 #include <type_traits>
 #include "k_ff_gemm.cuh"
+#include "k_ff_rows.cuh"
 
 #include <cstring>
 
@@ -30,8 +31,8 @@ hf_status matrix_map(const Device* d, CUtensorMap* m, int type, const void* base
 
 struct Matrix { const void* p; long long rows, cols, stride; };
 
-// How a launch's products are cut: thread blocks a tile (cg), accumulator columns a tile (bn).
-struct Tiling { int cg, bn; };
+// How a launch's products are cut: thread blocks a tile (cg), accumulator columns a tile (bn), parts of a tile's contraction (splits).
+struct Tiling { int cg, bn, splits; };
 struct Size { long long rows, cols, contraction; };
 
 // The tiling of least estimated time: rounds of tiles over the device times a tile's cycles.  A block of 64 of the contraction costs the MMAs
@@ -40,9 +41,10 @@ struct Size { long long rows, cols, contraction; };
 // 4096, the other products of the call unchanged: y in tiles of one thread block x 256 columns 140.2, 192 139, 224 139; of two x 256 137,
 // 224 135, 192 141, 128 151; dx one x 256 335, one x 192 330, two x 256 321, two x 192 345; of 1560 rows g, u one x 256 63, two x 256 65; y
 // one x 160 60, two x 192 57, two x 128 68.  An MN-major B comes in boxes of 64 columns a thread block, and other widths were slower than
-// this says (dw two x 256 317, two x 224 334).  most_bn: columns for which the kernel still has four stages with one thread block a tile.
-Tiling ff_tiling(const Device* d, const Size* s, int n, int segments, bool gated, bool b_mn, int most_bn = 256) {
-    Tiling best = {1, 64};
+// this says (dw two x 256 317, two x 224 334).  Few tiles with a long contraction are split: their parts' sums cost 8 bytes an element and part
+// on the way through L2 and another launch (STORE only).  most_bn: columns for which the kernel still has four stages with one thread block a tile.
+Tiling ff_tiling(const Device* d, const Size* s, int n, int segments, bool gated, bool b_mn, int most_bn = 256, bool may_split = true) {
+    Tiling best = {1, 64, 1};
     double least = 1e300;
     for (int cg = 1; cg <= 2; ++cg)
         for (int bn = b_mn ? 64 * cg : 64; bn <= 256; bn += gated ? 64 : (b_mn ? 64 * cg : 32)) {
@@ -54,9 +56,14 @@ Tiling ff_tiling(const Device* d, const Size* s, int n, int segments, bool gated
                 tiles += (s[i].rows + 128 * cg - 1) / (128 * cg) * ((s[i].cols + out - 1) / out);
                 if (blocks < (double)((s[i].contraction + 63) / 64)) blocks = (double)((s[i].contraction + 63) / 64);
             }
-            const double mma = 2.0 * bn, memory = (b_mn ? 1.75 : 1.6) * (128 + bn / cg);
-            const double cost = (double)((tiles + slots - 1) / slots) * (blocks * segments * (mma > memory ? mma : memory) + 1500.0);
-            if (cost < least) { least = cost; best = {cg, bn}; }
+            const double mma = 2.0 * bn, memory = (b_mn ? 1.75 : 1.6) * (128 + bn / cg), block = mma > memory ? mma : memory;
+            blocks *= segments;
+            for (int k = 1; k <= (may_split && tiles < slots ? 16 : 1); ++k) {
+                if (k > 1 && blocks < 4 * k) break;
+                double cost = (double)((tiles * k + slots - 1) / slots) * (blocks / k * block + 1500.0);
+                if (k > 1) cost += 4000.0 + tiles * k * 128.0 * cg * bn * 8.0 / 5000.0;
+                if (cost < least) { least = cost; best = {cg, bn, k}; }
+            }
         }
     return best;
 }
@@ -67,15 +74,20 @@ struct Launch {
     int type;
     Tiling tiling;
     FfGemmParams p;
+    FfJoinOut join = {};
     Launch(const Device* dev, int t, int act, Tiling cut) : d(dev), type(t), tiling(cut) {
         memset(&p, 0, sizeof(p));
-        p.segments = 1; p.act = act; p.dev_status = dev->status; p.bn = cut.bn;
+        p.segments = 1; p.act = act; p.dev_status = dev->status; p.bn = cut.bn; p.splits = cut.splits;
     }
     // Contraction-contiguous (K-major) operand of `tile` rows; row-contiguous (MN-major) operand.
     hf_status k_major(CUtensorMap* m, const Matrix& x, int tile) { return matrix_map(d, m, type, x.p, x.rows, x.cols, x.stride, 64, tile); }
     hf_status mn_major(CUtensorMap* m, const Matrix& x) { return matrix_map(d, m, type, x.p, x.rows, x.cols, x.stride, 64, 64); }
     // What an epilogue reads or writes: boxes of 32 x 32.
     hf_status box(CUtensorMap* m, const Matrix& x) { return matrix_map(d, m, type, x.p, x.rows, x.cols, x.stride, 32, 32); }
+    hf_status output(int i, const Matrix& x) {
+        join.out[i] = const_cast<void*>(x.p); join.stride[i] = x.stride;
+        return box(&p.out[i], x);
+    }
     void product(long long rows, int cols, long long contraction, int bn_out) {
         const int i = p.products++, bm = 128 * tiling.cg;
         p.rows[i] = (int)rows; p.cols[i] = cols; p.kb[i] = (int)((contraction + 63) / 64);
@@ -88,15 +100,20 @@ struct Launch {
         p.stages = C::stages_for(p.bn);
         auto kernel = k_ff_gemm<T, EPI, A_MN, B_MN, CG>;
         HFL_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_MAX));
-        const int tiles = p.tile0[p.products], slots = CG == 1 ? d->sm_count : d->pairs;
+        const int tiles = p.tile0[p.products] * p.splits, slots = CG == 1 ? d->sm_count : d->pairs;
         cudaLaunchConfig_t cfg = {};
-        cudaLaunchAttribute attr;
-        attr.id = cudaLaunchAttributeClusterDimension;
-        attr.val.clusterDim.x = CG; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+        cudaLaunchAttribute attr[2];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = CG; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+        attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[1].val.programmaticStreamSerializationAllowed = 1;
         cfg.gridDim = dim3(CG * (tiles < slots ? tiles : slots)); cfg.blockDim = dim3(C::THREADS);
-        cfg.dynamicSmemBytes = C::smem_bytes(p.bn, p.stages); cfg.stream = st; cfg.attrs = &attr; cfg.numAttrs = 1;
+        cfg.dynamicSmemBytes = C::smem_bytes(p.bn, p.stages); cfg.stream = st; cfg.attrs = attr; cfg.numAttrs = 2;
         HFL_CUDA(cudaLaunchKernelEx(&cfg, kernel, p));
-        return HF_OK;
+        if (p.splits == 1) return HF_OK;
+        const long long warps = (long long)p.tile0[p.products] * 4 * CG * (p.bn / 8);
+        join.cg = CG;
+        return launch_after(k_ff_join<T>, dim3((unsigned)((warps + 3) / 4)), dim3(128), 0, st, p, join);
     }
     template <int EPI, bool A_MN, bool B_MN>
     hf_status run(cudaStream_t st) {
@@ -127,6 +144,52 @@ hf_status ff_pointer(const void* p, const char* name) {
 }
 size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
 
+// The products' sizes and cuts.
+struct Sizes { Size data[3]; };
+Sizes y_sizes(const hf_ff_shape* g) { return {{{g->rows, g->out_width, g->hidden}}}; }
+Sizes dx_sizes(const hf_ff_shape* g) { return {{{g->rows, g->width, g->hidden}}}; }
+Sizes dw_sizes(const hf_ff_shape* g) {
+    return {{{g->hidden, g->width, g->rows}, {g->hidden, g->width, g->rows}, {g->out_width, g->hidden, g->rows}}};
+}
+Tiling cut_gated(const Device* d, const hf_ff_shape* g) {
+    const Size s = {g->rows, g->hidden, g->width};
+    return ff_tiling(d, &s, 1, 1, true, false, 256, false);
+}
+Tiling cut_y(const Device* d, const hf_ff_shape* g) { return ff_tiling(d, y_sizes(g).data, 1, 1, false, false); }
+Tiling cut_dh(const Device* d, const hf_ff_shape* g) {
+    const Size s = {g->rows, g->hidden, g->out_width};
+    return ff_tiling(d, &s, 1, 1, false, true, 128, false);
+}
+Tiling cut_dx(const Device* d, const hf_ff_shape* g) { return ff_tiling(d, dx_sizes(g).data, 1, 2, false, true); }
+Tiling cut_dw(const Device* d, const hf_ff_shape* g) { return ff_tiling(d, dw_sizes(g).data, 3, 1, false, true); }
+size_t ff_partial_bytes(const Tiling& t, const Size* s, int n) {
+    if (t.splits == 1) return 0;
+    size_t tiles = 0;
+    for (int i = 0; i < n; ++i)
+        tiles += (size_t)((s[i].rows + 128 * t.cg - 1) / (128 * t.cg)) * ((s[i].cols + t.bn - 1) / t.bn);
+    return tiles * t.splits * 128 * t.cg * t.bn * sizeof(float);
+}
+
+// Up to 16 rows: both products by k_ff_rows.
+#ifndef ROWS_MOST
+#define ROWS_MOST 16
+#endif
+constexpr int FF_ROWS_MOST = ROWS_MOST;
+template <typename T, int NT, int ACT>
+hf_status launch_rows(const hf_ff_shape* g, const FfRowsParams& first, const FfRowsParams& second, cudaStream_t st) {
+    HFL_TRY(launch_after(k_ff_rows<T, NT, true, ACT>, dim3((g->hidden + 7) / 8), dim3(256), 0, st, first));
+    return launch_after(k_ff_rows<T, NT, false, 0>, dim3((g->out_width + 7) / 8), dim3(512), 0, st, second);
+}
+template <typename T, int NT>
+hf_status launch_rows(const hf_ff_shape* g, const FfRowsParams& first, const FfRowsParams& second, cudaStream_t st) {
+    return g->act == HF_ACT_SILU ? launch_rows<T, NT, HF_ACT_SILU>(g, first, second, st) : launch_rows<T, NT, HF_ACT_GELU_TANH>(g, first, second, st);
+}
+template <typename T>
+hf_status launch_rows(const hf_ff_shape* g, const FfRowsParams& first, const FfRowsParams& second, cudaStream_t st) {
+    if (g->rows <= 8) return launch_rows<T, 1>(g, first, second, st);
+    return launch_rows<T, 2>(g, first, second, st);
+}
+
 }  // namespace
 
 namespace hf_layers {
@@ -151,8 +214,14 @@ extern "C" {
 hf_status hf_gated_ff_workspace(const hf_ff_shape* g, int backward, size_t* bytes) {
     HFL_TRY(ff_check(g));
     if (!bytes) return fail(HF_ERR_INVALID_ARG, "bytes is null");
+    const Device* d;
+    HFL_TRY(current_device(&d));
     const size_t h = round_up((size_t)g->rows * g->hidden * 2);
-    *bytes = backward ? 3 * h : h;          // h; dg, du, h
+    if (backward) {             // dg, du, h; the parts' sums of dx, then of dW
+        const size_t x = ff_partial_bytes(cut_dx(d, g), dx_sizes(g).data, 1), w = ff_partial_bytes(cut_dw(d, g), dw_sizes(g).data, 3);
+        *bytes = 3 * h + (x > w ? x : w);
+    } else
+        *bytes = h + ff_partial_bytes(cut_y(d, g), y_sizes(g).data, 1);
     return HF_OK;
 }
 
@@ -168,28 +237,32 @@ hf_status hf_gated_ff(const hf_ff_shape* g, const void* x, const void* w_gate, c
     HFL_TRY(current_device(&d));
     const cudaStream_t st = (cudaStream_t)stream;
     const long long M = g->rows, K = g->width, N = g->hidden, O = g->out_width;
+    if (M <= FF_ROWS_MOST) {
+        const FfRowsParams first = {x, w_gate, w_up, workspace, gate, up, g->x_stride, N, (int)M, (int)K, (int)N};
+        const FfRowsParams second = {workspace, w_down, w_down, y, nullptr, nullptr, N, g->y_stride, (int)M, (int)N, (int)O};
+        return g->type == HF_BF16 ? launch_rows<bf16>(g, first, second, st) : launch_rows<__half>(g, first, second, st);
+    }
     const Matrix h = {workspace, M, N, N};
     {
-        const Size size = {M, N, K};
-        Launch l(d, g->type, g->act, ff_tiling(d, &size, 1, 1, true, false));
+        Launch l(d, g->type, g->act, cut_gated(d, g));
         const int hn = l.p.bn / 2;
         HFL_TRY(l.k_major(&l.p.a[0], {x, M, K, g->x_stride}, 128));
         HFL_TRY(l.k_major(&l.p.b[0], {w_gate, N, K, K}, hn));
         HFL_TRY(l.k_major(&l.p.b[1], {w_up, N, K, K}, hn));
-        HFL_TRY(l.box(&l.p.out[0], h));
+        HFL_TRY(l.output(0, h));
         if (gate) {
-            HFL_TRY(l.box(&l.p.out[1], {gate, M, N, N}));
-            HFL_TRY(l.box(&l.p.out[2], {up, M, N, N}));
+            HFL_TRY(l.output(1, {gate, M, N, N}));
+            HFL_TRY(l.output(2, {up, M, N, N}));
             l.p.save = 1;
         }
         l.product(M, N, K, hn);
         HFL_TRY((l.run<FF_GATED, false, false>(st)));
     }
-    const Size size = {M, O, N};
-    Launch l(d, g->type, g->act, ff_tiling(d, &size, 1, 1, false, false));
+    Launch l(d, g->type, g->act, cut_y(d, g));
+    l.p.partials = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + round_up((size_t)M * N * 2));
     HFL_TRY(l.k_major(&l.p.a[0], h, 128));
     HFL_TRY(l.k_major(&l.p.b[0], {w_down, O, N, N}, l.p.bn / l.tiling.cg));
-    HFL_TRY(l.box(&l.p.out[0], {y, M, O, g->y_stride}));
+    HFL_TRY(l.output(0, {y, M, O, g->y_stride}));
     l.product(M, O, N, l.p.bn);
     return l.run<FF_STORE, false, false>(st);
 }
@@ -221,31 +294,30 @@ hf_status hf_gated_ff_backward(const hf_ff_shape* g, const void* dy, const void*
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     const Matrix mdy = {dy, M, O, g->y_stride}, mx = {x, M, K, g->x_stride}, dg = {ws, M, N, N}, du = {ws + part, M, N, N}, h = {ws + 2 * part, M, N, N};
     {
-        const Size size = {M, N, O};
-        Launch l(d, g->type, g->act, ff_tiling(d, &size, 1, 1, false, true, 128));
+        Launch l(d, g->type, g->act, cut_dh(d, g));
         HFL_TRY(l.box(&l.p.in[0], {gate, M, N, N})); HFL_TRY(l.box(&l.p.in[1], {up, M, N, N}));
         HFL_TRY(l.k_major(&l.p.a[0], mdy, 128));
         HFL_TRY(l.mn_major(&l.p.b[0], {w_down, O, N, N}));
-        HFL_TRY(l.box(&l.p.out[0], dg)); HFL_TRY(l.box(&l.p.out[1], du)); HFL_TRY(l.box(&l.p.out[2], h));
+        HFL_TRY(l.output(0, dg)); HFL_TRY(l.output(1, du)); HFL_TRY(l.output(2, h));
         l.product(M, (int)N, O, l.p.bn);
         HFL_TRY((l.run<FF_DHIDDEN, false, true>(st)));
     }
     if (dx) {
-        const Size size = {M, K, N};
-        Launch l(d, g->type, g->act, ff_tiling(d, &size, 1, 2, false, true));
+        Launch l(d, g->type, g->act, cut_dx(d, g));
+        l.p.partials = reinterpret_cast<float*>(ws + 3 * part);
         HFL_TRY(l.k_major(&l.p.a[0], dg, 128)); HFL_TRY(l.k_major(&l.p.a[1], du, 128));
         HFL_TRY(l.mn_major(&l.p.b[0], {w_gate, N, K, K})); HFL_TRY(l.mn_major(&l.p.b[1], {w_up, N, K, K}));
-        HFL_TRY(l.box(&l.p.out[0], {dx, M, K, K}));
+        HFL_TRY(l.output(0, {dx, M, K, K}));
         l.product(M, (int)K, N, l.p.bn);
         l.p.segments = 2; l.p.kb[1] = l.p.kb[0];
         HFL_TRY((l.run<FF_STORE, false, true>(st)));
     }
     if (n_dw) {
-        const Size sizes[3] = {{N, K, M}, {N, K, M}, {O, N, M}};
-        Launch l(d, g->type, g->act, ff_tiling(d, sizes, 3, 1, false, true));
+        Launch l(d, g->type, g->act, cut_dw(d, g));
+        l.p.partials = reinterpret_cast<float*>(ws + 3 * part);
         HFL_TRY(l.mn_major(&l.p.a[0], dg)); HFL_TRY(l.mn_major(&l.p.a[1], du)); HFL_TRY(l.mn_major(&l.p.a[2], mdy));
         HFL_TRY(l.mn_major(&l.p.b[0], mx)); l.p.b[1] = l.p.b[0]; HFL_TRY(l.mn_major(&l.p.b[2], h));
-        HFL_TRY(l.box(&l.p.out[0], {dw_gate, N, K, K})); HFL_TRY(l.box(&l.p.out[1], {dw_up, N, K, K})); HFL_TRY(l.box(&l.p.out[2], {dw_down, O, N, N}));
+        HFL_TRY(l.output(0, {dw_gate, N, K, K})); HFL_TRY(l.output(1, {dw_up, N, K, K})); HFL_TRY(l.output(2, {dw_down, O, N, N}));
         l.product(N, (int)K, M, l.p.bn); l.product(N, (int)K, M, l.p.bn); l.product(O, (int)N, M, l.p.bn);
         HFL_TRY((l.run<FF_STORE, true, true>(st)));
     }

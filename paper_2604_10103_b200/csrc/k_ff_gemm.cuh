@@ -26,6 +26,8 @@ struct FfGemmParams {
     int rows[3], cols[3];               // of the output
     int kb[3];                          // blocks of 64 of each product's (or segment's) contraction
     int segments;                       // contraction in this many segments (dx = dg Wg + du Wu: two)
+    int splits;                         // STORE: the contraction of a tile is split over this many, whose sums go to `partials` (k_ff_join adds them)
+    float* partials;
     int bn;                             // accumulator columns of a tile: a multiple of 32 (GATED: half of them g, half u)
     int stages;
     int act, save;
@@ -145,11 +147,14 @@ template <typename T, int ACT> __device__ __forceinline__ void ff_hidden_row(con
     }
 }
 
-struct FfTile { int product, m0, n0; };
+struct FfTile { int product, m0, n0, split, index; };
 // Tiles of a product in groups of 16 row tiles (bm rows each), all columns of a group before the next: the thread blocks at work at a time
 // share rows and columns of both operands in L2.
 __device__ __forceinline__ FfTile ff_tile(const FfGemmParams& p, int t, int bm, int bn_out) {
     FfTile r;
+    r.split = 0;
+    if (p.splits > 1) { r.split = t % p.splits; t /= p.splits; }
+    r.index = t;
     r.product = 0;
     while (r.product + 1 < p.products && t >= p.tile0[r.product + 1]) ++r.product;
     t -= p.tile0[r.product];
@@ -211,7 +216,7 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = CG == 1 ? 0 : (int)(blockIdx.x & 1);                   // (clusters are two neighbouring thread blocks)
     const int bn_out = EPI == FF_GATED ? p.bn / 2 : p.bn, bn_own = p.bn / CG;
-    const int n_tiles = p.tile0[p.products], tile_first = blockIdx.x / CG, tile_step = gridDim.x / CG;
+    const int n_tiles = p.tile0[p.products] * p.splits, tile_first = blockIdx.x / CG, tile_step = gridDim.x / CG;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < stages; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_free + 8 * s, 1); }
@@ -226,6 +231,9 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
     ff_meet<CG>();
     fence_after_sync();
     const uint32_t tmem = *tmem_slot;
+    // (launched while the kernel before still runs; the next may be launched once this one may read what all before have written)
+    pdl_wait();
+    pdl_trigger();
 
     if (warp == C::WARP_TMA) {
         // ================================================================= loader
@@ -238,27 +246,28 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
             for (int t = tile_first; ok && t < n_tiles; t += tile_step) {
                 const FfTile tile = ff_tile(p, t, CG * C::BM, bn_out);
                 const int m0 = tile.m0 + rank * C::BM, n0 = tile.n0 + (EPI == FF_GATED ? 0 : rank * bn_own);
-                for (int seg = 0; ok && seg < p.segments; ++seg) {
-                    const int i = tile.product + seg;           // (one of the two is always 0)
-                    for (int kb = 0; kb < p.kb[i]; ++kb) {
-                        if (!(ok = mbar_wait<true>(bar_free + 8 * s, phase, abort_flag, p.dev_status, 81))) break;
-                        const uint32_t sA = s_base + s * stage_bytes, sB = sA + C::A_BYTES, full = ff_first<CG>(bar_full + 8 * s);
-                        if (rank == 0) mbar_expect_tx(bar_full + 8 * s, bytes);
-                        if (A_MN) {
-                            ff_load<CG>(sA, &p.a[i], m0, kb * C::BK, full);
-                            ff_load<CG>(sA + 8192, &p.a[i], m0 + 64, kb * C::BK, full);
-                        } else
-                            ff_load<CG>(sA, &p.a[i], kb * C::BK, m0, full);
-                        if (EPI == FF_GATED) {
-                            // g's columns in front of u's: the pair's first thread block holds Wg's rows, the second Wu's
-                            ff_load<CG>(sB, &p.b[rank], kb * C::BK, n0, full);
-                            if (CG == 1) ff_load<CG>(sB + bn_out * C::BK * 2, &p.b[1], kb * C::BK, n0, full);
-                        } else if (B_MN) {
-                            for (int x = 0; x < b_boxes; ++x) ff_load<CG>(sB + x * 8192, &p.b[i], n0 + 64 * x, kb * C::BK, full);
-                        } else
-                            ff_load<CG>(sB, &p.b[i], kb * C::BK, n0, full);
-                        if (++s == stages) { s = 0; phase ^= 1; }
-                    }
+                const int k_all = p.kb[tile.product] * p.segments;      // (segments: of the same length)
+                const int k_end = (int)((long long)k_all * (tile.split + 1) / p.splits);
+                for (int k = (int)((long long)k_all * tile.split / p.splits); k < k_end; ++k) {
+                    if (!(ok = mbar_wait<true>(bar_free + 8 * s, phase, abort_flag, p.dev_status, 81))) break;
+                    const int seg = p.segments > 1 && k >= p.kb[0], i = tile.product + seg;       // (one of the two is always 0)
+                    const int kc = (k - seg * p.kb[0]) * C::BK;
+                    const uint32_t sA = s_base + s * stage_bytes, sB = sA + C::A_BYTES, full = ff_first<CG>(bar_full + 8 * s);
+                    if (rank == 0) mbar_expect_tx(bar_full + 8 * s, bytes);
+                    if (A_MN) {
+                        ff_load<CG>(sA, &p.a[i], m0, kc, full);
+                        ff_load<CG>(sA + 8192, &p.a[i], m0 + 64, kc, full);
+                    } else
+                        ff_load<CG>(sA, &p.a[i], kc, m0, full);
+                    if (EPI == FF_GATED) {
+                        // g's columns in front of u's: the pair's first thread block holds Wg's rows, the second Wu's
+                        ff_load<CG>(sB, &p.b[rank], kc, n0, full);
+                        if (CG == 1) ff_load<CG>(sB + bn_out * C::BK * 2, &p.b[1], kc, n0, full);
+                    } else if (B_MN) {
+                        for (int x = 0; x < b_boxes; ++x) ff_load<CG>(sB + x * 8192, &p.b[i], n0 + 64 * x, kc, full);
+                    } else
+                        ff_load<CG>(sB, &p.b[i], kc, n0, full);
+                    if (++s == stages) { s = 0; phase ^= 1; }
                 }
             }
             // every stage's MMAs are done before this thread block (whose memory the pair's MMAs read and signal) may leave
@@ -284,8 +293,8 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
         uint32_t phase = 0, acc_phase = 1;
         for (int t = tile_first; ok && t < n_tiles; t += tile_step) {
             const FfTile tile = ff_tile(p, t, CG * C::BM, bn_out);
-            int n_kb = p.kb[tile.product];
-            for (int seg = 1; seg < p.segments; ++seg) n_kb += p.kb[seg];
+            const int k_all = p.kb[tile.product] * p.segments;
+            const int n_kb = (int)((long long)k_all * (tile.split + 1) / p.splits) - (int)((long long)k_all * tile.split / p.splits);
             if (!(ok = mbar_wait_warp<true>(bar_acc_free + 8 * acc, acc_phase, abort_flag, p.dev_status, 82))) break;
             fence_after_sync();
             for (int kb = 0; kb < n_kb; ++kb) {
@@ -352,6 +361,12 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
                 tmem_ld32(at, r);
                 if constexpr (EPI == FF_STORE) {
                     tmem_wait_ld();
+                    if (p.splits > 1) {             // [tile][split][32 rows][32 columns]: column by column, so that a warp's stores are whole lines
+                        float* to = p.partials + ((((size_t)tile.index * p.splits + tile.split) * CG + rank) * 4 + quad) * 32 * p.bn + c * 1024 + lane;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) to[32 * j] = __uint_as_float(r[j]);
+                        continue;
+                    }
 #pragma unroll
                     for (int j = 0; j < 16; ++j) o[j] = pack2<T>(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
                     out.put(&p.out[tile.product], o, col, row, lane);
@@ -420,4 +435,29 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
         fence_after_sync();
         ff_tmem_dealloc<CG>(tmem);
     }
+}
+
+// out = the sum over the splits of the partials of k_ff_gemm, in order, rounded once.  A warp takes 32 rows x 8 columns.
+struct FfJoinOut { void* out[3]; long long stride[3]; int cg; };
+template <typename T>
+__global__ void __launch_bounds__(128)
+k_ff_join(const __grid_constant__ FfGemmParams p, const FfJoinOut o) {
+    const int lane = threadIdx.x & 31, eights = p.bn / 8, units = 4 * o.cg * eights;
+    const int id = blockIdx.x * 4 + (threadIdx.x >> 5), index = id / units, unit = id - index * units;
+    pdl_wait();
+    if (index >= p.tile0[p.products]) return;
+    const FfTile tile = ff_tile(p, index * p.splits, 128 * o.cg, p.bn);
+    const int rows32 = unit / eights, c = unit - rows32 * eights, row = tile.m0 + rows32 * 32 + lane, col = tile.n0 + 8 * c;
+    if (row >= p.rows[tile.product] || col >= p.cols[tile.product]) return;
+    const size_t step = (size_t)o.cg * 128 * p.bn;
+    const float* from = p.partials + (size_t)index * p.splits * step + (size_t)rows32 * 32 * p.bn + c * 256 + lane;
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < p.splits; ++s, from += step)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += from[32 * j];
+    T* to = static_cast<T*>(o.out[tile.product]) + (size_t)row * o.stride[tile.product] + col;
+    *reinterpret_cast<uint4*>(to) = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
 }
