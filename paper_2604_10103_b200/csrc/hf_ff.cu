@@ -15,14 +15,15 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 // Map of a matrix [rows, cols] of 16-bit elements with `stride` between rows; box of box_cols (64: 128-byte swizzle; 32: 64-byte) x box_rows.
+// planes: that many such matrices `plane_bytes` apart, and as many boxes at a time.
 hf_status matrix_map(const Device* d, CUtensorMap* m, int type, const void* base, long long rows, long long cols, long long stride,
-                     int box_cols, int box_rows) {
-    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-    const cuuint64_t strides[1] = {(cuuint64_t)(rows > 1 ? stride : (cols + 7) / 8 * 8) * 2};
-    const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
-    const cuuint32_t es[2] = {1, 1};
+                     int box_cols, int box_rows, int planes = 1, size_t plane_bytes = 0) {
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
+    const cuuint64_t strides[2] = {(cuuint64_t)(rows > 1 ? stride : (cols + 7) / 8 * 8) * 2, plane_bytes};
+    const cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, (cuuint32_t)planes};
+    const cuuint32_t es[3] = {1, 1, 1};
     const CUresult r = reinterpret_cast<EncodeTiledFn>(d->encode_tiled)(
-        m, type == HF_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void*>(base), dims, strides, box, es,
+        m, type == HF_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, planes > 1 ? 3 : 2, const_cast<void*>(base), dims, strides, box, es,
         CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return fail(HF_ERR_CUDA, "cuTensorMapEncodeTiled failed with %d", (int)r);
@@ -298,7 +299,7 @@ hf_status hf_gated_ff_backward(const hf_ff_shape* g, const void* dy, const void*
         HFL_TRY(l.box(&l.p.in[0], {gate, M, N, N})); HFL_TRY(l.box(&l.p.in[1], {up, M, N, N}));
         HFL_TRY(l.k_major(&l.p.a[0], mdy, 128));
         HFL_TRY(l.mn_major(&l.p.b[0], {w_down, O, N, N}));
-        HFL_TRY(l.output(0, dg)); HFL_TRY(l.output(1, du)); HFL_TRY(l.output(2, h));
+        HFL_TRY(matrix_map(d, &l.p.out[0], g->type, ws, M, N, N, 32, 32, 3, part));
         l.product(M, (int)N, O, l.p.bn);
         HFL_TRY((l.run<FF_DHIDDEN, false, true>(st)));
     }

@@ -20,6 +20,7 @@ enum { FF_GATED = 0, FF_STORE = 1, FF_DHIDDEN = 2 };
 
 struct FfGemmParams {
     CUtensorMap a[3], b[3], out[3];     // operands of each product, or of each segment of the contraction; GATED: b = Wg, Wu
+                                        // (DHIDDEN: out[0] is a map of dg, du, h as [3, rows, cols])
     CUtensorMap in[2];                  // DHIDDEN: gate and up [rows, cols]
     int products;                       // products of this launch, each with tiles of its own ...
     int tile0[4];                       // ... from tile0[i] to tile0[i + 1]
@@ -105,45 +106,49 @@ template <int CG> __device__ __forceinline__ void ff_meet() {
 // silu: a = g p, a' = p (1 + g (1 - p)), p = 1 / (1 + e^-g).   gelu (tanh form): with v = A (g + B g^3) the factor (1 + tanh v) / 2 is
 // 1 / (1 + e^-2v), so it is g p with another exponent: a' = p + g p (1 - p) 2 A (1 + 3 B g^2).
 // ex2.approx and rcp.approx (2 and 1 ulp; an exponential that overflows gives p = 0, the right limit).
-__device__ __forceinline__ float ff_sigmoid(float v) {
+__device__ __forceinline__ float ff_rcp(float v) {
     float r;
-    asm("rcp.approx.ftz.f32 %0, %1;\n" : "=f"(r) : "f"(1.f + fast_exp2(-1.4426950408889634f * v)));
+    asm("rcp.approx.ftz.f32 %0, %1;\n" : "=f"(r) : "f"(v));
     return r;
 }
-constexpr float FF_GELU_2A = 1.5957691216057308f, FF_GELU_B = 0.044715f;
-template <int ACT> __device__ __forceinline__ float ff_act(float g) {
-    return g * ff_sigmoid(ACT == HF_ACT_SILU ? g : FF_GELU_2A * fmaf(FF_GELU_B * g * g, g, g));
-}
-template <int ACT> __device__ __forceinline__ float ff_act(float g, float& slope) {
-    if constexpr (ACT == HF_ACT_SILU) {
-        const float p = ff_sigmoid(g);
-        slope = p * fmaf(g, 1.f - p, 1.f);
-        return g * p;
-    } else {
-        const float p = ff_sigmoid(FF_GELU_2A * fmaf(FF_GELU_B * g * g, g, g));
-        slope = fmaf(g * p * (1.f - p), FF_GELU_2A * fmaf(3.f * FF_GELU_B * g, g, 1.f), p);
-        return g * p;
+constexpr float FF_GELU_2A = 1.5957691216057308f, FF_GELU_B = 0.044715f, FF_LOG2E = 1.4426950408889634f;
+// Two elements at a time (packed float32 arithmetic): a and, where asked for, a'.
+template <int ACT, bool SLOPE> __device__ __forceinline__ float2 ff_act2(float2 g, float2* slope) {
+    const float2 one = make_float2(1.f, 1.f);
+    // - log2(e) times the exponent
+    float2 x;
+    if constexpr (ACT == HF_ACT_SILU) x = fmul2(g, make_float2(-FF_LOG2E, -FF_LOG2E));
+    else x = fmul2(fmul2(g, make_float2(-FF_LOG2E * FF_GELU_2A, -FF_LOG2E * FF_GELU_2A)), ffma2(fmul2(g, g), make_float2(FF_GELU_B, FF_GELU_B), one));
+    const float2 d = fadd2(make_float2(fast_exp2(x.x), fast_exp2(x.y)), one);
+    const float2 p = make_float2(ff_rcp(d.x), ff_rcp(d.y)), a = fmul2(g, p);
+    if constexpr (SLOPE) {
+        const float2 q = ffma2(p, make_float2(-1.f, -1.f), one);
+        if constexpr (ACT == HF_ACT_SILU) *slope = ffma2(a, q, p);
+        else *slope = ffma2(fmul2(a, q), ffma2(fmul2(g, g), make_float2(3.f * FF_GELU_B * FF_GELU_2A, 3.f * FF_GELU_B * FF_GELU_2A), make_float2(FF_GELU_2A, FF_GELU_2A)), p);
     }
+    return a;
 }
+template <int ACT> __device__ __forceinline__ float ff_act(float g) { return ff_act2<ACT, false>(make_float2(g, g), nullptr).x; }
 // The lane's 32 elements at a time, the activation known to the compiler: their latencies overlap, which a branch an element would prevent.
 // h = act(g) u from the accumulators:
 template <typename T, int ACT> __device__ __forceinline__ void ff_gated_row(const uint32_t (&g)[32], const uint32_t (&u)[32], uint32_t (&h)[16]) {
 #pragma unroll
-    for (int j = 0; j < 16; ++j)
-        h[j] = pack2<T>(ff_act<ACT>(__uint_as_float(g[2 * j])) * __uint_as_float(u[2 * j]),
-                        ff_act<ACT>(__uint_as_float(g[2 * j + 1])) * __uint_as_float(u[2 * j + 1]));
+    for (int j = 0; j < 16; ++j) {
+        const float2 a = ff_act2<ACT, false>(make_float2(__uint_as_float(g[2 * j]), __uint_as_float(g[2 * j + 1])), nullptr);
+        const float2 o = fmul2(a, make_float2(__uint_as_float(u[2 * j]), __uint_as_float(u[2 * j + 1])));
+        h[j] = pack2<T>(o.x, o.y);
+    }
 }
 // g, u -> dg, du; h; from dh:
 template <typename T, int ACT> __device__ __forceinline__ void ff_hidden_row(const uint32_t (&dh)[32], uint32_t (&g)[16], uint32_t (&u)[16], uint32_t (&h)[16]) {
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
-        const float2 gf = unpack2<T>(g[j]), uf = unpack2<T>(u[j]);
-        const float d0 = __uint_as_float(dh[2 * j]), d1 = __uint_as_float(dh[2 * j + 1]);
-        float s0, s1;
-        const float a0 = ff_act<ACT>(gf.x, s0), a1 = ff_act<ACT>(gf.y, s1);
-        g[j] = pack2<T>(d0 * uf.x * s0, d1 * uf.y * s1);
-        u[j] = pack2<T>(d0 * a0, d1 * a1);
-        h[j] = pack2<T>(a0 * uf.x, a1 * uf.y);
+        const float2 gf = unpack2<T>(g[j]), uf = unpack2<T>(u[j]), d = make_float2(__uint_as_float(dh[2 * j]), __uint_as_float(dh[2 * j + 1]));
+        float2 s;
+        const float2 a = ff_act2<ACT, true>(gf, &s), dg = fmul2(fmul2(d, uf), s), du = fmul2(d, a), o = fmul2(a, uf);
+        g[j] = pack2<T>(dg.x, dg.y);
+        u[j] = pack2<T>(du.x, du.y);
+        h[j] = pack2<T>(o.x, o.y);
     }
 }
 
@@ -409,8 +414,7 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
                     fence_proxy_async();
                     __syncwarp();
                     if (lane == 0) {
-#pragma unroll
-                        for (int i = 0; i < 3; ++i) tma_store_2d(&p.out[i], boxes + i * C::BOX, col, row);
+                        tma_store_3d(&p.out[0], boxes, col, row, 0);        // all three boxes
                         bulk_commit();
                     }
                 }
