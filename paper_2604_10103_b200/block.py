@@ -1,0 +1,187 @@
+"""A denoiser block around the hybrid attention: modulated layer norm, fused projection, rotary positions in time, height and width, hybrid
+attention, output projection; modulated layer norm, gated feed-forward; a gated residual after each half.
+
+`DenoiserBlock.forward` is one layer of one denoising step of a stream (no gradient), `commit` folds a finished chunk into the layer's cache and
+state, and `forward` under autograd is the step with gradient: every operator between the projections has its backward pass in the
+library, and the plain projections are torch's.  `python -m paper_2604_10103_b200.block` runs a short stream and one training step at the
+832x480 shape on synthetic data and prints their times.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import binding as hf
+from . import inputs as gen
+from . import layers
+from . import rope
+
+
+class _Norm(torch.autograd.Function):
+    """Layer norm with scale and shift per group of rows: y = xhat (1 + scale_g) + shift_g."""
+
+    @staticmethod
+    def forward(ctx, x, scale, shift, rows_per_group, eps):
+        y, mean, rstd = layers.layer_norm(x, scale, shift, eps=eps, weight_offset=1.0, rows_per_group=rows_per_group)
+        ctx.save_for_backward(x, scale, mean, rstd)
+        ctx.rows_per_group = rows_per_group
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, scale, mean, rstd = ctx.saved_tensors
+        dx, dscale, dshift = layers.layer_norm_backward(dy.contiguous(), x, mean, rstd, scale, weight_offset=1.0, rows_per_group=ctx.rows_per_group)
+        return dx, dscale.to(scale.dtype), dshift.to(scale.dtype), None, None
+
+
+class _HeadsRope(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, qkv, heads, pos, tables):
+        ctx.pos, ctx.tables = pos, tables
+        return layers.split_heads_rope(qkv, heads, heads, pos, tables)
+
+    @staticmethod
+    def backward(ctx, dq, dk, dv):
+        return layers.split_heads_rope_backward(dq, dk, dv, ctx.pos, ctx.tables), None, None, None
+
+
+class _GatedFF(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w_gate, w_up, w_down, act):
+        y, gate, up = layers.gated_ff(x, w_gate, w_up, w_down, act=act, save=True)
+        ctx.save_for_backward(x, w_gate, w_up, w_down, gate, up)
+        ctx.act = act
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        return layers.gated_ff_backward(dy.contiguous(), *ctx.saved_tensors, act=ctx.act) + (None,)
+
+
+class _Attention(torch.autograd.Function):
+    """The hybrid attention of one layer for the step with gradient: its selection is held fixed, the cached chunks and the state get no
+    gradient (Alg. 1).  The context must keep this layer's cache and selection until the backward pass."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, context, layer):
+        o, o_hist = torch.empty_like(q), torch.empty_like(q)
+        lse = q.new_empty(q.shape[:3], dtype=torch.float32)
+        context.hf_block_select(layer, q, k)
+        context.hf_sparse_swa(layer, q, k, v, o, lse=lse)
+        context.hf_linear_attn(layer, q, o_hist)
+        ctx.save_for_backward(q, k, v, o, lse)
+        ctx.context, ctx.layer = context, layer
+        return o + o_hist
+
+    @staticmethod
+    def backward(ctx, g):
+        q, k, v, o, lse = ctx.saved_tensors
+        g = g.contiguous()
+        dq, dq_hist, dk, dv = (torch.empty_like(q) for _ in range(4))
+        ctx.context.hf_sparse_swa_backward_dq(ctx.layer, q, k, v, o, lse, g, dq)
+        ctx.context.hf_sparse_swa_backward_dkv(ctx.layer, q, k, v, o, lse, g, dk, dv)
+        ctx.context.hf_linear_attn_backward_dq(ctx.layer, q, g, dq_hist)
+        return dq + dq_hist, dk, dv, None, None
+
+
+class DenoiserBlock(torch.nn.Module):
+    """One layer.  w: an `inputs.Workload` (batch, heads, head_dim, frames); high x wide tokens a frame; context: the `binding.Context`
+    that holds the layer's cache and state."""
+
+    def __init__(self, w, high, wide, context, layer=0, hidden=None, act="silu", last_frame=255, eps=1e-6, device="cuda", dtype=torch.bfloat16):
+        super().__init__()
+        if high * wide != w.tokens_per_frame:
+            raise ValueError(f"{high} x {wide} tokens are not a frame of {w.tokens_per_frame}")
+        self.w, self.context, self.layer, self.act, self.eps = w, context, layer, act, eps
+        width = w.heads * w.head_dim
+        hidden = hidden or (8 * width // 3 + 63) // 64 * 64
+
+        def matrix(n_out, n_in):
+            return torch.nn.Parameter(torch.randn(n_out, n_in, device=device).mul_(n_in ** -0.5).to(dtype))
+        self.w_qkv, self.w_out = matrix(3 * width, width), matrix(width, width)
+        self.w_gate, self.w_up, self.w_down = matrix(hidden, width), matrix(hidden, width), matrix(width, hidden)
+        n = w.head_dim // 2
+        self.pairs, self.extents = (n - 2 * (n // 3), n // 3, n // 3), (last_frame + 1, high, wide)
+        cos, sin = rope.axis_tables(self.extents, self.pairs)
+        self.register_buffer("cos", torch.from_numpy(cos).to(device))
+        self.register_buffer("sin", torch.from_numpy(sin).to(device))
+        grid = torch.meshgrid(torch.arange(w.chunk_frames), torch.arange(high), torch.arange(wide), indexing="ij")
+        self.register_buffer("pos", torch.stack([g.reshape(-1) for g in grid], dim=1).to(torch.int32).to(device))
+
+    def positions(self, first_frame):
+        pos = self.pos.clone()
+        pos[:, 0] += first_frame
+        return pos
+
+    def _heads(self, x, shift, scale, pos, eps):
+        B, T, width = x.shape
+        frame = self.w.tokens_per_frame
+        h = _Norm.apply(x, scale.reshape(-1, width), shift.reshape(-1, width), frame, eps)
+        return _HeadsRope.apply(torch.nn.functional.linear(h, self.w_qkv), self.w.heads, pos, (self.cos, self.sin, self.extents, self.pairs))
+
+    def forward(self, x, mod, pos):
+        """x [batch, tokens of a chunk, width]; mod [batch, frames of the chunk, 6, width]: shift, scale, gate of the attention half, then of the
+        feed-forward's; pos: `positions` of the chunk's first frame."""
+        B, T, width = x.shape
+        q, k, v = self._heads(x, mod[:, :, 0], mod[:, :, 1], pos, self.eps)
+        if torch.is_grad_enabled() and q.requires_grad:
+            o = _Attention.apply(q, k, v, self.context, self.layer)
+        else:
+            o = torch.empty_like(q)
+            self.context.hf_hybrid_forward(self.layer, q, k, v, o)
+        per_token = mod.repeat_interleave(self.w.tokens_per_frame, dim=1)
+        x = x + per_token[:, :, 2] * torch.nn.functional.linear(o.transpose(1, 2).flatten(2), self.w_out)
+        h = _Norm.apply(x, mod[:, :, 4].reshape(-1, width), mod[:, :, 3].reshape(-1, width), self.w.tokens_per_frame, self.eps)
+        if torch.is_grad_enabled():
+            y = _GatedFF.apply(h, self.w_gate, self.w_up, self.w_down, self.act)
+        else:
+            y = layers.gated_ff(h, self.w_gate, self.w_up, self.w_down, act=self.act)
+        return x + per_token[:, :, 5] * y
+
+    @torch.no_grad()
+    def commit(self, x, mod, pos):
+        """The finished chunk's keys and values go into the layer's cache (and the oldest chunk into its state)."""
+        _, k, v = self._heads(x, mod[:, :, 0], mod[:, :, 1], pos, self.eps)
+        self.context.hf_kv_append(self.layer, k, v)
+
+
+def main():
+    w = gen.layer_832x480()
+    context = hf.Context(hf.make_config(w, merge=hf.HF_MERGE_IDENTITY))
+    torch.manual_seed(0)
+    block = DenoiserBlock(w, 30, 52, context)
+    T, width = w.chunk_frames * w.tokens_per_frame, w.heads * w.head_dim
+
+    def chunk():
+        return torch.randn(w.batch, T, width, device="cuda").bfloat16(), 0.3 * torch.randn(w.batch, w.chunk_frames, 6, width, device="cuda").bfloat16()
+
+    def timed(f):
+        e = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+        for _ in range(3):
+            f()
+        e[0].record()
+        for _ in range(10):
+            f()
+        e[1].record()
+        torch.cuda.synchronize()
+        return e[0].elapsed_time(e[1]) / 10
+
+    with torch.no_grad():
+        for i in range(4):
+            x, mod = chunk()
+            y = block(x, mod, block.positions(i * w.chunk_frames))
+            block.commit(y, mod, block.positions(i * w.chunk_frames))
+        x, mod = chunk()
+        pos = block.positions(4 * w.chunk_frames)
+        print(f"one layer of one denoising step, {T} tokens: {timed(lambda: block(x, mod, pos)):.3f} ms")
+    x.requires_grad_()
+
+    def step():
+        block.zero_grad(set_to_none=True)
+        block(x, mod, pos).float().square().mean().backward()
+    print(f"the same with gradient: {timed(step):.3f} ms")
+    context.hf_get_device_status()
+    hf.hf_layers_status()
+
+
+if __name__ == "__main__":
+    main()
