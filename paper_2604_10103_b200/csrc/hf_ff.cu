@@ -37,19 +37,24 @@ struct Tiling { int cg, bn, splits; };
 struct Size { long long rows, cols, contraction; };
 
 // The tiling of least estimated time: rounds of tiles over the device times a tile's cycles.  A block of 64 of the contraction costs the MMAs
-// 2 bn cycles, and shared memory, which takes each operand byte in and gives it out once, 2 x 128 (128 + bn / cg) bytes at 128 a cycle,
-// of which four fifths were seen to count, a little more with an MN-major B.  What was seen, us a call, of 4680 rows, width 1536, hidden
-// 4096, the other products of the call unchanged: y in tiles of one thread block x 256 columns 140.2, 192 139, 224 139; of two x 256 137,
-// 224 135, 192 141, 128 151; dx one x 256 335, one x 192 330, two x 256 321, two x 192 345; of 1560 rows g, u one x 256 63, two x 256 65; y
-// one x 160 60, two x 192 57, two x 128 68.  An MN-major B comes in boxes of 64 columns a thread block, and other widths were slower than
-// this says (dw two x 256 317, two x 224 334).  Few tiles with a long contraction are split: their parts' sums cost 8 bytes an element and part
-// on the way through L2 and another launch (STORE only).  most_bn: columns for which the kernel still has four stages with one thread block a tile.
-Tiling ff_tiling(const Device* d, const Size* s, int n, int segments, bool gated, bool b_mn, int most_bn = 256, bool may_split = true) {
+// 2 bn cycles, and shared memory, which takes each operand byte in and gives it out once, 2 x 128 (128 + bn / cg) bytes at 128 a cycle; how
+// much of that counts was seen to be four fifths with both operands K-major, a little more with an MN-major B, about all (pairs: 1.2 of
+// it) with both MN-major.  What was seen, us a call, of 4680 rows, width 1536, hidden 4096, the other products of the call unchanged: y in
+// tiles of one thread block x 256 columns 140.2, 192 139, 224 139; of two x 256 137, 224 135, 192 141, 128 151; dx one x 256 335, one x 192
+// 330, two x 256 321, two x 192 345; dw one x 256 335, two x 256 317 (later, with other parts faster, 292; two x 512 278); of 1560
+// rows g, u one x 256 63, two x 256 65; y one x 160 60, two x 192 57, two x 128 68.  An MN-major B comes in boxes of 64 columns a thread
+// block, and other widths were slower than this says (dw two x 256 317, two x 224 334).  Tiles of 512 columns (dw) have their epilogue
+// between the MMAs: some 5000 cycles.  Few tiles with a long contraction are split (STORE): their parts' sums cost 8 bytes an element and
+// part on the way through L2 and another launch.
+enum FfCut { FF_CUT_GATED, FF_CUT_Y, FF_CUT_DH, FF_CUT_DX, FF_CUT_DW };
+Tiling ff_tiling(const Device* d, const Size* s, int n, int segments, FfCut cut) {
+    const bool gated = cut == FF_CUT_GATED, b_mn = cut >= FF_CUT_DH, a_mn = cut == FF_CUT_DW, may_split = cut != FF_CUT_GATED && cut != FF_CUT_DH;
     Tiling best = {1, 64, 1};
     double least = 1e300;
     for (int cg = 1; cg <= 2; ++cg)
-        for (int bn = b_mn ? 64 * cg : 64; bn <= 256; bn += gated ? 64 : (b_mn ? 64 * cg : 32)) {
-            if (cg == 1 && bn > most_bn) break;
+        for (int bn = b_mn ? 64 * cg : 64; bn <= (a_mn && cg == 2 ? 512 : 256); bn += gated ? 64 : (b_mn ? 64 * cg : 32)) {
+            if (bn > 256 && bn != 512) continue;
+            if (cut == FF_CUT_DH && cg == 1 && bn > 128) break;         // (its staging leaves two stages)
             const int out = gated ? bn / 2 : bn, slots = cg == 1 ? d->sm_count : d->pairs;
             long long tiles = 0;
             double blocks = 0;
@@ -57,11 +62,12 @@ Tiling ff_tiling(const Device* d, const Size* s, int n, int segments, bool gated
                 tiles += (s[i].rows + 128 * cg - 1) / (128 * cg) * ((s[i].cols + out - 1) / out);
                 if (blocks < (double)((s[i].contraction + 63) / 64)) blocks = (double)((s[i].contraction + 63) / 64);
             }
-            const double mma = 2.0 * bn, memory = (b_mn ? 1.75 : 1.6) * (128 + bn / cg), block = mma > memory ? mma : memory;
+            const double mma = 2.0 * bn, memory = (a_mn ? (cg == 1 ? 1.9 : 2.45) : (b_mn ? 1.75 : 1.6)) * (128 + bn / cg), block = mma > memory ? mma : memory;
+            const double between = bn == 512 ? 6500.0 : 1500.0;
             blocks *= segments;
-            for (int k = 1; k <= (may_split && tiles < slots ? 16 : 1); ++k) {
+            for (int k = 1; k <= (may_split && bn <= 256 && tiles < slots ? 16 : 1); ++k) {
                 if (k > 1 && blocks < 4 * k) break;
-                double cost = (double)((tiles * k + slots - 1) / slots) * (blocks / k * block + 1500.0);
+                double cost = (double)((tiles * k + slots - 1) / slots) * (blocks / k * block + between);
                 if (k > 1) cost += 4000.0 + tiles * k * 128.0 * cg * bn * 8.0 / 5000.0;
                 if (cost < least) { least = cost; best = {cg, bn, k}; }
             }
@@ -95,11 +101,11 @@ struct Launch {
         const long long tiles = (rows + bm - 1) / bm * ((cols + bn_out - 1) / bn_out);
         p.tile0[i + 1] = p.tile0[i] + (int)tiles;
     }
-    template <typename T, int EPI, bool A_MN, bool B_MN, int CG>
+    template <typename T, int EPI, bool A_MN, bool B_MN, int CG, int NB = 1>
     hf_status run_t(cudaStream_t st) {
-        typedef FfGemm<EPI, CG> C;
+        typedef FfGemm<EPI, CG, NB> C;
         p.stages = C::stages_for(p.bn);
-        auto kernel = k_ff_gemm<T, EPI, A_MN, B_MN, CG>;
+        auto kernel = k_ff_gemm<T, EPI, A_MN, B_MN, CG, NB>;
         HFL_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_MAX));
         const int tiles = p.tile0[p.products] * p.splits, slots = CG == 1 ? d->sm_count : d->pairs;
         cudaLaunchConfig_t cfg = {};
@@ -118,6 +124,11 @@ struct Launch {
     }
     template <int EPI, bool A_MN, bool B_MN>
     hf_status run(cudaStream_t st) {
+        if constexpr (A_MN)
+            if (tiling.bn == 512) {
+                p.bn = 256;
+                return type == HF_BF16 ? run_t<bf16, EPI, A_MN, B_MN, 2, 2>(st) : run_t<__half, EPI, A_MN, B_MN, 2, 2>(st);
+            }
         if (tiling.cg == 1) return type == HF_BF16 ? run_t<bf16, EPI, A_MN, B_MN, 1>(st) : run_t<__half, EPI, A_MN, B_MN, 1>(st);
         return type == HF_BF16 ? run_t<bf16, EPI, A_MN, B_MN, 2>(st) : run_t<__half, EPI, A_MN, B_MN, 2>(st);
     }
@@ -154,15 +165,15 @@ Sizes dw_sizes(const hf_ff_shape* g) {
 }
 Tiling cut_gated(const Device* d, const hf_ff_shape* g) {
     const Size s = {g->rows, g->hidden, g->width};
-    return ff_tiling(d, &s, 1, 1, true, false, 256, false);
+    return ff_tiling(d, &s, 1, 1, FF_CUT_GATED);
 }
-Tiling cut_y(const Device* d, const hf_ff_shape* g) { return ff_tiling(d, y_sizes(g).data, 1, 1, false, false); }
+Tiling cut_y(const Device* d, const hf_ff_shape* g) { return ff_tiling(d, y_sizes(g).data, 1, 1, FF_CUT_Y); }
 Tiling cut_dh(const Device* d, const hf_ff_shape* g) {
     const Size s = {g->rows, g->hidden, g->out_width};
-    return ff_tiling(d, &s, 1, 1, false, true, 128, false);
+    return ff_tiling(d, &s, 1, 1, FF_CUT_DH);
 }
-Tiling cut_dx(const Device* d, const hf_ff_shape* g) { return ff_tiling(d, dx_sizes(g).data, 1, 2, false, true); }
-Tiling cut_dw(const Device* d, const hf_ff_shape* g) { return ff_tiling(d, dw_sizes(g).data, 3, 1, false, true); }
+Tiling cut_dx(const Device* d, const hf_ff_shape* g) { return ff_tiling(d, dx_sizes(g).data, 1, 2, FF_CUT_DX); }
+Tiling cut_dw(const Device* d, const hf_ff_shape* g) { return ff_tiling(d, dw_sizes(g).data, 3, 1, FF_CUT_DW); }
 size_t ff_partial_bytes(const Tiling& t, const Size* s, int n) {
     if (t.splits == 1) return 0;
     size_t tiles = 0;
@@ -319,7 +330,7 @@ hf_status hf_gated_ff_backward(const hf_ff_shape* g, const void* dy, const void*
         HFL_TRY(l.mn_major(&l.p.a[0], dg)); HFL_TRY(l.mn_major(&l.p.a[1], du)); HFL_TRY(l.mn_major(&l.p.a[2], mdy));
         HFL_TRY(l.mn_major(&l.p.b[0], mx)); l.p.b[1] = l.p.b[0]; HFL_TRY(l.mn_major(&l.p.b[2], h));
         HFL_TRY(l.output(0, {dw_gate, N, K, K})); HFL_TRY(l.output(1, {dw_up, N, K, K})); HFL_TRY(l.output(2, {dw_down, O, N, N}));
-        l.product(N, (int)K, M, l.p.bn); l.product(N, (int)K, M, l.p.bn); l.product(O, (int)N, M, l.p.bn);
+        l.product(N, (int)K, M, l.tiling.bn); l.product(N, (int)K, M, l.tiling.bn); l.product(O, (int)N, M, l.tiling.bn);
         HFL_TRY((l.run<FF_STORE, true, true>(st)));
     }
     return HF_OK;

@@ -35,7 +35,9 @@ struct FfGemmParams {
     int* dev_status;
 };
 
-template <int EPI, int CG>
+// NB: accumulators of 256 columns a tile.  1: a tile's epilogue runs under the next tile's MMAs; 2 (STORE, long contractions): tiles of 512
+// columns, a quarter less operand traffic, with the epilogue in between.
+template <int EPI, int CG, int NB = 1>
 struct FfGemm {
     static constexpr int BM = 128, BK = 64;             // rows of a thread block, contraction of a stage
     static constexpr int A_BYTES = BM * BK * 2;
@@ -47,8 +49,8 @@ struct FfGemm {
     static constexpr int BOX = 64 * CW, STAGING = (EPI == FF_DHIDDEN ? 6 : 2) * BOX;
     static constexpr int BAR_BYTES = 384;
     static constexpr int SMEM_MAX = 232448;
-    // bn: columns of the tile, bn / CG of them in each thread block (in boxes of 64 where the operand is MN-major)
-    __host__ __device__ static constexpr int stage_bytes(int bn) { return A_BYTES + (bn / CG + 63) / 64 * 64 * BK * 2; }
+    // bn: columns of an accumulator; NB bn / CG columns of B in each thread block (in boxes of 64 where the operand is MN-major)
+    __host__ __device__ static constexpr int stage_bytes(int bn) { return A_BYTES + (NB * bn / CG + 63) / 64 * 64 * BK * 2; }
     static constexpr int smem_bytes(int bn, int stages) { return stages * stage_bytes(bn) + EPI_WARPS * STAGING + BAR_BYTES + 1024; }
     static constexpr int stages_for(int bn) {
         const int n = (SMEM_MAX - EPI_WARPS * STAGING - BAR_BYTES - 1024) / stage_bytes(bn);
@@ -204,11 +206,11 @@ struct FfOut {
     }
 };
 
-template <typename T, int EPI, bool A_MN, bool B_MN, int CG>
-__global__ void __launch_bounds__(FfGemm<EPI, CG>::THREADS, 1)
+template <typename T, int EPI, bool A_MN, bool B_MN, int CG, int NB = 1>
+__global__ void __launch_bounds__(FfGemm<EPI, CG, NB>::THREADS, 1)
 k_ff_gemm(const __grid_constant__ FfGemmParams p) {
     using namespace tc5;
-    typedef FfGemm<EPI, CG> C;
+    typedef FfGemm<EPI, CG, NB> C;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t s_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* s_gen = smem_raw + (s_base - smem_u32(smem_raw));
@@ -220,7 +222,8 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
     volatile int* abort_flag = reinterpret_cast<volatile int*>(bar_gen + 164);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = CG == 1 ? 0 : (int)(blockIdx.x & 1);                   // (clusters are two neighbouring thread blocks)
-    const int bn_out = EPI == FF_GATED ? p.bn / 2 : p.bn, bn_own = p.bn / CG;
+    const int bn_out = EPI == FF_GATED ? p.bn / 2 : NB * p.bn, bn_own = NB * p.bn / CG;
+    constexpr int ACCS = 2 / NB;                        // accumulators (sets of them) in turn
     const int n_tiles = p.tile0[p.products] * p.splits, tile_first = blockIdx.x / CG, tile_step = gridDim.x / CG;
 
     if (threadIdx.x == 0) {
@@ -293,6 +296,7 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
         const uint64_t da0 = smem_desc_sw128(s_base, A_MN ? 8192 : 16, 1024);
         const uint64_t db0 = smem_desc_sw128(s_base + C::A_BYTES, B_MN ? 8192 : 16, 1024);
         constexpr int A_STEP = (A_MN ? 2048 : 32) >> 4, B_STEP = (B_MN ? 2048 : 32) >> 4;
+        const int b_half = (p.bn / CG * C::BK * 2) >> 4;            // (NB 2: bn / CG is a multiple of 64)
         bool ok = rank == 0;
         int s = 0, acc = 0;
         uint32_t phase = 0, acc_phase = 1;
@@ -309,15 +313,16 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
                     const uint64_t off = (uint64_t)((s * stage_bytes) >> 4);
 #pragma unroll
                     for (int ks = 0; ks < C::BK / 16; ++ks)
-                        ff_mma<CG>(tmem + acc * 256, da0 + off + ks * A_STEP, db0 + off + ks * B_STEP, idesc, kb > 0 || ks > 0);
+#pragma unroll
+                        for (int h = 0; h < NB; ++h)
+                            ff_mma<CG>(tmem + (acc + h) * 256, da0 + off + ks * A_STEP, db0 + off + ks * B_STEP + h * b_half, idesc, kb > 0 || ks > 0);
                     ff_commit<CG>(bar_free + 8 * s);
                     if (kb == n_kb - 1) ff_commit<CG>(bar_acc + 8 * acc);
                 }
                 __syncwarp();
                 if (++s == stages) { s = 0; phase ^= 1; }
             }
-            if (acc) acc_phase ^= 1;
-            acc ^= 1;
+            if (++acc == ACCS) { acc = 0; acc_phase ^= 1; }
         }
     } else {
         // ================================================================= epilogue: warps w and w + 4 share the accumulator rows 32 (w & 3) ...
@@ -359,9 +364,12 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
             const bool rows_on = row < p.rows[tile.product];
             bool ok = true;
             for (int c = half; c < bn_out / CW; c += 2) {
-                const int col = tile.n0 + CW * c;
-                if (!rows_on || col >= cols) break;
-                const uint32_t at = lane_base + acc * 256 + CW * c;
+                // NB 2: columns h bn + ... of the accumulators are, of each thread block's half of the tile's columns, the h-th half
+                const int h2 = NB == 1 ? 0 : c / (p.bn / CW), in = CW * c - h2 * p.bn, owner = NB == 1 ? 0 : in / (p.bn / CG);
+                const int col = tile.n0 + (NB == 1 ? in : owner * bn_own + h2 * (p.bn / CG) + in - owner * (p.bn / CG));
+                if (!rows_on || (NB == 1 && col >= cols)) break;
+                if (NB == 2 && col >= cols) continue;
+                const uint32_t at = lane_base + (acc + h2) * 256 + in;
                 uint32_t r[32], o[16];
                 tmem_ld32(at, r);
                 if constexpr (EPI == FF_STORE) {
@@ -423,8 +431,7 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
             fence_before_sync();
             __syncwarp();
             if (lane == 0) ff_arrive_first<CG>(ff_first<CG>(bar_acc_free + 8 * acc));
-            if (acc) acc_phase ^= 1;
-            acc ^= 1;
+            if (++acc == ACCS) { acc = 0; acc_phase ^= 1; }
         }
         if (lane == 0) bulk_wait_all();
         if (EPI == FF_DHIDDEN && *abort_flag) {         // boxes in flight land before the thread block leaves
