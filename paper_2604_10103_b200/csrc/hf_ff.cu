@@ -276,6 +276,7 @@ hf_status hf_gated_ff(const hf_ff_shape* g, const void* x, const void* w_gate, c
     HFL_TRY(l.k_major(&l.p.b[0], {w_down, O, N, N}, l.p.bn / l.tiling.cg));
     HFL_TRY(l.output(0, {y, M, O, g->y_stride}));
     l.product(M, O, N, l.p.bn);
+    l.p.early_b = 1;
     return l.run<FF_STORE, false, false>(st);
 }
 
@@ -322,6 +323,7 @@ hf_status hf_gated_ff_backward(const hf_ff_shape* g, const void* dy, const void*
         HFL_TRY(l.output(0, {dx, M, K, K}));
         l.product(M, (int)K, N, l.p.bn);
         l.p.segments = 2; l.p.kb[1] = l.p.kb[0];
+        l.p.early_b = 1;
         HFL_TRY((l.run<FF_STORE, false, true>(st)));
     }
     if (n_dw) {

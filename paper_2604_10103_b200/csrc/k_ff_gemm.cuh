@@ -32,6 +32,7 @@ struct FfGemmParams {
     int bn;                             // accumulator columns of a tile: a multiple of 32 (GATED: half of them g, half u)
     int stages;
     int act, save;
+    int early_b;                        // B may be read before the kernel before this one is done
     int* dev_status;
 };
 
@@ -59,16 +60,16 @@ struct FfGemm {
 };
 
 namespace tc5 {
-template <int CG> __device__ __forceinline__ void ff_tmem_alloc(uint32_t smem_dst) {
-    if constexpr (CG == 1) { tmem_alloc(smem_dst, 512); tmem_relinquish(); }
+template <int CG> __device__ __forceinline__ void ff_tmem_alloc(uint32_t smem_dst, uint32_t columns) {
+    if constexpr (CG == 1) { tmem_alloc(smem_dst, columns); tmem_relinquish(); }
     else {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_dst), "r"(512) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_dst), "r"(columns) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;\n" ::: "memory");
     }
 }
-template <int CG> __device__ __forceinline__ void ff_tmem_dealloc(uint32_t taddr) {
-    if constexpr (CG == 1) tmem_dealloc(taddr, 512);
-    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;\n" ::"r"(taddr), "r"(512) : "memory");
+template <int CG> __device__ __forceinline__ void ff_tmem_dealloc(uint32_t taddr, uint32_t columns) {
+    if constexpr (CG == 1) tmem_dealloc(taddr, columns);
+    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;\n" ::"r"(taddr), "r"(columns) : "memory");
 }
 template <int CG> __device__ __forceinline__ void ff_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
     if constexpr (CG == 1) mma_ss(d, a, b, idesc, accumulate);
@@ -224,6 +225,7 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
     const int rank = CG == 1 ? 0 : (int)(blockIdx.x & 1);                   // (clusters are two neighbouring thread blocks)
     const int bn_out = EPI == FF_GATED ? p.bn / 2 : NB * p.bn, bn_own = NB * p.bn / CG;
     constexpr int ACCS = 2 / NB;                        // accumulators (sets of them) in turn
+    const uint32_t acc_stride = p.bn > 128 ? 256 : (p.bn > 64 ? 128 : 64);         // columns of tensor memory from one to the next
     const int n_tiles = p.tile0[p.products] * p.splits, tile_first = blockIdx.x / CG, tile_step = gridDim.x / CG;
 
     if (threadIdx.x == 0) {
@@ -234,15 +236,14 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
-    if (warp == C::WARP_MMA) ff_tmem_alloc<CG>(smem_u32(tmem_slot));
+    if (warp == C::WARP_MMA) ff_tmem_alloc<CG>(smem_u32(tmem_slot), 2 * acc_stride);
     fence_before_sync();
     ff_meet<CG>();
     fence_after_sync();
     const uint32_t tmem = *tmem_slot;
-    // (launched while the kernel before still runs; the next may be launched once this one may read what all before have written)
-    pdl_wait();
-    pdl_trigger();
-
+    // The kernel may have been launched while the one before it still runs: only the threads that read global memory themselves wait for
+    // that, everything else follows from what they read.  The next kernel may be launched once this one has waited, so that what was
+    // written before this one is there for it from the start (early_b).
     if (warp == C::WARP_TMA) {
         // ================================================================= loader
         if (lane == 0) {
@@ -251,30 +252,54 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
             uint32_t phase = 1;                 // (the stages are free at first)
             const int b_boxes = B_MN ? (bn_own + 63) / 64 : 1;
             const uint32_t bytes = CG * (C::A_BYTES + (B_MN ? b_boxes * 8192 : bn_own * C::BK * 2));        // of the whole tile
+            auto load_a = [&](const FfTile& tile, int k, uint32_t sA, uint32_t full) {
+                const int seg = p.segments > 1 && k >= p.kb[0], i = tile.product + seg;       // (one of the two is always 0)
+                const int kc = (k - seg * p.kb[0]) * C::BK, m0 = tile.m0 + rank * C::BM;
+                if (A_MN) {
+                    ff_load<CG>(sA, &p.a[i], m0, kc, full);
+                    ff_load<CG>(sA + 8192, &p.a[i], m0 + 64, kc, full);
+                } else
+                    ff_load<CG>(sA, &p.a[i], kc, m0, full);
+            };
+            auto load_b = [&](const FfTile& tile, int k, uint32_t sB, uint32_t full) {
+                const int seg = p.segments > 1 && k >= p.kb[0], i = tile.product + seg;
+                const int kc = (k - seg * p.kb[0]) * C::BK, n0 = tile.n0 + (EPI == FF_GATED ? 0 : rank * bn_own);
+                if (EPI == FF_GATED) {
+                    // g's columns in front of u's: the pair's first thread block holds Wg's rows, the second Wu's
+                    ff_load<CG>(sB, &p.b[rank], kc, n0, full);
+                    if (CG == 1) ff_load<CG>(sB + bn_out * C::BK * 2, &p.b[1], kc, n0, full);
+                } else if (B_MN) {
+                    for (int x = 0; x < b_boxes; ++x) ff_load<CG>(sB + x * 8192, &p.b[i], n0 + 64 * x, kc, full);
+                } else
+                    ff_load<CG>(sB, &p.b[i], kc, n0, full);
+            };
+            bool first = true;
             for (int t = tile_first; ok && t < n_tiles; t += tile_step) {
                 const FfTile tile = ff_tile(p, t, CG * C::BM, bn_out);
-                const int m0 = tile.m0 + rank * C::BM, n0 = tile.n0 + (EPI == FF_GATED ? 0 : rank * bn_own);
                 const int k_all = p.kb[tile.product] * p.segments;      // (segments: of the same length)
                 const int k_end = (int)((long long)k_all * (tile.split + 1) / p.splits);
-                for (int k = (int)((long long)k_all * tile.split / p.splits); k < k_end; ++k) {
+                int k = (int)((long long)k_all * tile.split / p.splits);
+                if (first) {
+                    first = false;
+                    // weights on their way before the rows of the other operand are there
+                    const int ahead = p.early_b ? min(stages, k_end - k) : 0;
+                    for (int j = 0; j < ahead; ++j) {
+                        if (rank == 0) mbar_expect_tx(bar_full + 8 * j, bytes);
+                        load_b(tile, k + j, s_base + j * stage_bytes + C::A_BYTES, ff_first<CG>(bar_full + 8 * j));
+                    }
+                    pdl_wait();
+                    pdl_trigger();
+                    for (int j = 0; j < ahead; ++j, ++k) {
+                        load_a(tile, k, s_base + j * stage_bytes, ff_first<CG>(bar_full + 8 * j));
+                        if (++s == stages) { s = 0; phase ^= 1; }
+                    }
+                }
+                for (; k < k_end; ++k) {
                     if (!(ok = mbar_wait<true>(bar_free + 8 * s, phase, abort_flag, p.dev_status, 81))) break;
-                    const int seg = p.segments > 1 && k >= p.kb[0], i = tile.product + seg;       // (one of the two is always 0)
-                    const int kc = (k - seg * p.kb[0]) * C::BK;
-                    const uint32_t sA = s_base + s * stage_bytes, sB = sA + C::A_BYTES, full = ff_first<CG>(bar_full + 8 * s);
+                    const uint32_t sA = s_base + s * stage_bytes, full = ff_first<CG>(bar_full + 8 * s);
                     if (rank == 0) mbar_expect_tx(bar_full + 8 * s, bytes);
-                    if (A_MN) {
-                        ff_load<CG>(sA, &p.a[i], m0, kc, full);
-                        ff_load<CG>(sA + 8192, &p.a[i], m0 + 64, kc, full);
-                    } else
-                        ff_load<CG>(sA, &p.a[i], kc, m0, full);
-                    if (EPI == FF_GATED) {
-                        // g's columns in front of u's: the pair's first thread block holds Wg's rows, the second Wu's
-                        ff_load<CG>(sB, &p.b[rank], kc, n0, full);
-                        if (CG == 1) ff_load<CG>(sB + bn_out * C::BK * 2, &p.b[1], kc, n0, full);
-                    } else if (B_MN) {
-                        for (int x = 0; x < b_boxes; ++x) ff_load<CG>(sB + x * 8192, &p.b[i], n0 + 64 * x, kc, full);
-                    } else
-                        ff_load<CG>(sB, &p.b[i], kc, n0, full);
+                    load_a(tile, k, sA, full);
+                    load_b(tile, k, sA + C::A_BYTES, full);
                     if (++s == stages) { s = 0; phase ^= 1; }
                 }
             }
@@ -315,7 +340,7 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
                     for (int ks = 0; ks < C::BK / 16; ++ks)
 #pragma unroll
                         for (int h = 0; h < NB; ++h)
-                            ff_mma<CG>(tmem + (acc + h) * 256, da0 + off + ks * A_STEP, db0 + off + ks * B_STEP + h * b_half, idesc, kb > 0 || ks > 0);
+                            ff_mma<CG>(tmem + (acc + h) * acc_stride, da0 + off + ks * A_STEP, db0 + off + ks * B_STEP + h * b_half, idesc, kb > 0 || ks > 0);
                     ff_commit<CG>(bar_free + 8 * s);
                     if (kb == n_kb - 1) ff_commit<CG>(bar_acc + 8 * acc);
                 }
@@ -355,7 +380,7 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
                 return;
             }
         };
-        if (EPI == FF_DHIDDEN && lane == 0) ask();
+        if (EPI == FF_DHIDDEN && lane == 0) { pdl_wait(); ask(); }
         for (int t = tile_first; t < n_tiles; t += tile_step) {
             const FfTile tile = ff_tile(p, t, CG * C::BM, bn_out);
             if (!mbar_wait_warp<true>(bar_acc + 8 * acc, acc_phase, abort_flag, p.dev_status, 84)) break;
@@ -369,7 +394,7 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
                 const int col = tile.n0 + (NB == 1 ? in : owner * bn_own + h2 * (p.bn / CG) + in - owner * (p.bn / CG));
                 if (!rows_on || (NB == 1 && col >= cols)) break;
                 if (NB == 2 && col >= cols) continue;
-                const uint32_t at = lane_base + (acc + h2) * 256 + in;
+                const uint32_t at = lane_base + (acc + h2) * acc_stride + in;
                 uint32_t r[32], o[16];
                 tmem_ld32(at, r);
                 if constexpr (EPI == FF_STORE) {
@@ -444,7 +469,7 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
     ff_meet<CG>();
     if (warp == C::WARP_MMA) {
         fence_after_sync();
-        ff_tmem_dealloc<CG>(tmem);
+        ff_tmem_dealloc<CG>(tmem, 2 * acc_stride);
     }
 }
 
