@@ -36,16 +36,15 @@ struct Matrix { const void* p; long long rows, cols, stride; };
 struct Tiling { int cg, bn, splits; };
 struct Size { long long rows, cols, contraction; };
 
-// The tiling of least estimated time: rounds of tiles over the device times a tile's cycles.  A block of 64 of the contraction costs the MMAs
-// 2 bn cycles, and shared memory, which takes each operand byte in and gives it out once, 2 x 128 (128 + bn / cg) bytes at 128 a cycle; how
-// much of that counts was seen to be four fifths with both operands K-major, a little more with an MN-major B, about all (pairs: 1.2 of
-// it) with both MN-major.  What was seen, us a call, of 4680 rows, width 1536, hidden 4096, the other products of the call unchanged: y in
-// tiles of one thread block x 256 columns 140.2, 192 139, 224 139; of two x 256 137, 224 135, 192 141, 128 151; dx one x 256 335, one x 192
-// 330, two x 256 321, two x 192 345; dw one x 256 335, two x 256 317 (later, with other parts faster, 292; two x 512 278); of 1560
-// rows g, u one x 256 63, two x 256 65; y one x 160 60, two x 192 57, two x 128 68.  An MN-major B comes in boxes of 64 columns a thread
-// block, and other widths were slower than this says (dw two x 256 317, two x 224 334).  Tiles of 512 columns (dw) have their epilogue
-// between the MMAs: some 5000 cycles.  Few tiles with a long contraction are split (STORE): their parts' sums cost 8 bytes an element and
-// part on the way through L2 and another launch.
+// The tiling of least estimated time, in cycles: rounds of tiles over the device, each of the tile's blocks of 64 of the contraction (2 bn cycles
+// of MMAs, or what bringing 128 + bn / cg columns of both operands into shared memory and out of it was seen to take, which depends on how
+// they lie) and some cycles between tiles.  Tiles of 512 columns (dW) have their epilogue between the MMAs.  STORE may split the contraction:
+// another launch, the parts' sums (8 bytes an element and part) on their way through L2, and something for each part.
+// What the numbers come from, us a call with the other products of the call unchanged, width 1536, hidden 4096, [thread blocks] x columns
+// (/ splits).  4680 rows: g, u 2x256 125.7, 1x256 130.6, 2x192 132; y 2x224 135, 2x256 137, 1x192 139, 1x256 140, 2x192 141, 2x128 151;
+// dx 2x256 321, 1x192 330, 1x256 335, 2x192 345; dW 2x512 278, 2x256 292, (2x256 317, 2x224 334, 1x256 335 before other parts were faster).
+// 1000 rows: dx 2x256/3 82, /2 87, /1 96, 2x128 92, 1x128 96.  300 rows: dx 1x128/4 56.5, 2x128/3 57, 1x64 67.5; y 1x64 30.5, 2x128 31; g, u 1x256
+// 31.9, 2x256 32, 1x128 35, 1x64 41.  77 rows: y 1x64/3 22.4, /4 23, /6 25.6, /1 26.8; dx 1x128/6 38.9, /4 40.9, /12 43.4, 1x64 57.9.
 enum FfCut { FF_CUT_GATED, FF_CUT_Y, FF_CUT_DH, FF_CUT_DX, FF_CUT_DW };
 Tiling ff_tiling(const Device* d, const Size* s, int n, int segments, FfCut cut) {
     const bool gated = cut == FF_CUT_GATED, b_mn = cut >= FF_CUT_DH, a_mn = cut == FF_CUT_DW, may_split = cut != FF_CUT_GATED && cut != FF_CUT_DH;
@@ -62,13 +61,14 @@ Tiling ff_tiling(const Device* d, const Size* s, int n, int segments, FfCut cut)
                 tiles += (s[i].rows + 128 * cg - 1) / (128 * cg) * ((s[i].cols + out - 1) / out);
                 if (blocks < (double)((s[i].contraction + 63) / 64)) blocks = (double)((s[i].contraction + 63) / 64);
             }
-            const double mma = 2.0 * bn, memory = (a_mn ? (cg == 1 ? 1.9 : 2.45) : (b_mn ? 1.75 : 1.6)) * (128 + bn / cg), block = mma > memory ? mma : memory;
+            const double columns = 128 + bn / cg, mma = 2.0 * bn;
+            const double memory = a_mn ? 430 + 0.78 * columns : (b_mn ? 260 + 0.95 * columns : 150 + 1.15 * columns), block = mma > memory ? mma : memory;
             const double between = bn == 512 ? 6500.0 : 1500.0;
             blocks *= segments;
             for (int k = 1; k <= (may_split && bn <= 256 && tiles < slots ? 16 : 1); ++k) {
                 if (k > 1 && blocks < 4 * k) break;
                 double cost = (double)((tiles * k + slots - 1) / slots) * (blocks / k * block + between);
-                if (k > 1) cost += 4000.0 + tiles * k * 128.0 * cg * bn * 8.0 / 5000.0;
+                if (k > 1) cost += 4000.0 + 1200.0 * k + tiles * k * 128.0 * cg * bn * 8.0 / 2300.0;
                 if (cost < least) { least = cost; best = {cg, bn, k}; }
             }
         }
@@ -182,11 +182,8 @@ size_t ff_partial_bytes(const Tiling& t, const Size* s, int n) {
     return tiles * t.splits * 128 * t.cg * t.bn * sizeof(float);
 }
 
-// Up to 16 rows: both products by k_ff_rows.
-#ifndef ROWS_MOST
-#define ROWS_MOST 16
-#endif
-constexpr int FF_ROWS_MOST = ROWS_MOST;
+// Up to 16 rows: both products by k_ff_rows (width 1536, hidden 4096: 1 row 10.5 us, 16 rows 13.7; with tiles 23.5; its form for 32 rows took 26).
+constexpr int FF_ROWS_MOST = 16;
 template <typename T, int NT, int ACT>
 hf_status launch_rows(const hf_ff_shape* g, const FfRowsParams& first, const FfRowsParams& second, cudaStream_t st) {
     HFL_TRY(launch_after(k_ff_rows<T, NT, true, ACT>, dim3((g->hidden + 7) / 8), dim3(256), 0, st, first));
