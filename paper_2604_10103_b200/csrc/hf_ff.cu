@@ -106,7 +106,8 @@ struct Launch {
         typedef FfGemm<EPI, CG, NB> C;
         p.stages = C::stages_for(p.bn);
         auto kernel = k_ff_gemm<T, EPI, A_MN, B_MN, CG, NB>;
-        HFL_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_MAX));
+        struct Key {};
+        HFL_TRY(allow_shared<Key>(d, kernel, C::SMEM_MAX));
         const int tiles = p.tile0[p.products] * p.splits, slots = CG == 1 ? d->sm_count : d->pairs;
         cudaLaunchConfig_t cfg = {};
         cudaLaunchAttribute attr[2];

@@ -119,11 +119,13 @@ NormPlan norm_bwd_plan(const hf_norm_shape* g, bool wide, int sms) {
     p.teams = 12 / warps;
     const long long most = (rows + 2 * n - 1) / (2 * n);
     if (p.teams > most) p.teams = most < 1 ? 1 : (int)most;
-    const int fixed = (g->width * 4 + 15) / 16 * 16 + p.teams * NORM_TEAM_BYTES, row = p.teams * 2 * g->width * e;
-    p.stages = wide ? (NORM_SMEM - fixed) / row : 0;
+    const int factors = (g->width * 4 + 15) / 16 * 16, row = 2 * g->width * e;
+    auto fit = [&] { return (NORM_SMEM - factors - p.teams * NORM_TEAM_BYTES) / (p.teams * row); };
+    while (wide && p.teams > 1 && fit() < 2) --p.teams;
+    p.stages = wide ? fit() : 0;
     if (p.stages > 4) p.stages = 4;
     if (p.stages < 2) p.stages = 0;             // (rows too long for rings)
-    p.smem = fixed + p.stages * row;
+    p.smem = factors + p.teams * (NORM_TEAM_BYTES + p.stages * row);
     const int join = p.teams * 2 * V * p.nv * p.tpr * 4;
     if (join > p.smem) p.smem = join;
     if (n > (rows + p.teams - 1) / p.teams) n = (rows + p.teams - 1) / p.teams;
@@ -162,8 +164,9 @@ hf_status launch_norm_of(const NormParams& p, bool wide, cudaStream_t st) {
 }
 
 template <typename T, int V, int NV, bool RING>
-hf_status launch_norm_bwd(const NormParams& p, const NormPlan& n, cudaStream_t st) {
-    if (n.smem > 48 * 1024) HFL_CUDA(cudaFuncSetAttribute(k_norm_bwd<T, V, NV, RING>, cudaFuncAttributeMaxDynamicSharedMemorySize, NORM_SMEM));
+hf_status launch_norm_bwd(const Device* d, const NormParams& p, const NormPlan& n, cudaStream_t st) {
+    struct Key {};
+    HFL_TRY(allow_shared<Key>(d, k_norm_bwd<T, V, NV, RING>, NORM_SMEM));
     k_norm_bwd<T, V, NV, RING><<<(unsigned)((long long)n.groups * n.group_blocks), dim3(n.tpr, n.teams), n.smem, st>>>(p);
     HFL_CUDA(cudaGetLastError());
     if (n.group_blocks > 1 && (p.dw || p.db))
@@ -172,26 +175,27 @@ hf_status launch_norm_bwd(const NormParams& p, const NormPlan& n, cudaStream_t s
     return HF_OK;
 }
 template <typename T, bool RING>
-hf_status launch_norm_bwd_wide(const NormParams& p, const NormPlan& n, cudaStream_t st) {
+hf_status launch_norm_bwd_wide(const Device* d, const NormParams& p, const NormPlan& n, cudaStream_t st) {
     if constexpr (sizeof(T) == 2) {
-        if (n.nv == 1) return launch_norm_bwd<T, 8, 1, RING>(p, n, st);
-        if (n.nv == 2) return launch_norm_bwd<T, 8, 2, RING>(p, n, st);
-        if (n.nv == 4) return launch_norm_bwd<T, 8, 4, RING>(p, n, st);
-        return launch_norm_bwd<T, 8, 6, RING>(p, n, st);
+        if (n.nv == 1) return launch_norm_bwd<T, 8, 1, RING>(d, p, n, st);
+        if (n.nv == 2) return launch_norm_bwd<T, 8, 2, RING>(d, p, n, st);
+        if (n.nv == 4) return launch_norm_bwd<T, 8, 4, RING>(d, p, n, st);
+        return launch_norm_bwd<T, 8, 6, RING>(d, p, n, st);
     } else {
-        if (n.nv == 2) return launch_norm_bwd<T, 4, 2, RING>(p, n, st);
-        if (n.nv == 4) return launch_norm_bwd<T, 4, 4, RING>(p, n, st);
-        if (n.nv == 8) return launch_norm_bwd<T, 4, 8, RING>(p, n, st);
-        return launch_norm_bwd<T, 4, 12, RING>(p, n, st);
+        if (n.nv == 2) return launch_norm_bwd<T, 4, 2, RING>(d, p, n, st);
+        if (n.nv == 4) return launch_norm_bwd<T, 4, 4, RING>(d, p, n, st);
+        if (n.nv == 8) return launch_norm_bwd<T, 4, 8, RING>(d, p, n, st);
+        return launch_norm_bwd<T, 4, 12, RING>(d, p, n, st);
     }
 }
 template <typename T>
-hf_status launch_norm_bwd_of(const NormParams& p, const NormPlan& n, cudaStream_t st) {
-    if (n.stages) return launch_norm_bwd_wide<T, true>(p, n, st);
-    if (n.wide) return launch_norm_bwd<T, 16 / sizeof(T), 48 * sizeof(T) / 16, false>(p, n, st);       // (only rows of over 9216 elements are too long for rings)
-    if (n.nv == 8) return launch_norm_bwd<T, 1, 8, false>(p, n, st);
-    if (n.nv == 24) return launch_norm_bwd<T, 1, 24, false>(p, n, st);
-    return launch_norm_bwd<T, 1, 48, false>(p, n, st);
+hf_status launch_norm_bwd_of(const Device* d, const NormParams& p, const NormPlan& n, cudaStream_t st) {
+    if (n.stages) return launch_norm_bwd_wide<T, true>(d, p, n, st);
+    if constexpr (sizeof(T) == 4)           // (rows of over 14300 floats are too long for a ring of two)
+        if (n.wide) return launch_norm_bwd<T, 4, 12, false>(d, p, n, st);
+    if (n.nv == 8) return launch_norm_bwd<T, 1, 8, false>(d, p, n, st);
+    if (n.nv == 24) return launch_norm_bwd<T, 1, 24, false>(d, p, n, st);
+    return launch_norm_bwd<T, 1, 48, false>(d, p, n, st);
 }
 
 // ------------------------------------------------------------------------------------------------ rotary positions
@@ -199,10 +203,10 @@ template <typename T, int V, bool HALVES, bool WIDE>
 hf_status launch_rope(RopeParams& p, int sms, cudaStream_t st) {
     p.units = p.head_dim / (2 * V);
     const long long threads = (long long)p.batch * p.tokens * p.units, blocks = (threads + 255) / 256;
-    // Heads are cut into slices while all thread blocks still run at once (four a multiprocessor), each with six heads at least: the angles
-    // are looked up once a slice.
-    int slices = (int)(4LL * sms / blocks);
-    const int most = (p.total_heads + 3) / 4;
+    // Heads are cut into slices while all thread blocks still run at once, a batch of heads each at least: the angles are
+    // looked up once a slice.
+    int slices = (int)((long long)ROPE_BLOCKS * sms / blocks);
+    const int batch = rope_batch<T, V, WIDE>(), most = (p.total_heads + batch - 1) / batch;
     p.slices = slices < 1 ? 1 : (slices > most ? most : slices);
     k_rope_axes<T, V, HALVES, WIDE><<<dim3((unsigned)blocks, p.slices), 256, 0, st>>>(p);
     HFL_CUDA(cudaGetLastError());
@@ -291,9 +295,9 @@ hf_status hf_layer_norm_backward(const hf_norm_shape* g, const void* dy, const v
     p.rows_per_group = g->rows_per_group; p.param_stride = g->param_stride;
     p.width = g->width; p.params_f32 = g->param_type == HF_F32; p.weight_offset = g->weight_offset; p.eps = g->eps; p.group_blocks = n.group_blocks;
     p.stages = n.stages; p.dev_status = d->status;
-    if (g->type == HF_BF16) return launch_norm_bwd_of<bf16>(p, n, st);
-    if (g->type == HF_F16) return launch_norm_bwd_of<__half>(p, n, st);
-    return launch_norm_bwd_of<float>(p, n, st);
+    if (g->type == HF_BF16) return launch_norm_bwd_of<bf16>(d, p, n, st);
+    if (g->type == HF_F16) return launch_norm_bwd_of<__half>(d, p, n, st);
+    return launch_norm_bwd_of<float>(d, p, n, st);
 }
 
 hf_status hf_rope_axes(const hf_rope_shape* g, const hf_rope_tensor* tensors, int n_tensors, const float* cos_tab, const float* sin_tab,

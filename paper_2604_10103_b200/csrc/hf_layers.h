@@ -20,6 +20,17 @@ hf_status count_pairs(int* pairs);
 inline int element_bytes(int type) { return type == HF_F32 ? 4 : 2; }
 inline bool aligned(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
+// Raises a kernel's limit of dynamic shared memory, once a device (KERNEL: the key, a type of the caller's that stands for the instantiation).
+template <typename KERNEL, typename F>
+hf_status allow_shared(const Device* d, F kernel, int bytes) {
+    static volatile bool done[64];
+    if (done[d->index]) return HF_OK;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != cudaSuccess) return fail(HF_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
+    done[d->index] = true;
+    return HF_OK;
+}
+
 // Launch of a kernel that may start while the one before it in the stream still runs (it calls pdl_wait() before it touches what that
 // kernel wrote).
 template <typename... P, typename... A>

@@ -2,7 +2,9 @@
 // axis, read from tables: (x0, x1) -> (x0 c - x1 s, x0 s + x1 c) (inverse: s -> -s, the transposed rotation, which is the backward pass).
 // Products and sums in float32, one rounding at the end.  Up to three tensors of [batch, tokens, heads, head_dim] with strides of their
 // own go through one launch (q, k, v between a projection's rows and head-major tensors); one that is not rotated is copied.
-// Memory bounds it: a thread keeps the angles of its features of a token in registers and walks heads with them.
+// Memory bounds it: a thread keeps the angles of its features of a token in registers and walks heads with them.  (Floors at the measured
+// copy rate: 13.2 and 92.3 us for the two sizes below; the rest is the launch and the first loads' latency, and in the long call reads and
+// writes of 256 bytes at a time on one of the two sides.)
 #pragma once
 #include "k_vec.cuh"
 
@@ -27,10 +29,16 @@ struct RopeParams {
 // HALVES: pair p = features (p, n_pairs + p), otherwise (2p, 2p + 1).  A thread owns 2 V features of a token: V pairs, or 2 V features
 // behind the rotated ones, in two pieces of V (neighbours unless HALVES).  WIDE: every piece of every tensor starts on a boundary of its
 // own size (at most 16 bytes); otherwise V is 1 and elements are accessed one by one.
+// Heads of a batch, whose loads are in flight together, and thread blocks a multiprocessor (registers): four 16-byte pieces and four thread
+// blocks.  Rows of 12 + 24 heads of 128, us for 4680 and (backward) 32760 tokens: 19.3, 111.5 (5.4 TB/s); batches of twelve and two thread
+// blocks 24.0, 146; of six and four 19.3, 112.3; of three and five 20.6, 109.5; of two and six 20.6, 125.
+template <typename T, int V, bool WIDE> __host__ __device__ constexpr int rope_batch() { return WIDE && V * sizeof(T) == 16 ? 2 : 4; }
+constexpr int ROPE_BLOCKS = 4;
+
 template <typename T, int V, bool HALVES, bool WIDE>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, ROPE_BLOCKS)
 k_rope_axes(const RopeParams p) {
-    constexpr int HB = 4;
+    constexpr int HB = rope_batch<T, V, WIDE>();
     const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
     const long long bt = id / p.units;
     if (bt >= (long long)p.batch * p.tokens) return;
@@ -40,6 +48,36 @@ k_rope_axes(const RopeParams p) {
     const bool turned = pair0 < p.n_pairs;                          // (HALVES: n_pairs is a multiple of V)
     const int f0 = HALVES && turned ? pair0 : 2 * pair0;
     const int f1 = HALVES && turned ? p.n_pairs + pair0 : f0 + V;
+    // this slice's part of all tensors' heads, one after the other; a batch stays inside a tensor
+    int h = (int)((long long)p.total_heads * blockIdx.y / p.slices), n = 0, base = 0;
+    const int h_end = (int)((long long)p.total_heads * (blockIdx.y + 1) / p.slices);
+    Vec<T, V, WIDE> lo[HB], hi[HB];
+    const T* x; T* y;
+    int stop;
+    auto seek = [&]() {             // the tensor of head h
+        while (h >= base + p.t[n].heads) { base += p.t[n].heads; ++n; }
+        const RopeTensor& t = p.t[n];
+        stop = min(h_end, base + t.heads);
+        x = static_cast<const T*>(t.x) + b * t.xb + tok * t.xt + (h - base) * t.xh;
+        y = static_cast<T*>(t.y) + b * t.yb + tok * t.yt + (h - base) * t.yh;
+    };
+    auto load = [&]() {
+        const long long xh = p.t[n].xh;
+#pragma unroll
+        for (int k = 0; k < HB; ++k)
+            if (h + k < stop) {
+                if constexpr (HALVES || !WIDE) {
+                    lo[k] = load_vec<T, V, WIDE>(x + k * xh + f0);
+                    hi[k] = load_vec<T, V, WIDE>(x + k * xh + f1);
+                } else {
+                    const Vec<T, 2 * V> v = load_vec<T, 2 * V>(x + k * xh + f0);
+                    memcpy(&lo[k], &v, sizeof(lo[k]));
+                    memcpy(&hi[k], reinterpret_cast<const char*>(&v) + sizeof(lo[k]), sizeof(hi[k]));
+                }
+            }
+    };
+    seek();
+    load();                         // (on its way while the angles are looked up)
     float c[V], s[V];
     bool on[V];
 #pragma unroll
@@ -61,65 +99,47 @@ k_rope_axes(const RopeParams p) {
             s[j] = p.inverse ? -p.sin_tab[e] : p.sin_tab[e];
         }
     }
-    // this slice's part of all tensors' heads, one after the other
-    int h = (int)((long long)p.total_heads * blockIdx.y / p.slices);
-    const int h_end = (int)((long long)p.total_heads * (blockIdx.y + 1) / p.slices);
-    int n = 0, base = 0;
-    while (n < p.n_tensors && h < h_end) {
+    // (x and y may be the same tensor: a thread writes only what it alone reads, and has read)
+    for (;;) {
         const RopeTensor& t = p.t[n];
-        if (h >= base + t.heads) { base += t.heads; ++n; continue; }
-        const int stop = min(h_end, base + t.heads);
-        const T* x = static_cast<const T*>(t.x) + b * t.xb + tok * t.xt + (h - base) * t.xh;
-        T* y = static_cast<T*>(t.y) + b * t.yb + tok * t.yt + (h - base) * t.yh;
-        const bool rot = t.rotate != 0;
-        // HB heads' loads are in flight together (x and y may be the same tensor, so the order of the code is the order of the accesses)
-        for (; h < stop; h += HB, x += HB * t.xh, y += HB * t.yh) {
-            Vec<T, V, WIDE> lo[HB], hi[HB];
 #pragma unroll
-            for (int k = 0; k < HB; ++k)
-                if (h + k < stop) {
-                    if constexpr (HALVES || !WIDE) {
-                        lo[k] = load_vec<T, V, WIDE>(x + k * t.xh + f0);
-                        hi[k] = load_vec<T, V, WIDE>(x + k * t.xh + f1);
-                    } else {
-                        const Vec<T, 2 * V> v = load_vec<T, 2 * V>(x + k * t.xh + f0);
-                        memcpy(&lo[k], &v, sizeof(lo[k]));
-                        memcpy(&hi[k], reinterpret_cast<const char*>(&v) + sizeof(lo[k]), sizeof(hi[k]));
-                    }
+        for (int k = 0; k < HB; ++k)
+            if (h + k < stop) {
+                if (t.rotate) {
+                    float e[2 * V], l[V], u2[V];
+                    to_floats(lo[k], l);
+                    to_floats(hi[k], u2);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) { e[j] = l[j]; e[V + j] = u2[j]; }
+#pragma unroll
+                    for (int j = 0; j < V; ++j)
+                        if (on[j]) {            // (an infinity behind the rotated pairs is copied, not multiplied by a zero sine)
+                            const int i0 = HALVES ? j : 2 * j, i1 = HALVES ? V + j : 2 * j + 1;     // neighbours: pair j is elements (2j, 2j + 1)
+                            const float x0 = e[i0], x1 = e[i1];
+                            e[i0] = x0 * c[j] - x1 * s[j];
+                            e[i1] = x0 * s[j] + x1 * c[j];
+                        }
+#pragma unroll
+                    for (int j = 0; j < V; ++j) { l[j] = e[j]; u2[j] = e[V + j]; }
+                    from_floats(lo[k], l);
+                    from_floats(hi[k], u2);
                 }
-#pragma unroll
-            for (int k = 0; k < HB; ++k)
-                if (h + k < stop) {
-                    if (rot) {
-                        float e[2 * V], l[V], u2[V];
-                        to_floats(lo[k], l);
-                        to_floats(hi[k], u2);
-#pragma unroll
-                        for (int j = 0; j < V; ++j) { e[j] = l[j]; e[V + j] = u2[j]; }
-#pragma unroll
-                        for (int j = 0; j < V; ++j)
-                            if (on[j]) {            // (an infinity behind the rotated pairs is copied, not multiplied by a zero sine)
-                                const int i0 = HALVES ? j : 2 * j, i1 = HALVES ? V + j : 2 * j + 1;     // neighbours: pair j is elements (2j, 2j + 1)
-                                const float x0 = e[i0], x1 = e[i1];
-                                e[i0] = x0 * c[j] - x1 * s[j];
-                                e[i1] = x0 * s[j] + x1 * c[j];
-                            }
-#pragma unroll
-                        for (int j = 0; j < V; ++j) { l[j] = e[j]; u2[j] = e[V + j]; }
-                        from_floats(lo[k], l);
-                        from_floats(hi[k], u2);
-                    }
-                    if constexpr (HALVES || !WIDE) {
-                        store_vec(y + k * t.yh + f0, lo[k]);
-                        store_vec(y + k * t.yh + f1, hi[k]);
-                    } else {
-                        Vec<T, 2 * V> v;
-                        memcpy(&v, &lo[k], sizeof(lo[k]));
-                        memcpy(reinterpret_cast<char*>(&v) + sizeof(lo[k]), &hi[k], sizeof(hi[k]));
-                        store_vec(y + k * t.yh + f0, v);
-                    }
+                if constexpr (HALVES || !WIDE) {
+                    store_vec(y + k * t.yh + f0, lo[k]);
+                    store_vec(y + k * t.yh + f1, hi[k]);
+                } else {
+                    Vec<T, 2 * V> v;
+                    memcpy(&v, &lo[k], sizeof(lo[k]));
+                    memcpy(reinterpret_cast<char*>(&v) + sizeof(lo[k]), &hi[k], sizeof(hi[k]));
+                    store_vec(y + k * t.yh + f0, v);
                 }
+            }
+        h += HB; x += HB * t.xh; y += HB * t.yh;
+        if (h >= stop) {
+            h = stop;
+            if (h >= h_end) break;
+            seek();
         }
-        h = stop;
+        load();
     }
 }

@@ -26,12 +26,10 @@ _F32 = torch.float32
 _empty_like = torch.empty_like
 
 
-def _device() -> int:
-    # torch's raw getter, which has no public name, spares a microsecond a call
-    try:
-        return torch._C._cuda_getDevice()
-    except AttributeError:
-        return torch.cuda.current_device()
+try:
+    _device = torch._C._cuda_getDevice          # torch's raw getter, which has no public name, spares a microsecond a call
+except AttributeError:
+    _device = torch.cuda.current_device
 
 
 def _fail(text: str):
@@ -43,10 +41,12 @@ def _here(name, t, dev):
         _fail(f"{name} is on {t.device}, not on the current CUDA device")
 
 
-def _current(t) -> int:
-    if not t.is_cuda:
-        _fail(f"a tensor on {t.device}: CUDA tensors are taken")
-    return _device()
+def _current(name, t) -> int:
+    """The current device, which t has to be on."""
+    dev = t.get_device()
+    if dev < 0 or dev != _device():
+        _fail(f"{name} is on {t.device}, not on the current CUDA device")
+    return dev
 
 
 def _like(name, t, dev, shape, dtype):
@@ -115,8 +115,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-6, weight_offset=0.0, rows_per_
     """y = (x - mean) * rstd * (weight_offset + weight) + bias over the last axis; returns (y, mean, rstd), the last two float32 [rows].
     x: bf16, f16 or f32 [..., width], rows with one common stride.  weight, bias: [width] or [1, width]; with rows_per_group > 0
     [groups, width], row r of x taking row r // rows_per_group (slices of a modulation tensor are fine); x's type or float32; or None."""
-    dev = _current(x)
-    _here("x", x, dev)
+    dev = _current("x", x)
     rows, width, stride = _rows("x", x)
     t = _norm_type(x, width)
     pt, ps = _norm_params(weight, bias, dev, x.dtype, width, -(-rows // rows_per_group) if rows_per_group > 0 else 1)
@@ -134,8 +133,7 @@ def _norm_workspace(dev, shape):
 
 def layer_norm_backward(dy, x, mean, rstd, weight=None, weight_offset=0.0, rows_per_group=0):
     """Gradients of `layer_norm`: (dx in x's type, dweight, dbias float32 [groups, width]).  mean, rstd: as the forward returned them."""
-    dev = _current(x)
-    _here("x", x, dev)
+    dev = _current("x", x)
     rows, width, stride = _rows("x", x)
     t = _norm_type(x, width)
     groups = -(-rows // rows_per_group) if rows_per_group > 0 else 1
@@ -179,8 +177,7 @@ def rope_axes(x, pos, tables, out=None, pairing="adjacent", inverse=False):
     """x [batch, tokens, heads, head_dim] (any strides, features contiguous) turned by its tokens' positions.  pos: int32 [tokens, axes]
     or [batch, tokens, axes]; tables: (cos, sin, extents, pairs per axis) as `rope.axis_tables` forms cos and sin, on the device.
     out: a tensor of x's shape and type with strides of its own, or x itself; None: a new one.  inverse: the backward pass."""
-    dev = _current(x)
-    _here("x", x, dev)
+    dev = _current("x", x)
     if x.dim() != 4:
         _fail("x is [batch, tokens, heads, head_dim]")
     if out is None:
@@ -199,8 +196,7 @@ def rope_axes(x, pos, tables, out=None, pairing="adjacent", inverse=False):
 def split_heads_rope(qkv, heads, kv_heads, pos, tables, pairing="adjacent"):
     """Rows of a fused projection [batch, tokens, (heads + 2 kv_heads) * head_dim] (row stride free) -> q, k, v [batch, heads, tokens, head_dim]
     as the hybrid attention takes them, q and k turned by their positions, in one launch."""
-    dev = _current(qkv)
-    _here("qkv", qkv, dev)
+    dev = _current("qkv", qkv)
     if qkv.dim() != 3:
         _fail("qkv is [batch, tokens, (heads + 2 kv_heads) * head_dim]")
     B, T, W = qkv.shape
@@ -222,8 +218,7 @@ def split_heads_rope(qkv, heads, kv_heads, pos, tables, pairing="adjacent"):
 
 def split_heads_rope_backward(dq, dk, dv, pos, tables, pairing="adjacent"):
     """Gradient of `split_heads_rope` with respect to the rows: [batch, tokens, (heads + 2 kv_heads) * head_dim], contiguous."""
-    dev = _current(dq)
-    _here("dq", dq, dev)
+    dev = _current("dq", dq)
     if dq.dim() != 4 or dk.dim() != 4:
         _fail("dq, dk, dv are [batch, heads, tokens, head_dim]")
     B, H, T, d = dq.shape
@@ -246,8 +241,7 @@ def split_heads_rope_backward(dq, dk, dv, pos, tables, pairing="adjacent"):
 # ------------------------------------------------------------------------------------------------ gated feed-forward
 def _ff_operands(x, w_gate, w_up, w_down, act):
     """(device, type, rows, width, hidden, out_width, row stride of x) of checked operands."""
-    dev = _current(x)
-    _here("x", x, dev)
+    dev = _current("x", x)
     rows, width, stride = _rows("x", x)
     if act not in _ACTS:
         _fail(f"act {act!r} unknown")
