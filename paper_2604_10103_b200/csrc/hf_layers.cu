@@ -96,33 +96,33 @@ bool norm_wide(const hf_norm_shape* g, const void* const* rows, const long long*
     return !((w || b) && norm_groups(g) > 1 && !stride_ok(g->param_stride, pe));
 }
 
-// Backward: threads a row, teams of them, thread blocks.  With 16-byte pieces a team has as few warps as its columns' sums fit in (48 columns
-// a thread; 32760 rows of 1536 bf16: 59 us, with 24 columns and two warps a team 64, with 16 and three 69); element by element, where a
-// thread's loads are many and short, eight columns a thread while there are warps.  A thread block has up to twelve warps, fewer where
-// there are not two rows a team for every multiprocessor.  The number of thread blocks depends on the shape and its alignment alone, as
-// the workspace does.
+// Backward: threads a row, teams of them, thread blocks.  A team has as few warps as its columns' sums fit in (48 columns a thread; 32760 rows
+// of 1536 bf16: 59 us, with 24 columns and two warps a team 64, with 16 and three 69).  A thread block has up to twelve warps, fewer where
+// there are not two rows a team for every multiprocessor or two rows of each team do not fit in shared memory.  The number of thread
+// blocks depends on the shape and its alignment alone, as the workspace does.
 NormPlan norm_bwd_plan(const hf_norm_shape* g, bool wide, int sms) {
     NormPlan p;
-    const int e = element_bytes(g->type), V = wide ? 16 / e : 1;
+    const int e = element_bytes(g->type), V = wide ? 16 / e : 4 / e;
     p.wide = wide;
     p.groups = norm_groups(g);
-    int warps = (g->width + 32 * (wide ? 48 : 8) - 1) / (32 * (wide ? 48 : 8));
-    if (warps > 12) warps = 12;
+    // (floats one by one want a few registers more: 32 columns a thread where twelve warps are enough then)
+    const int most_cols = V == 1 && g->width <= 12 * 32 * 32 ? 32 : 48, warps = (g->width + 32 * most_cols - 1) / (32 * most_cols);
     p.tpr = 32 * warps;
     p.nv = (g->width + V * p.tpr - 1) / (V * p.tpr);
     // (the instantiations)
     if (V == 8) p.nv = p.nv <= 1 ? 1 : (p.nv <= 2 ? 2 : (p.nv <= 4 ? 4 : 6));
     else if (V == 4) p.nv = p.nv <= 2 ? 2 : (p.nv <= 4 ? 4 : (p.nv <= 8 ? 8 : 12));
-    else p.nv = p.nv <= 8 ? 8 : (p.nv <= 24 ? 24 : 48);
+    else if (V == 2) p.nv = p.nv <= 4 ? 4 : (p.nv <= 12 ? 12 : 24);
+    else p.nv = p.nv <= 8 ? 8 : (p.nv <= 24 ? 24 : (p.nv <= 32 ? 32 : 48));
     const long long rows = g->rows_per_group ? (g->rows < g->rows_per_group ? g->rows : g->rows_per_group) : g->rows;
-    long long n = (sms + p.groups - 1) / p.groups;
-    p.teams = 12 / warps;
+    long long n = sms > p.groups ? sms / p.groups : 1;         // one round of thread blocks
+    p.teams = norm_bwd_warps(V * p.nv) / warps;
     const long long most = (rows + 2 * n - 1) / (2 * n);
     if (p.teams > most) p.teams = most < 1 ? 1 : (int)most;
-    const int factors = (g->width * 4 + 15) / 16 * 16, row = 2 * g->width * e;
+    const int factors = (g->width * 4 + 4 + 15) / 16 * 16, row = 2 * (wide ? g->width * e : (g->width * e + 30) / 16 * 16);
     auto fit = [&] { return (NORM_SMEM - factors - p.teams * NORM_TEAM_BYTES) / (p.teams * row); };
-    while (wide && p.teams > 1 && fit() < 2) --p.teams;
-    p.stages = wide ? fit() : 0;
+    while (p.teams > 1 && fit() < 2) --p.teams;
+    p.stages = fit();
     if (p.stages > 4) p.stages = 4;
     if (p.stages < 2) p.stages = 0;             // (rows too long for rings)
     p.smem = factors + p.teams * (NORM_TEAM_BYTES + p.stages * row);
@@ -133,10 +133,9 @@ NormPlan norm_bwd_plan(const hf_norm_shape* g, bool wide, int sms) {
     return p;
 }
 
-template <typename T, int V, int NV, int TPR>
+template <typename T, int V, int NV, int TPR, bool WIDE = true>
 hf_status launch_norm(const NormParams& p, cudaStream_t st) {
-    const unsigned blocks = TPR == 32 ? (unsigned)((p.rows + 7) / 8) : (unsigned)p.rows;
-    k_norm<T, V, NV, TPR><<<blocks, TPR == 32 ? 256 : TPR, 0, st>>>(p);
+    k_norm<T, V, NV, TPR, WIDE><<<TPR == 32 ? (unsigned)((p.rows + 7) / 8) : (unsigned)p.rows, TPR == 32 ? 256 : TPR, 0, st>>>(p);
     HFL_CUDA(cudaGetLastError());
     return HF_OK;
 }
@@ -157,45 +156,96 @@ hf_status launch_norm_of(const NormParams& p, bool wide, cudaStream_t st) {
         if (n <= 64) return launch_norm<T, V, 4, 512>(p, st);
         return launch_norm<T, V, 8, 512>(p, st);
     }
-    if (w <= 256) return launch_norm<T, 1, 8, 32>(p, st);
-    if (w <= 1024) return launch_norm<T, 1, 8, 128>(p, st);
-    if (w <= 4096) return launch_norm<T, 1, 8, 512>(p, st);
-    return launch_norm<T, 1, 32, 512>(p, st);
+    constexpr int P = 4 / sizeof(T);            // 16-bit elements in pairs
+    if (w <= 256) return launch_norm<T, P, 8 / P, 32, false>(p, st);
+    if (w <= 512) return launch_norm<T, P, 4 / P, 128, false>(p, st);
+    if (w <= 1024) return launch_norm<T, P, 8 / P, 128, false>(p, st);
+    if (w <= 2048) return launch_norm<T, P, 16 / P, 128, false>(p, st);
+    if (w <= 4096) return launch_norm<T, P, 8 / P, 512, false>(p, st);
+    if (w <= 8192) return launch_norm<T, P, 16 / P, 512, false>(p, st);
+    return launch_norm<T, P, 32 / P, 512, false>(p, st);
 }
 
-template <typename T, int V, int NV, bool RING>
+// Many rows (k_norm_rows): as norm_bwd_plan, with 24 warps a thread block, and no sums over rows to hold.  us, this / a thread block's rows at
+// once (k_norm): 28213 x 1456 bf16 34 / 40, 8000 rows 16.6 / 17.6, 4680 x 1536 10.3 / 9 (so from two rows a team on); rows that do not
+// start on 16 bytes, where the copies also align them: 28213 x 1455 61 / 125, 4000 rows 17 / 19, 600 rows 7.5 / 7.2, 300 rows 7.5 / 6.8,
+// 600 x 6001 10 / 16 (so from four rows a multiprocessor on).  Floats on 16 bytes: 28213 x 1536 69 / 58 (never).
+template <typename T, int V, int NV, bool WIDE>
+hf_status launch_norm_rows(const Device* d, const NormParams& p, const NormPlan& n, cudaStream_t st) {
+    struct Key {};
+    HFL_TRY(allow_shared<Key>(d, k_norm_rows<T, V, NV, WIDE>, NORM_SMEM));
+    k_norm_rows<T, V, NV, WIDE><<<(unsigned)(n.groups * n.group_blocks), dim3(n.tpr, n.teams), n.smem, st>>>(p);
+    HFL_CUDA(cudaGetLastError());
+    return HF_OK;
+}
+bool norm_rows_plan(const hf_norm_shape* g, bool wide, int sms, NormPlan* p) {
+    const int e = element_bytes(g->type), V = wide ? 16 / e : 4 / e;
+    p->groups = norm_groups(g);
+    const long long rows = g->rows_per_group ? (g->rows < g->rows_per_group ? g->rows : g->rows_per_group) : g->rows;
+    const int most_cols = V == 1 ? 24 : 48, warps = (g->width + 32 * most_cols - 1) / (32 * most_cols);
+    p->tpr = 32 * warps;
+    p->nv = (g->width + V * p->tpr - 1) / (V * p->tpr);
+    p->group_blocks = sms / p->groups;
+    if (p->group_blocks < 1 || (wide && e == 4)) return false;
+    p->teams = NORM_ROWS_WARPS / warps;
+    const long long each = (rows + p->group_blocks - 1) / p->group_blocks;
+    if (p->teams > each) p->teams = each < 1 ? 1 : (int)each;
+    const int factors = 2 * ((g->width * 4 + 4 + 15) / 16 * 16), row = wide ? g->width * e : (g->width * e + 30) / 16 * 16;
+    auto fit = [&] { return (NORM_SMEM - factors - p->teams * NORM_ROWS_TEAM_BYTES) / (p->teams * row); };
+    while (p->teams > 1 && fit() < 2) --p->teams;
+    p->stages = fit() > 4 ? 4 : fit();
+    p->smem = factors + p->teams * (NORM_ROWS_TEAM_BYTES + p->stages * row);
+    return p->stages >= 2 && (wide ? rows >= 2LL * p->group_blocks * p->teams : each >= 4);
+}
+template <typename T>
+hf_status launch_norm_rows_of(const Device* d, const NormParams& p, const NormPlan& n, bool wide, cudaStream_t st) {
+    constexpr int P = 4 / sizeof(T);
+    if constexpr (sizeof(T) == 2) {
+        if (wide) {
+            if (n.nv <= 1) return launch_norm_rows<T, 8, 1, true>(d, p, n, st);
+            if (n.nv <= 3) return launch_norm_rows<T, 8, 3, true>(d, p, n, st);
+            return launch_norm_rows<T, 8, 6, true>(d, p, n, st);
+        }
+        if (n.nv > 12) return launch_norm_rows<T, 2, 24, false>(d, p, n, st);
+    }
+    if (n.nv <= 8 / P) return launch_norm_rows<T, P, 8 / P, false>(d, p, n, st);
+    return launch_norm_rows<T, P, 24 / P, false>(d, p, n, st);
+}
+
+template <typename T, int V, int NV, bool RING, bool WIDE = true>
 hf_status launch_norm_bwd(const Device* d, const NormParams& p, const NormPlan& n, cudaStream_t st) {
     struct Key {};
-    HFL_TRY(allow_shared<Key>(d, k_norm_bwd<T, V, NV, RING>, NORM_SMEM));
-    k_norm_bwd<T, V, NV, RING><<<(unsigned)((long long)n.groups * n.group_blocks), dim3(n.tpr, n.teams), n.smem, st>>>(p);
+    HFL_TRY(allow_shared<Key>(d, k_norm_bwd<T, V, NV, RING, WIDE>, NORM_SMEM));
+    k_norm_bwd<T, V, NV, RING, WIDE><<<(unsigned)((long long)n.groups * n.group_blocks), dim3(n.tpr, n.teams), n.smem, st>>>(p);
     HFL_CUDA(cudaGetLastError());
     if (n.group_blocks > 1 && (p.dw || p.db))
         HFL_TRY(launch_after(k_norm_bwd_sum, dim3((p.width + 31) / 32, 2 * n.groups), dim3(32, 32), 0, st, (const float*)p.partials, n.group_blocks,
                              p.width, p.dw, p.db));
     return HF_OK;
 }
-template <typename T, bool RING>
-hf_status launch_norm_bwd_wide(const Device* d, const NormParams& p, const NormPlan& n, cudaStream_t st) {
-    if constexpr (sizeof(T) == 2) {
-        if (n.nv == 1) return launch_norm_bwd<T, 8, 1, RING>(d, p, n, st);
-        if (n.nv == 2) return launch_norm_bwd<T, 8, 2, RING>(d, p, n, st);
-        if (n.nv == 4) return launch_norm_bwd<T, 8, 4, RING>(d, p, n, st);
-        return launch_norm_bwd<T, 8, 6, RING>(d, p, n, st);
-    } else {
-        if (n.nv == 2) return launch_norm_bwd<T, 4, 2, RING>(d, p, n, st);
-        if (n.nv == 4) return launch_norm_bwd<T, 4, 4, RING>(d, p, n, st);
-        if (n.nv == 8) return launch_norm_bwd<T, 4, 8, RING>(d, p, n, st);
-        return launch_norm_bwd<T, 4, 12, RING>(d, p, n, st);
-    }
-}
 template <typename T>
 hf_status launch_norm_bwd_of(const Device* d, const NormParams& p, const NormPlan& n, cudaStream_t st) {
-    if (n.stages) return launch_norm_bwd_wide<T, true>(d, p, n, st);
     if constexpr (sizeof(T) == 4)           // (rows of over 14300 floats are too long for a ring of two)
-        if (n.wide) return launch_norm_bwd<T, 4, 12, false>(d, p, n, st);
-    if (n.nv == 8) return launch_norm_bwd<T, 1, 8, false>(d, p, n, st);
-    if (n.nv == 24) return launch_norm_bwd<T, 1, 24, false>(d, p, n, st);
-    return launch_norm_bwd<T, 1, 48, false>(d, p, n, st);
+        if (!n.stages) return n.wide ? launch_norm_bwd<T, 4, 12, false>(d, p, n, st) : launch_norm_bwd<T, 1, 48, false, false>(d, p, n, st);
+    if (!n.wide) {
+        constexpr int P = 4 / sizeof(T);
+        if (n.nv == 8 / P) return launch_norm_bwd<T, P, 8 / P, true, false>(d, p, n, st);
+        if (n.nv == 24 / P) return launch_norm_bwd<T, P, 24 / P, true, false>(d, p, n, st);
+        if constexpr (P == 1)
+            if (n.nv == 32) return launch_norm_bwd<T, 1, 32, true, false>(d, p, n, st);
+        return launch_norm_bwd<T, P, 48 / P, true, false>(d, p, n, st);
+    }
+    if constexpr (sizeof(T) == 2) {
+        if (n.nv == 1) return launch_norm_bwd<T, 8, 1, true>(d, p, n, st);
+        if (n.nv == 2) return launch_norm_bwd<T, 8, 2, true>(d, p, n, st);
+        if (n.nv == 4) return launch_norm_bwd<T, 8, 4, true>(d, p, n, st);
+        return launch_norm_bwd<T, 8, 6, true>(d, p, n, st);
+    } else {
+        if (n.nv == 2) return launch_norm_bwd<T, 4, 2, true>(d, p, n, st);
+        if (n.nv == 4) return launch_norm_bwd<T, 4, 4, true>(d, p, n, st);
+        if (n.nv == 8) return launch_norm_bwd<T, 4, 8, true>(d, p, n, st);
+        return launch_norm_bwd<T, 4, 12, true>(d, p, n, st);
+    }
 }
 
 // ------------------------------------------------------------------------------------------------ rotary positions
@@ -244,6 +294,13 @@ hf_status hf_layer_norm(const hf_norm_shape* g, const void* x, const void* weigh
     const long long strides[2] = {g->x_stride, g->y_stride};
     const bool wide = norm_wide(g, rows, strides, 2, weight, bias);
     const cudaStream_t st = (cudaStream_t)stream;
+    NormPlan n;
+    if (norm_rows_plan(g, wide, d->sm_count, &n)) {
+        p.group_blocks = n.group_blocks; p.stages = n.stages; p.dev_status = d->status;
+        if (g->type == HF_BF16) return launch_norm_rows_of<bf16>(d, p, n, wide, st);
+        if (g->type == HF_F16) return launch_norm_rows_of<__half>(d, p, n, wide, st);
+        return launch_norm_rows_of<float>(d, p, n, wide, st);
+    }
     if (g->type == HF_BF16) return launch_norm_of<bf16>(p, wide, st);
     if (g->type == HF_F16) return launch_norm_of<__half>(p, wide, st);
     return launch_norm_of<float>(p, wide, st);

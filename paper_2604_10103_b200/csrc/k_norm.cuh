@@ -9,6 +9,9 @@
 #include "tc5_common.cuh"
 
 constexpr int NORM_TEAM_BYTES = 64 + 2 * 12 * 8;          // backward, per team: up to 8 barriers, two buffers of sums of up to 12 warps
+constexpr int NORM_ROWS_TEAM_BYTES = 64 + 4 * 24 * 4;     // forward, many rows: up to 8 barriers, four sums of up to 24 warps
+// Warps of a thread block of the backward kernel, by the columns of a thread (registers): short rows are bound by their latency, and want more.
+__host__ __device__ constexpr int norm_bwd_warps(int columns) { return columns <= 16 ? 24 : 12; }
 
 struct NormParams {
     const void* x; void* y;                 // forward; backward: y = dx
@@ -26,16 +29,18 @@ struct NormParams {
     int* dev_status;
 };
 
-// V parameters from column col of row g on.
-template <typename T, int V>
-__device__ __forceinline__ void norm_params(const void* base, bool f32, long long row_at, int col, float (&out)[V]) {
+// V parameters from column col of row g on; `two`: of a pair, whether there is a second.
+template <typename T, int V, bool WIDE>
+__device__ __forceinline__ void norm_params(const void* base, bool f32, long long row_at, int col, float (&out)[V], bool two) {
     if (f32) {
-        const Vec<float, V> p = load_vec<float, V>(static_cast<const float*>(base) + row_at + col);
-        to_floats(p, out);
-    } else {
-        const Vec<T, V> p = load_vec<T, V>(static_cast<const T*>(base) + row_at + col);
-        to_floats(p, out);
-    }
+        const float* p = static_cast<const float*>(base) + row_at + col;
+        if constexpr (WIDE) to_floats(load_vec<float, V>(p), out);
+        else {
+            out[0] = p[0];
+            if constexpr (V == 2) out[1] = two ? p[1] : 0.f;
+        }
+    } else
+        Row<T, V, WIDE>(static_cast<const T*>(base) + row_at).get(col, out, two);
 }
 
 __device__ __forceinline__ float warp_sum(float v) {
@@ -59,24 +64,32 @@ __device__ __forceinline__ float row_sum(float v, float* shared) {
 
 // TPR threads share a row and hold V NV elements of it each.  TPR 32: eight rows a thread block of eight warps; otherwise one row.
 // The row stays packed (at most 64 registers a thread for the row lengths of models, so that 4736 rows are at work at a time).
-template <typename T, int V, int NV, int TPR>
-__global__ void __launch_bounds__(TPR == 32 ? 256 : TPR, TPR == 32 ? 4 : (TPR == 128 && NV <= 4 ? 8 : 1))
+// WIDE: 16-byte pieces; otherwise 16-bit elements in pairs, whatever the rows' alignment, and floats one by one.
+template <typename T, int V, int NV, int TPR, bool WIDE>
+__global__ void __launch_bounds__(TPR == 32 ? 256 : TPR, TPR == 32 ? 4 : (TPR == 128 && NV * V <= 32 ? 8 : 1))
 k_norm(const NormParams p) {
     __shared__ float s_sum[2][TPR / 32];
     const int t = TPR == 32 ? threadIdx.x & 31 : threadIdx.x;
     const long long row = TPR == 32 ? (long long)blockIdx.x * 8 + (threadIdx.x >> 5) : blockIdx.x;
     if (row >= p.rows) return;                  // (a whole warp; with TPR > 32 the grid is the rows)
-    const T* x = static_cast<const T*>(p.x) + row * p.x_stride;
     Vec<T, V> xv[NV];
-    float s = 0.f;
+    const Row<T, V, WIDE> x(static_cast<const T*>(p.x) + row * p.x_stride);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int col = (i * TPR + t) * V;
-        if (col < p.width) xv[i] = load_vec<T, V>(x + col);
+        if constexpr (WIDE) {
+            if (col < p.width) xv[i] = load_vec<T, V>(x.p + col);
+        } else {                                // (many short steps: no branch among them, so that their loads overlap)
+            float f[V];
+            x.get(col < p.width ? col : 0, f, col + 1 < p.width);
+            if (col >= p.width) f[0] = 0.f;
+            from_floats(xv[i], f);              // (exact: they were of this type)
+        }
     }
+    float s = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
-        if ((i * TPR + t) * V < p.width) {
+        if (!WIDE || (i * TPR + t) * V < p.width) {
             float f[V];
             to_floats(xv[i], f);
 #pragma unroll
@@ -87,13 +100,18 @@ k_norm(const NormParams p) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) stay_packed(xv[i]);
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-        if ((i * TPR + t) * V < p.width) {
+    for (int i = 0; i < NV; ++i) {
+        const int col = (i * TPR + t) * V;
+        if (!WIDE || col < p.width) {
             float f[V];
             to_floats(xv[i], f);
 #pragma unroll
-            for (int j = 0; j < V; ++j) { const float c = f[j] - mean; s = fmaf(c, c, s); }
+            for (int j = 0; j < V; ++j) {
+                const float c = WIDE || col + j < p.width ? f[j] - mean : 0.f;
+                s = fmaf(c, c, s);
+            }
         }
+    }
     const float rstd = 1.f / sqrtf(row_sum<TPR>(s, s_sum[1]) / (float)p.width + p.eps);
     if (t == 0) {
         if (p.mean) p.mean[row] = mean;
@@ -105,35 +123,176 @@ k_norm(const NormParams p) {
     T* y = static_cast<T*>(p.y) + row * p.y_stride;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int col = (i * TPR + t) * V;
-        if (col >= p.width) continue;
-        float a[V], b[V];
+        int col = (i * TPR + t) * V;
+        if constexpr (WIDE) { if (col >= p.width) continue; }
+        const bool in = col < p.width, two = col + 1 < p.width;
+        if constexpr (!WIDE) col = in ? col : 0;
+        float a[V], b[V], f[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) { a[j] = 1.f; b[j] = 0.f; }
         if (p.w) {
-            norm_params<T, V>(p.w, p.params_f32, at, col, a);
+            norm_params<T, V, WIDE>(p.w, p.params_f32, at, col, a, two);
 #pragma unroll
             for (int j = 0; j < V; ++j) a[j] += p.weight_offset;
         }
-        if (p.b) norm_params<T, V>(p.b, p.params_f32, at, col, b);
-        Vec<T, V> o;
-        float f[V];
+        if (p.b) norm_params<T, V, WIDE>(p.b, p.params_f32, at, col, b, two);
         to_floats(xv[i], f);
 #pragma unroll
         for (int j = 0; j < V; ++j) f[j] = fmaf((f[j] - mean) * rstd, a[j], b[j]);
-        from_floats(o, f);
-        store_vec(y + col, o);
+        if (in) put_floats<T, V, WIDE>(y + col, f, two);
+    }
+}
+
+// The same for many rows: thread blocks stay, one a multiprocessor, and their teams of tpr threads walk the rows of a group (the factors and
+// shifts of the group in shared memory), each with a ring of `stages` rows in shared memory that bulk copies fill: as k_norm_bwd does,
+// which see.  A row's stage is free as soon as its elements are in the team's registers.
+constexpr int NORM_ROWS_WARPS = 24;
+template <typename T, int V, int NV, bool WIDE>
+__global__ void __launch_bounds__(32 * NORM_ROWS_WARPS, 1)
+k_norm_rows(const NormParams p) {
+    extern __shared__ __align__(16) uint8_t s_raw[];    // factors [width], shifts [width] | per team: barriers, sums | rings
+    const int t = threadIdx.x, tpr = blockDim.x, team = threadIdx.y, teams = blockDim.y, warps = tpr >> 5;
+    const int nb = p.group_blocks, slot = blockIdx.x % nb;
+    const long long g = blockIdx.x / nb, g0 = p.rows_per_group ? g * p.rows_per_group : 0;
+    const long long g1 = p.rows_per_group ? min(p.rows, g0 + p.rows_per_group) : p.rows;
+    const float inv = 1.f / (float)p.width;
+    const int factor_bytes = (p.width * 4 + 4 + 15) / 16 * 16;
+    float* s_a = reinterpret_cast<float*>(s_raw);
+    float* s_b = reinterpret_cast<float*>(s_raw + factor_bytes);
+    uint8_t* s_team = s_raw + 2 * factor_bytes + team * NORM_ROWS_TEAM_BYTES;
+    float* s_sum = reinterpret_cast<float*>(s_team + 64);               // [2 rows in turn][sum, squares][warps of the team]
+    const uint32_t row_bytes = p.width * sizeof(T), slot_bytes = WIDE ? row_bytes : (row_bytes + 30) / 16 * 16;
+    uint8_t* s_ring = s_raw + 2 * factor_bytes + teams * NORM_ROWS_TEAM_BYTES + (size_t)team * p.stages * slot_bytes;
+    const uint32_t bar = smem_u32(s_team), ring = smem_u32(s_ring);
+    const long long first = g0 + (long long)slot * teams, step = (long long)nb * teams;
+    auto load = [&](long long row, int s) {
+        const T* from = static_cast<const T*>(p.x) + row * p.x_stride;
+        const uint32_t lead = WIDE ? 0 : (uint32_t)(reinterpret_cast<uintptr_t>(from) & 15), bytes = WIDE ? row_bytes : (lead + row_bytes + 15) / 16 * 16;
+        tc5::mbar_expect_tx(bar + 8 * s, bytes);
+        tc5::bulk_load(ring + s * slot_bytes, reinterpret_cast<const uint8_t*>(from) - lead, bytes, bar + 8 * s);
+    };
+    if (t == 0) {
+        for (int s = 0; s < p.stages; ++s) tc5::mbar_init(bar + 8 * s, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+        for (int s = 0; s < p.stages && first + team + s * step < g1; ++s) load(first + team + s * step, s);
+    }
+    // (V 8: the first and the second four of a thread's eight columns apart, so that neighbouring threads read neighbouring 16 bytes)
+    for (int c = team * tpr + t; c < p.width; c += teams * tpr) {
+        float a[1] = {1.f}, b[1] = {0.f};
+        if (p.w) { norm_params<T, 1, false>(p.w, p.params_f32, g * p.param_stride, c, a, false); a[0] += p.weight_offset; }
+        if (p.b) norm_params<T, 1, false>(p.b, p.params_f32, g * p.param_stride, c, b, false);
+        const int at = V == 8 ? (c >> 2 & 1) * (p.width / 2) + (c >> 3) * 4 + (c & 3) : c;
+        s_a[at] = a[0]; s_b[at] = b[0];
+    }
+    __syncthreads();
+    auto factors = [&](const float* from, int col, float (&a)[V]) {
+        if constexpr (V == 8) {
+            const float4 lo = *reinterpret_cast<const float4*>(from + col / 2), hi = *reinterpret_cast<const float4*>(from + p.width / 2 + col / 2);
+            a[0] = lo.x; a[1] = lo.y; a[2] = lo.z; a[3] = lo.w; a[4] = hi.x; a[5] = hi.y; a[6] = hi.z; a[7] = hi.w;
+        } else if constexpr (V == 2) {
+            const float2 v = *reinterpret_cast<const float2*>(from + col);
+            a[0] = v.x; a[1] = v.y;
+        } else
+            to_floats(load_vec<float, V>(from + col), a);
+    };
+    int stage = 0, buf = 0;
+    uint32_t phase = 0;
+    for (long long r0 = first; r0 < g1; r0 += step, buf ^= 1) {         // (the teams walk in step)
+        const long long row = r0 + team;
+        const bool on = row < g1;
+        const T* gx = static_cast<const T*>(p.x) + row * p.x_stride;
+        const Row<T, V, WIDE> x(s_ring + stage * slot_bytes, WIDE ? 0 : (uint32_t)(reinterpret_cast<uintptr_t>(gx) & 15));
+        // bounded like every wait: a row that never came would leave garbage, and the flag
+        if (on && !tc5::mbar_try_wait(bar + 8 * stage, phase)) {
+            const long long t0 = clock64();
+            while (!tc5::mbar_try_wait(bar + 8 * stage, phase) && clock64() - t0 < tc5::WAIT_LIMIT_CYCLES) {}
+            if (clock64() - t0 >= tc5::WAIT_LIMIT_CYCLES) {
+                atomicOr(p.dev_status, HF_DEV_TIMEOUT_FLAG);
+                atomicExch(p.dev_status + 1, 92);
+            }
+        }
+        Vec<T, V> xv[NV];
+        float s[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) s[j] = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int col = (i * tpr + t) * V;
+            float f[V];
+            x.get(col < p.width ? col : 0, f, col + 1 < p.width);
+            if (col >= p.width) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) f[j] = 0.f;
+            }
+            from_floats(xv[i], f);              // (exact: they were of this type)
+            vadd(s, f);
+        }
+        float* own = s_sum + buf * 2 * warps;
+        float sum = warp_sum(vsum(s));
+        if (tpr > 32) {
+            if ((t & 31) == 0) own[t >> 5] = sum;
+            __syncthreads();
+            sum = 0.f;
+            for (int w = 0; w < warps; ++w) sum += own[w];
+        }
+        // (every thread of the team has its elements)
+        if (t == 0 && on && row + p.stages * step < g1) load(row + p.stages * step, stage);
+        if (++stage == p.stages) { stage = 0; phase ^= 1; }
+        const float mean = sum * inv;
+#pragma unroll
+        for (int j = 0; j < V; ++j) s[j] = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) stay_packed(xv[i]);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int col = (i * tpr + t) * V;
+            float f[V];
+            to_floats(xv[i], f);
+#pragma unroll
+            for (int j = 0; j < V; ++j) f[j] = (WIDE ? col : col + j) < p.width ? f[j] - mean : 0.f;
+            vfma(s, f, f, s);
+        }
+        sum = warp_sum(vsum(s));
+        if (tpr > 32) {
+            if ((t & 31) == 0) own[warps + (t >> 5)] = sum;
+            __syncthreads();
+            sum = 0.f;
+            for (int w = 0; w < warps; ++w) sum += own[warps + w];
+        }
+        const float rstd = 1.f / sqrtf(sum * inv + p.eps);
+        if (!on) continue;
+        if (t == 0) {
+            if (p.mean) p.mean[row] = mean;
+            if (p.rstd) p.rstd[row] = rstd;
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) stay_packed(xv[i]);
+        T* y = static_cast<T*>(p.y) + row * p.y_stride;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int col = (i * tpr + t) * V;
+            const bool in = col < p.width;
+            float f[V], a[V], b[V];
+            to_floats(xv[i], f);
+            factors(s_a, in ? col : 0, a);
+            factors(s_b, in ? col : 0, b);
+#pragma unroll
+            for (int j = 0; j < V; ++j) f[j] = (f[j] - mean) * rstd;
+            vfma(f, f, a, b);
+            if (in) put_floats<T, V, WIDE>(y + col, f, col + 1 < p.width);
+        }
     }
 }
 
 // grid groups x thread blocks per group, block (tpr, teams): a team of tpr threads shares a row, each thread V NV columns of it, the same
 // ones in every row, so that the sums over rows stay in its registers (2 V NV of them, at most 96); at the end the teams' sums are added in
 // shared memory, in order, and a thread block writes one partial of the group's dw and db (the only one: dw and db themselves).  A row is
-// read twice, for its sums and for dx, from where it lies: RING (16-byte pieces): each team has a ring of `stages` rows of x and dy in
-// shared memory, filled by bulk copies, so memory's latency is hidden whatever the registers allow; otherwise from global memory, the
-// second time out of the caches.  A team of one warp (rows of up to 1536 16-bit elements) needs no barrier.
-template <typename T, int V, int NV, bool RING>
-__global__ void __launch_bounds__(384, 1)
+// read twice, for its sums and for dx, from where it lies: RING: each team has a ring of `stages` rows of x and dy in shared memory, filled by
+// bulk copies, so memory's latency is hidden whatever the registers allow; otherwise (rows too long for that) from global memory, the second
+// time out of the caches.  A team of one warp (rows of up to 1536 elements) needs no barrier.  WIDE: rows start on 16 bytes and are taken
+// in such pieces; otherwise a copy takes the 16-byte units that hold the row, and threads take 16-bit elements in pairs, floats one by one.
+template <typename T, int V, int NV, bool RING, bool WIDE>
+__global__ void __launch_bounds__(32 * norm_bwd_warps(V * NV), 1)
 k_norm_bwd(const NormParams p) {
     extern __shared__ __align__(16) uint8_t s_raw[];    // factors [width] | per team: barriers, sums | rings; at the end the teams' sums
     const int t = threadIdx.x, tpr = blockDim.x, team = threadIdx.y, teams = blockDim.y, warps = tpr >> 5;
@@ -141,19 +300,26 @@ k_norm_bwd(const NormParams p) {
     const long long g = blockIdx.x / nb, g0 = p.rows_per_group ? g * p.rows_per_group : 0;
     const long long g1 = p.rows_per_group ? min(p.rows, g0 + p.rows_per_group) : p.rows;
     const float inv = 1.f / (float)p.width;
-    const int factor_bytes = (p.width * 4 + 15) / 16 * 16;
+    const int factor_bytes = (p.width * 4 + 4 + 15) / 16 * 16;
     float* s_a = reinterpret_cast<float*>(s_raw);
     uint8_t* s_team = s_raw + factor_bytes + team * NORM_TEAM_BYTES;
     float2* s_sum = reinterpret_cast<float2*>(s_team + 64);             // [2][warps of the team]
-    const uint32_t row_bytes = p.width * sizeof(T);
-    uint8_t* s_ring = s_raw + factor_bytes + teams * NORM_TEAM_BYTES + (size_t)team * p.stages * 2 * row_bytes;
+    const uint32_t row_bytes = p.width * sizeof(T), slot_bytes = WIDE ? row_bytes : (row_bytes + 30) / 16 * 16;
+    uint8_t* s_ring = s_raw + factor_bytes + teams * NORM_TEAM_BYTES + (size_t)team * p.stages * 2 * slot_bytes;
     const uint32_t bar = smem_u32(s_team), ring = smem_u32(s_ring);
     const long long first = g0 + (long long)slot * teams, step = (long long)nb * teams;     // the thread block's rows, one for each team
     // one thread of the team: the copies of a row into stage s
     auto load = [&](long long row, int s) {
-        tc5::mbar_expect_tx(bar + 8 * s, 2 * row_bytes);
-        tc5::bulk_load(ring + 2 * s * row_bytes, static_cast<const T*>(p.x) + row * p.x_stride, row_bytes, bar + 8 * s);
-        tc5::bulk_load(ring + (2 * s + 1) * row_bytes, static_cast<const T*>(p.dy) + row * p.y_stride, row_bytes, bar + 8 * s);
+        const T* from[2] = {static_cast<const T*>(p.x) + row * p.x_stride, static_cast<const T*>(p.dy) + row * p.y_stride};
+        uint32_t lead[2] = {0, 0}, bytes[2] = {row_bytes, row_bytes};
+        if constexpr (!WIDE) {
+            lead[0] = (uint32_t)(reinterpret_cast<uintptr_t>(from[0]) & 15); lead[1] = (uint32_t)(reinterpret_cast<uintptr_t>(from[1]) & 15);
+            bytes[0] = (lead[0] + row_bytes + 15) / 16 * 16; bytes[1] = (lead[1] + row_bytes + 15) / 16 * 16;
+        }
+        tc5::mbar_expect_tx(bar + 8 * s, bytes[0] + bytes[1]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            tc5::bulk_load(ring + (2 * s + i) * slot_bytes, reinterpret_cast<const uint8_t*>(from[i]) - lead[i], bytes[i], bar + 8 * s);
     };
     if (RING && t == 0) {
         for (int s = 0; s < p.stages; ++s) tc5::mbar_init(bar + 8 * s, 1);
@@ -163,7 +329,7 @@ k_norm_bwd(const NormParams p) {
     // (V 8: the first and the second four of a thread's eight columns apart, so that neighbouring threads read neighbouring 16 bytes)
     for (int c = team * tpr + t; c < p.width; c += teams * tpr) {
         float a[1] = {1.f};
-        if (p.w) { norm_params<T, 1>(p.w, p.params_f32, g * p.param_stride, c, a); a[0] += p.weight_offset; }
+        if (p.w) { norm_params<T, 1, false>(p.w, p.params_f32, g * p.param_stride, c, a, false); a[0] += p.weight_offset; }
         s_a[V == 8 ? (c >> 2 & 1) * (p.width / 2) + (c >> 3) * 4 + (c & 3) : c] = a[0];
     }
     __syncthreads();
@@ -171,6 +337,9 @@ k_norm_bwd(const NormParams p) {
         if constexpr (V == 8) {
             const float4 lo = *reinterpret_cast<const float4*>(s_a + col / 2), hi = *reinterpret_cast<const float4*>(s_a + p.width / 2 + col / 2);
             a[0] = lo.x; a[1] = lo.y; a[2] = lo.z; a[3] = lo.w; a[4] = hi.x; a[5] = hi.y; a[6] = hi.z; a[7] = hi.w;
+        } else if constexpr (V == 2) {
+            const float2 v = *reinterpret_cast<const float2*>(s_a + col);           // (one float of padding)
+            a[0] = v.x; a[1] = v.y;
         } else
             to_floats(load_vec<float, V>(s_a + col), a);
     };
@@ -190,11 +359,12 @@ k_norm_bwd(const NormParams p) {
         const bool on = row < g1;
         const float rstd = rstd_next, neg = -mean_next * rstd;          // xhat = x rstd + neg
         if (row + step < g1) { mean_next = p.mean[row + step]; rstd_next = p.rstd[row + step]; }
-        const T* x = static_cast<const T*>(p.x) + row * p.x_stride;
-        const T* dy = static_cast<const T*>(p.dy) + row * p.y_stride;
+        const T* gx = static_cast<const T*>(p.x) + row * p.x_stride;
+        const T* gd = static_cast<const T*>(p.dy) + row * p.y_stride;
+        const uint8_t* slot_x = s_ring + 2 * stage * slot_bytes;
+        const Row<T, V, WIDE> x = RING ? Row<T, V, WIDE>(slot_x, WIDE ? 0 : (uint32_t)(reinterpret_cast<uintptr_t>(gx) & 15)) : Row<T, V, WIDE>(gx);
+        const Row<T, V, WIDE> dy = RING ? Row<T, V, WIDE>(slot_x + slot_bytes, WIDE ? 0 : (uint32_t)(reinterpret_cast<uintptr_t>(gd) & 15)) : Row<T, V, WIDE>(gd);
         if constexpr (RING) {
-            x = reinterpret_cast<const T*>(s_ring + 2 * stage * row_bytes);
-            dy = reinterpret_cast<const T*>(s_ring + (2 * stage + 1) * row_bytes);
             // bounded like every wait: a row that never came would leave garbage, and the flag
             if (on && !tc5::mbar_try_wait(bar + 8 * stage, phase)) {
                 const long long t0 = clock64();
@@ -211,12 +381,15 @@ k_norm_bwd(const NormParams p) {
         if (on) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int col = (i * tpr + t) * V;
-                if (col >= p.width) continue;
+                int col = (i * tpr + t) * V;
+                if constexpr (WIDE) { if (col >= p.width) continue; }
                 float xf[V], d[V], gh[V], a[V];
-                to_floats(load_vec<T, V>(x + col), xf);
-                to_floats(load_vec<T, V>(dy + col), d);
+                const bool in = col < p.width, two = col + 1 < p.width;
+                if constexpr (!WIDE) col = in ? col : 0;        // (many short steps: no branch among them, so that their loads overlap)
+                x.get(col, xf, two);
+                dy.get(col, d, two);
                 load_factors(col, a);
+                if constexpr (!WIDE) { if (!in) d[0] = 0.f; }
                 vfma(xf, xf, rstd, neg);
                 vmul(gh, d, a);
                 vfma(accw[i], d, xf, accw[i]);
@@ -245,19 +418,19 @@ k_norm_bwd(const NormParams p) {
         T* dx = static_cast<T*>(p.y) + row * p.dx_stride;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int col = (i * tpr + t) * V;
-            if (col >= p.width) continue;
+            int col = (i * tpr + t) * V;
+            if constexpr (WIDE) { if (col >= p.width) continue; }
             float xf[V], d[V], a[V];
-            to_floats(load_vec<T, V>(x + col), xf);
-            to_floats(load_vec<T, V>(dy + col), d);
+            const bool in = col < p.width, two = col + 1 < p.width;
+            if constexpr (!WIDE) col = in ? col : 0;
+            x.get(col, xf, two);
+            dy.get(col, d, two);
             load_factors(col, a);
             vfma(xf, xf, rstd, neg);
             vmul(d, d, a);
             vfma(xf, xf, c2, c1);
             vfma(xf, d, rstd, xf);
-            Vec<T, V> o;
-            from_floats(o, xf);
-            store_vec(dx + col, o);
+            if (in) put_floats<T, V, WIDE>(dx + col, xf, two);
         }
     }
     if (p.dw == nullptr && p.db == nullptr) return;

@@ -96,6 +96,47 @@ __device__ __forceinline__ void from_floats(Vec<T, V, WIDE>& x, const float (&f)
 template <typename T, int V, bool WIDE>
 __device__ __forceinline__ void set_zero(Vec<T, V, WIDE>& x) { memset(&x, 0, sizeof(x)); }
 
+// A row of elements at p, aligned to an element: V of them from column col (a multiple of V) on.  WIDE: one access.  V 2, 16-bit elements:
+// pairs out of the 4-byte words that hold them: whether the row starts in the middle of a word is looked at once, for the row.
+// `two`: whether a pair has a second element; nothing is read beyond the words of the row's own elements.
+template <typename T, int V, bool WIDE>
+struct Row {
+    const T* p;
+    uint32_t shift;
+    __device__ __forceinline__ explicit Row(const T* at) : p(at), shift(0) {
+        if constexpr (!WIDE && V == 2) {
+            shift = (uint32_t)(reinterpret_cast<uintptr_t>(at) & 2) * 8;
+            p = at - (shift ? 1 : 0);
+        }
+    }
+    // The same with the start given: `base` aligned to a word, `lead` bytes in front of the row (a shared-memory address stays one).
+    __device__ __forceinline__ Row(const uint8_t* base, uint32_t lead) : p(reinterpret_cast<const T*>(base + (lead & ~3u))), shift((lead & 2) * 8) {
+        if constexpr (WIDE || V != 2) p = reinterpret_cast<const T*>(base + lead);
+    }
+    __device__ __forceinline__ void get(int col, float (&f)[V], bool two) const {
+        if constexpr (WIDE) to_floats(load_vec<T, V>(p + col), f);
+        else if constexpr (V == 1) f[0] = to_float(p[col]);
+        else {
+            static_assert(V != 2 || sizeof(T) == 2, "pairs of 16-bit elements");
+            const uint32_t* w = reinterpret_cast<const uint32_t*>(p + col);
+            uint32_t v = w[0];
+            if (shift) v = __funnelshift_r(v, two ? w[1] : 0u, 16);
+            const float2 r = unpack2<T>(v);
+            f[0] = r.x; f[1] = two ? r.y : 0.f;
+        }
+    }
+};
+template <typename T, int V, bool WIDE>
+__device__ __forceinline__ void put_floats(T* p, const float (&f)[V], bool two) {
+    if constexpr (WIDE) { Vec<T, V> o; from_floats(o, f); store_vec(p, o); }
+    else if constexpr (V == 1) p[0] = from_float<T>(f[0]);
+    else if (two && (reinterpret_cast<uintptr_t>(p) & 2) == 0) *reinterpret_cast<uint32_t*>(p) = pack2<T>(f[0], f[1]);
+    else {
+        p[0] = from_float<T>(f[0]);
+        if (two) p[1] = from_float<T>(f[1]);
+    }
+}
+
 // Packed elements that the compiler may not keep unpacked beside them: what is computed from v behind this is computed anew, which costs an
 // instruction or two an element and saves the registers.
 template <typename T, int V>

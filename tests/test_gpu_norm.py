@@ -7,6 +7,16 @@ import torch
 from tests import layer_forms as lf
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def no_wait_ran_out():
+    """A bounded wait that runs out may leave right numbers behind: the status word tells."""
+    yield
+    from paper_2604_10103_b200 import binding as hf
+    assert hf.hf_layers_status() == (0, 0)
+
+
 BF, HALF, F32 = torch.bfloat16, torch.float16, torch.float32
 
 
@@ -99,6 +109,31 @@ def test_strided_rows_slices_of_a_modulation_tensor_and_parameter_types(param):
     y1 = layers.layer_norm(off, w, b, weight_offset=1.0, rows_per_group=group)
     bound = lf.norm(x, w, b, 1e-6, 1.0, group)
     lf.close(y1[0], bound[0], forward_bound(x, bound[0], bound[3], bound[4], 2.0, bound[2], BF), "y of unaligned rows")
+
+
+@pytest.mark.parametrize("dtype", [BF, HALF, F32])
+@pytest.mark.parametrize("width", [6, 31, 96, 641, 1454, 2167])
+def test_rows_that_start_anywhere(width, dtype):
+    """Every offset of x's, dy's and the parameters' first element within 16 bytes, and row strides that are no multiple of it."""
+    from paper_2604_10103_b200 import layers
+    rows = 29
+    x, w, b, dy = make(rows, width, dtype)
+
+    def moved(t, off, pad):
+        m = torch.full((t.shape[0] * (width + pad) + off + 1,), float("nan"), dtype=t.dtype, device="cuda")
+        v = m[off:off + t.shape[0] * (width + pad)].view(t.shape[0], width + pad)[:, :width]
+        v.copy_(t)
+        return v
+    ry, rmean, rrstd, xhat, a = lf.norm(x, w, b, 1e-6, 0.0, 0)
+    bound = forward_bound(x, ry, xhat, a, lf.f64(b).abs().max(), rrstd, dtype)
+    for off, pad in ((0, 1), (1, 0), (2, 2), (3, 5), (4, 4), (5, 3), (6, 0), (7, 7)):
+        xm, dm, wm, bm = moved(x, off, pad), moved(dy, (3 * off + 1) % 8, pad + 1), moved(w, (off + 2) % 8, 0), moved(b, (off + 2) % 8, 0)
+        y, mean, rstd = layers.layer_norm(xm, wm, bm)
+        lf.close(y, ry, bound, f"y at {off}, {pad}")
+        dx, dw, db = layers.layer_norm_backward(dm, xm, mean, rstd, wm)
+        rdx, rdw, rdb, adw, adb = lf.norm_backward(dy, x, mean, rstd, w, 0.0, 0)
+        lf.close(db, rdb, (rows + 8) * 2.0 ** -24 * adb, f"db at {off}, {pad}")
+        assert lf.rel(dw, rdw) < 1e-5 and lf.rel(dx, rdx) < lf.U[dtype] + 1e-5
 
 
 def test_without_parameters_and_in_leading_axes():

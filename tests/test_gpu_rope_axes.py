@@ -6,6 +6,16 @@ import torch
 from tests import layer_forms as lf
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def no_wait_ran_out():
+    """A bounded wait that runs out may leave right numbers behind: the status word tells."""
+    yield
+    from paper_2604_10103_b200 import binding as hf
+    assert hf.hf_layers_status() == (0, 0)
+
+
 BF, HALF, F32 = torch.bfloat16, torch.float16, torch.float32
 
 
