@@ -11,6 +11,13 @@
 // accumulator and half of B, which the tensor cores of both read, so a tile costs a third less operand traffic; the first of the pair
 // issues the MMAs of both.  Every wait is bounded (~1 s) and reports through the status word; the two cluster barriers are reached by every
 // thread whatever became of its waits: one before the roles part, one behind all of them.
+// What bounds it: the MMAs, shared memory's bandwidth and the power limit, all near their ends at once.  Tiles of 256 x 256 a pair take 512
+// cycles of MMAs for each 64 of the contraction, in which 32 KB are written into and 32 KB read out of each thread block's shared memory:
+// its 128 bytes a cycle.  So tiles of one thread block (96 KB in the same cycles) are slower the longer they run, what an epilogue moves
+// through shared memory stops the MMAs, and dW, whose contraction is long, has tiles of 256 x 512 (a quarter less).  us (TFLOP/s) alone: 4680
+// rows, width 1536, hidden 4096: g, u, h 80 (1470), y 50 (1180: 114 tiles of 256 x 256, 133 of 224, on 74 pairs), dh and its epilogue 73
+// (810: 304 tiles, four rounds and eight tiles; see FF_DHIDDEN below), dx 96 (1230), dW 118 (1500); 32760 rows: dh 410 (1005), dx 560 (1470), dW 751
+// (1650).  In a loop the power limit takes a tenth off.
 #pragma once
 #include <cooperative_groups.h>
 #include "tc5_common.cuh"
@@ -358,7 +365,10 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
         FfOut out = {staging, 0};
         int acc = 0;
         uint32_t acc_phase = 0;
-        // DHIDDEN: boxes of gate and up come in by TMA one step ahead of their use and leave as dg and du, in place, with h in a third box; two
+        // DHIDDEN moves five elements for each of dh (in: gate, up; out: dg, du, h).  us of 4680 rows under a profiler: this form 73; gate and up through
+        // registers 76.5; sixteen warps with boxes of 16 columns 74.5; straight between registers and global memory, 32 bytes a lane, 87; without
+        // an epilogue at all 50.
+        // Boxes of gate and up come in by TMA one step ahead of their use and leave as dg and du, in place, with h in a third box; two
         // sets of the three in turn.  in_*: the next step to ask for.
         const uint32_t in_bar = bar_in + warp * 16;
         int in_t = tile_first, in_c = half, in_set = 0, use_n = 0;
