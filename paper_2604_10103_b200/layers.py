@@ -21,9 +21,11 @@ _ACTS = {"silu": hf.HF_ACT_SILU, "gelu_tanh": hf.HF_ACT_GELU_TANH}
 _NORM = struct.Struct("@3i6q2f").pack                       # hf_norm_shape
 _ROPE = struct.Struct("@5i4i4i2iq").pack                    # hf_rope_shape
 _ROPE_TENSOR = struct.Struct("@2P6q2i").pack                # hf_rope_tensor
+_ROPE_TENSORS = struct.Struct("@2P6q2i2P6q2i2P6q2i").pack   # three of them
 _FF = struct.Struct("@2iq3i2q").pack                        # hf_ff_shape
-_F32 = torch.float32
+_F32, _I32 = torch.float32, torch.int32
 _empty_like = torch.empty_like
+_lib, _stream, _check = hf.lib, hf._stream, hf._check
 
 
 try:
@@ -85,22 +87,32 @@ def _rows(name, t):
 
 
 # ------------------------------------------------------------------------------------------------ layer norm
-def _norm_params(weight, bias, dev, dtype, width, groups):
-    """Type and row stride of weight and bias."""
-    ptype, pstride = dtype, width
-    for name, p in (("weight", weight), ("bias", bias)):
-        if p is None:
-            continue
+def _norm_param(name, p, dev, dtype, width, groups):
+    """Type and row stride of weight or bias."""
+    shape, kind = p.shape, p.dtype
+    if kind != dtype and kind != _F32:
+        _fail(f"{name} is {kind}: x's type or float32 is taken")
+    if p.get_device() != dev:
         _here(name, p, dev)
-        n, w, stride = _rows(name, p)
-        if w != width or n != groups:
-            _fail(f"{name} has shape {tuple(p.shape)}: {groups} rows of {width} are taken")
-        if p.dtype != dtype and p.dtype != _F32:
-            _fail(f"{name} is {p.dtype}: x's type or float32 is taken")
-        if p is bias and weight is not None and (p.dtype != ptype or stride != pstride):
-            _fail("weight and bias differ in their type or their stride")
-        ptype, pstride = p.dtype, stride
-    return _TYPES[ptype], pstride
+    if shape != (groups, width) and not (groups == 1 and shape == (width,)):
+        _fail(f"{name} has shape {tuple(shape)}: {groups} rows of {width} are taken")
+    strides = p.stride()
+    if strides[-1] != 1 and width > 1:
+        _fail(f"{name}: the last axis has to be contiguous")
+    return kind, strides[0] if groups > 1 else width
+
+
+def _norm_params(weight, bias, dev, dtype, width, groups):
+    """Type and row stride of weight and bias together."""
+    if weight is None and bias is None:
+        return _TYPES[dtype], width
+    if weight is None:
+        kind, stride = _norm_param("bias", bias, dev, dtype, width, groups)
+        return _TYPES[kind], stride
+    kind, stride = _norm_param("weight", weight, dev, dtype, width, groups)
+    if bias is not None and _norm_param("bias", bias, dev, dtype, width, groups) != (kind, stride):
+        _fail("weight and bias differ in their type or their stride")
+    return _TYPES[kind], stride
 
 
 def _norm_type(x, width):
@@ -122,7 +134,11 @@ def layer_norm(x, weight=None, bias=None, eps=1e-6, weight_offset=0.0, rows_per_
     y = _empty_like(x) if stride == width else x.new_empty(x.shape)
     mean = x.new_empty(rows, dtype=_F32)
     rstd = _empty_like(mean)
-    hf.hf_layer_norm(_NORM(t, pt, width, rows, stride, width, width, rows_per_group, ps, weight_offset, eps), x, weight, bias, y, mean, rstd)
+    status = _lib().hf_layer_norm(_NORM(t, pt, width, rows, stride, width, width, rows_per_group, ps, weight_offset, eps), x.data_ptr(),
+                                  weight.data_ptr() if weight is not None else None, bias.data_ptr() if bias is not None else None,
+                                  y.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _stream())
+    if status:
+        _check(status)
     return y, mean, rstd
 
 
@@ -146,7 +162,11 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, weight_offset=0.0, rows_
     db = _empty_like(dw)
     shape = _NORM(t, pt, width, rows, stride, _rows("dy", dy)[2], width, rows_per_group, ps, weight_offset, 0.0)
     ws = mean.new_empty(_norm_workspace(dev, shape) // 4)
-    hf.hf_layer_norm_backward(shape, dy, x, mean, rstd, weight, dx, dw, db, ws)
+    status = _lib().hf_layer_norm_backward(shape, dy.data_ptr(), x.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+                                           weight.data_ptr() if weight is not None else None, dx.data_ptr(), dw.data_ptr(), db.data_ptr(),
+                                           ws.data_ptr(), _stream())
+    if status:
+        _check(status)
     return dx, dw, db
 
 
@@ -161,16 +181,24 @@ def _rope(x, B, T, d, tensors, n, pos, tables, pairing, inverse, dev):
         _fail(f"pairing {pairing!r} unknown")
     if x.dtype not in _TYPES:
         _fail(f"{x.dtype}: bfloat16, float16 and float32 are taken")
-    entries = (sum(map(int.__mul__, extents, pairs)),)
-    _dense("cos", cos, dev, entries, _F32)
-    _dense("sin", sin, dev, entries, _F32)
+    n_entries = 0
+    for e, p in zip(extents, pairs):
+        n_entries += e * p
+    if not (cos.dtype is _F32 and sin.dtype is _F32 and cos.get_device() == dev == sin.get_device() and cos.is_contiguous()
+            and sin.is_contiguous() and cos.shape == (n_entries,) == sin.shape):
+        _dense("cos", cos, dev, (n_entries,), _F32)
+        _dense("sin", sin, dev, (n_entries,), _F32)
     shape = pos.shape
     if shape != (T, axes) and shape != (1, T, axes) and shape != (B, T, axes):
         _fail(f"pos has shape {tuple(shape)}: [{T}, {axes}] or [{B}, {T}, {axes}] is taken")
-    _dense("pos", pos, dev, shape, torch.int32)
+    if pos.dtype is not _I32 or pos.get_device() != dev or not pos.is_contiguous():
+        _dense("pos", pos, dev, shape, _I32)
     rest = (0,) * (4 - axes)
-    hf.hf_rope_axes(_ROPE(_TYPES[x.dtype], B, T, d, axes, *pairs, *rest, *extents, *rest, _PAIRINGS[pairing], inverse,
-                          T * axes if B > 1 and len(shape) == 3 and shape[0] == B else 0), tensors, n, cos, sin, pos)
+    status = _lib().hf_rope_axes(_ROPE(_TYPES[x.dtype], B, T, d, axes, *pairs, *rest, *extents, *rest, _PAIRINGS[pairing], inverse,
+                                       T * axes if B > 1 and len(shape) == 3 and shape[0] == B else 0), tensors, n, cos.data_ptr(), sin.data_ptr(),
+                                 pos.data_ptr(), _stream())
+    if status:
+        _check(status)
 
 
 def rope_axes(x, pos, tables, out=None, pairing="adjacent", inverse=False):
@@ -210,9 +238,11 @@ def split_heads_rope(qkv, heads, kv_heads, pos, tables, pairing="adjacent"):
     k = qkv.new_empty(B, kv_heads, T, d)
     v = _empty_like(k)
     x, td, e = qkv.data_ptr(), T * d, qkv.element_size()
-    _rope(qkv, B, T, d, _ROPE_TENSOR(x, q.data_ptr(), xb, xt, d, heads * td, d, td, heads, 1)
-          + _ROPE_TENSOR(x + heads * d * e, k.data_ptr(), xb, xt, d, kv_heads * td, d, td, kv_heads, 1)
-          + _ROPE_TENSOR(x + (heads + kv_heads) * d * e, v.data_ptr(), xb, xt, d, kv_heads * td, d, td, kv_heads, 0), 3, pos, tables, pairing, 0, dev)
+    de, kv_batch = d * e, kv_heads * td
+    _rope(qkv, B, T, d, _ROPE_TENSORS(x, q.data_ptr(), xb, xt, d, heads * td, d, td, heads, 1,
+                                      x + heads * de, k.data_ptr(), xb, xt, d, kv_batch, d, td, kv_heads, 1,
+                                      x + (heads + kv_heads) * de, v.data_ptr(), xb, xt, d, kv_batch, d, td, kv_heads, 0),
+          3, pos, tables, pairing, 0, dev)
     return q, k, v
 
 
@@ -250,9 +280,12 @@ def _ff_operands(x, w_gate, w_up, w_down, act):
     dtype, hidden, out_width = x.dtype, w_gate.shape[0], w_down.shape[0]
     if dtype not in _TYPES:
         _fail(f"x is {dtype}: bfloat16 and float16 are taken")
-    _dense("w_gate", w_gate, dev, (hidden, width), dtype)
-    _dense("w_up", w_up, dev, (hidden, width), dtype)
-    _dense("w_down", w_down, dev, (out_width, hidden), dtype)
+    if not (w_gate.dtype is dtype and w_up.dtype is dtype and w_down.dtype is dtype and w_gate.shape == (hidden, width) == w_up.shape
+            and w_down.shape == (out_width, hidden) and w_gate.get_device() == dev == w_up.get_device() and w_down.get_device() == dev
+            and w_gate.is_contiguous() and w_up.is_contiguous() and w_down.is_contiguous()):
+        _dense("w_gate", w_gate, dev, (hidden, width), dtype)
+        _dense("w_up", w_up, dev, (hidden, width), dtype)
+        _dense("w_down", w_down, dev, (out_width, hidden), dtype)
     return dev, _TYPES[dtype], rows, width, hidden, out_width, stride
 
 
@@ -271,7 +304,10 @@ def gated_ff(x, w_gate, w_up, w_down, act="silu", save=False):
     up = _empty_like(gate) if save else None
     shape = _FF(t, _ACTS[act], rows, width, hidden, out_width, stride, out_width)
     ws = x.new_empty(_ff_workspace(dev, shape, 0) // 2)
-    hf.hf_gated_ff(shape, x, w_gate, w_up, w_down, y, gate, up, ws)
+    status = _lib().hf_gated_ff(shape, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), y.data_ptr(),
+                                gate.data_ptr() if save else None, up.data_ptr() if save else None, ws.data_ptr(), _stream())
+    if status:
+        _check(status)
     return (y, gate, up) if save else y
 
 
@@ -285,5 +321,9 @@ def gated_ff_backward(dy, x, w_gate, w_up, w_down, gate, up, act="silu"):
     dwg, dwu, dwd = _empty_like(w_gate), _empty_like(w_up), _empty_like(w_down)
     shape = _FF(t, _ACTS[act], rows, width, hidden, out_width, stride, _rows("dy", dy)[2])
     ws = x.new_empty(_ff_workspace(dev, shape, 1) // 2)
-    hf.hf_gated_ff_backward(shape, dy, x, w_gate, w_up, w_down, gate, up, dx, dwg, dwu, dwd, ws)
+    status = _lib().hf_gated_ff_backward(shape, dy.data_ptr(), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(),
+                                         gate.data_ptr(), up.data_ptr(), dx.data_ptr(), dwg.data_ptr(), dwu.data_ptr(), dwd.data_ptr(),
+                                         ws.data_ptr(), _stream())
+    if status:
+        _check(status)
     return dx, dwg, dwu, dwd
