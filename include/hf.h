@@ -338,7 +338,7 @@ typedef struct {
 } hf_norm_shape;
 
 /* weight, bias, mean, rstd may be NULL (no factor, no shift; not written).  mean, rstd float [rows].  y may be x.  Pointers are aligned to
- * their element; rows whose starts are all 16-byte aligned and whose width is a multiple of 16 bytes are read and written in 16-byte pieces. */
+ * their element, and rows may start anywhere; rows that all start on 16 bytes, with a width of a multiple of 16 bytes, are the fastest. */
 hf_status hf_layer_norm(const hf_norm_shape* shape, const void* x, const void* weight, const void* bias, void* y, float* mean,
                         float* rstd, void* stream);
 

@@ -202,9 +202,12 @@ hf_status launch_rows(const hf_ff_shape* g, const FfRowsParams& first, const FfR
 
 }  // namespace
 
-namespace hf_layers {
-// Pairs of multiprocessors that can hold a cluster of two thread blocks at a time (a persistent grid of more would run in two rounds).
-hf_status count_pairs(int* pairs) {
+namespace {
+// The current device, with the pairs of multiprocessors that can hold a cluster of two thread blocks at a time (a persistent grid of more
+// would run in two rounds): asked on the first call of this module, which is loaded by it.
+hf_status ff_device(const Device** out) {
+    HFL_TRY(current_device(out));
+    if ((*out)->pairs) return HF_OK;
     typedef FfGemm<FF_STORE, 2> C;
     auto kernel = k_ff_gemm<bf16, FF_STORE, false, false, 2>;
     HFL_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_MAX));
@@ -213,11 +216,13 @@ hf_status count_pairs(int* pairs) {
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = 2; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
     cfg.gridDim = dim3(256); cfg.blockDim = dim3(C::THREADS); cfg.dynamicSmemBytes = C::SMEM_MAX; cfg.attrs = &attr; cfg.numAttrs = 1;
-    HFL_CUDA(cudaOccupancyMaxActiveClusters(pairs, kernel, &cfg));
-    if (*pairs < 1) return fail(HF_ERR_UNSUPPORTED, "the device holds no cluster of two thread blocks");
+    int pairs = 0;
+    HFL_CUDA(cudaOccupancyMaxActiveClusters(&pairs, kernel, &cfg));
+    if (pairs < 1) return fail(HF_ERR_UNSUPPORTED, "the device holds no cluster of two thread blocks");
+    (*out)->pairs = pairs;
     return HF_OK;
 }
-}  // namespace hf_layers
+}  // namespace
 
 extern "C" {
 
@@ -225,7 +230,7 @@ hf_status hf_gated_ff_workspace(const hf_ff_shape* g, int backward, size_t* byte
     HFL_TRY(ff_check(g));
     if (!bytes) return fail(HF_ERR_INVALID_ARG, "bytes is null");
     const Device* d;
-    HFL_TRY(current_device(&d));
+    HFL_TRY(ff_device(&d));
     const size_t h = round_up((size_t)g->rows * g->hidden * 2);
     if (backward) {             // dg, du, h; the parts' sums of dx, then of dW
         const size_t x = ff_partial_bytes(cut_dx(d, g), dx_sizes(g).data, 1), w = ff_partial_bytes(cut_dw(d, g), dw_sizes(g).data, 3);
@@ -244,7 +249,7 @@ hf_status hf_gated_ff(const hf_ff_shape* g, const void* x, const void* w_gate, c
     if ((gate == nullptr) != (up == nullptr)) return fail(HF_ERR_INVALID_ARG, "gate and up are saved together or not at all");
     if (gate) { HFL_TRY(ff_pointer(gate, "gate")); HFL_TRY(ff_pointer(up, "up")); }
     const Device* d;
-    HFL_TRY(current_device(&d));
+    HFL_TRY(ff_device(&d));
     const cudaStream_t st = (cudaStream_t)stream;
     const long long M = g->rows, K = g->width, N = g->hidden, O = g->out_width;
     if (M <= FF_ROWS_MOST) {
@@ -300,7 +305,7 @@ hf_status hf_gated_ff_backward(const hf_ff_shape* g, const void* dy, const void*
     HFL_TRY(ff_pointer(w_down, "w_down")); HFL_TRY(ff_pointer(gate, "gate")); HFL_TRY(ff_pointer(up, "up")); HFL_TRY(ff_pointer(workspace, "workspace"));
     if (dx) HFL_TRY(ff_pointer(dx, "dx"));
     const Device* d;
-    HFL_TRY(current_device(&d));
+    HFL_TRY(ff_device(&d));
     const size_t part = round_up((size_t)M * N * 2);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     const Matrix mdy = {dy, M, O, g->y_stride}, mx = {x, M, K, g->x_stride}, dg = {ws, M, N, N}, du = {ws + part, M, N, N}, h = {ws + 2 * part, M, N, N};

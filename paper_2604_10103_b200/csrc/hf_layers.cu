@@ -38,7 +38,7 @@ hf_status current_device(const Device** out) {
     if (!g_known[dev]) {
         std::lock_guard<std::mutex> lock(g_mutex);
         if (!g_known[dev]) {
-            Device d = {dev, 0, 0, nullptr, nullptr};
+            Device d = {dev, 0, nullptr, nullptr, 0};
             int major = 0;
             HFL_CUDA(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev));
             if (major != 10) return fail(HF_ERR_UNSUPPORTED, "device of compute capability %d.x; this library is built for sm_100a only", major);
@@ -50,8 +50,8 @@ hf_status current_device(const Device** out) {
             e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &d.encode_tiled, cudaEnableDefault, &q);
             if (e != cudaSuccess || q != cudaDriverEntryPointSuccess || d.encode_tiled == nullptr)
                 return fail(HF_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
-            HFL_TRY(count_pairs(&d.pairs));
-            g_devices[dev] = d;
+            g_devices[dev].index = d.index; g_devices[dev].sm_count = d.sm_count;
+            g_devices[dev].status = d.status; g_devices[dev].encode_tiled = d.encode_tiled;
             g_known[dev] = true;
         }
     }
@@ -288,7 +288,8 @@ hf_status hf_layer_norm(const hf_norm_shape* g, const void* x, const void* weigh
     HFL_TRY(current_device(&d));
     NormParams p = {};
     p.x = x; p.y = y; p.w = weight; p.b = bias; p.mean = mean; p.rstd = rstd;
-    p.rows = g->rows; p.x_stride = g->x_stride; p.y_stride = g->y_stride; p.rows_per_group = g->rows_per_group; p.param_stride = g->param_stride;
+    p.rows = g->rows; p.x_stride = g->x_stride; p.y_stride = g->y_stride; p.param_stride = g->param_stride;
+    p.rows_per_group = g->rows_per_group < g->rows ? g->rows_per_group : g->rows;
     p.width = g->width; p.params_f32 = g->param_type == HF_F32; p.weight_offset = g->weight_offset; p.eps = g->eps;
     const void* rows[2] = {x, y};
     const long long strides[2] = {g->x_stride, g->y_stride};

@@ -9,14 +9,15 @@ namespace hf_layers {
 
 // What is known of a device after its first call.
 struct Device {
-    int index, sm_count, pairs;     // pairs: clusters of two thread blocks with a multiprocessor each that run at a time
+    int index, sm_count;
     int* status;            // device status word of the calls without a context, as a context's: [0] flags, [1] detail
     void* encode_tiled;     // cuTensorMapEncodeTiled
+    mutable volatile int pairs;     // clusters of two thread blocks with a multiprocessor each that run at a time (0: not asked yet)
 };
 
 hf_status fail(hf_status s, const char* fmt, ...);
 hf_status current_device(const Device** out);
-hf_status count_pairs(int* pairs);
+
 inline int element_bytes(int type) { return type == HF_F32 ? 4 : 2; }
 inline bool aligned(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 

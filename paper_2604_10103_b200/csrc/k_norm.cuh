@@ -74,6 +74,8 @@ k_norm(const NormParams p) {
     const int t = TPR == 32 ? threadIdx.x & 31 : threadIdx.x;
     const long long row = TPR == 32 ? (long long)blockIdx.x * 8 + (threadIdx.x >> 5) : blockIdx.x;
     if (row >= p.rows) return;                  // (a whole warp; with TPR > 32 the grid is the rows)
+    // (rows and rows_per_group fit 31 bits; a division of 64 costs a microsecond here)
+    const long long at = p.rows_per_group ? (uint32_t)row / (uint32_t)p.rows_per_group * p.param_stride : 0;
     Vec<T, V> xv[NV];
     const Row<T, V, WIDE> x(static_cast<const T*>(p.x) + row * p.x_stride);
 #pragma unroll
@@ -121,7 +123,6 @@ k_norm(const NormParams p) {
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) stay_packed(xv[i]);
-    const long long at = p.rows_per_group ? row / p.rows_per_group * p.param_stride : 0;
     T* y = static_cast<T*>(p.y) + row * p.y_stride;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {

@@ -93,8 +93,6 @@ __device__ __forceinline__ void from_floats(Vec<T, V, WIDE>& x, const float (&f)
         for (int i = 0; i < V; ++i) x.v[i] = from_float<T>(f[i]);
     }
 }
-template <typename T, int V, bool WIDE>
-__device__ __forceinline__ void set_zero(Vec<T, V, WIDE>& x) { memset(&x, 0, sizeof(x)); }
 
 // A row of elements at p, aligned to an element: V of them from column col (a multiple of V) on.  WIDE: one access.  V 2, 16-bit elements:
 // pairs out of the 4-byte words that hold them: whether the row starts in the middle of a word is looked at once, for the row.

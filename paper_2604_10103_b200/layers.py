@@ -24,7 +24,7 @@ _ROPE_TENSOR = struct.Struct("@2P6q2i").pack                # hf_rope_tensor
 _ROPE_TENSORS = struct.Struct("@2P6q2i2P6q2i2P6q2i").pack   # three of them
 _FF = struct.Struct("@2iq3i2q").pack                        # hf_ff_shape
 _F32, _I32 = torch.float32, torch.int32
-_empty_like = torch.empty_like
+_empty_like, _empty_strided = torch.empty_like, torch.empty_strided
 _lib, _stream, _check = hf.lib, hf._stream, hf._check
 
 
@@ -132,7 +132,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-6, weight_offset=0.0, rows_per_
     t = _norm_type(x, width)
     pt, ps = _norm_params(weight, bias, dev, x.dtype, width, -(-rows // rows_per_group) if rows_per_group > 0 else 1)
     y = _empty_like(x) if stride == width else x.new_empty(x.shape)
-    mean = x.new_empty(rows, dtype=_F32)
+    mean = _empty_strided((rows,), (1,), dtype=_F32, device=x.device)
     rstd = _empty_like(mean)
     status = _lib().hf_layer_norm(_NORM(t, pt, width, rows, stride, width, width, rows_per_group, ps, weight_offset, eps), x.data_ptr(),
                                   weight.data_ptr() if weight is not None else None, bias.data_ptr() if bias is not None else None,
