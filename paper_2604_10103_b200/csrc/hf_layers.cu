@@ -105,8 +105,11 @@ NormPlan norm_bwd_plan(const hf_norm_shape* g, bool wide, int sms) {
     const int e = element_bytes(g->type), V = wide ? 16 / e : 4 / e;
     p.wide = wide;
     p.groups = norm_groups(g);
-    // (floats one by one want a few registers more: 32 columns a thread where twelve warps are enough then)
-    const int most_cols = V == 1 && g->width <= 12 * 32 * 32 ? 32 : 48, warps = (g->width + 32 * most_cols - 1) / (32 * most_cols);
+    const int factors = (g->width * 4 + 4 + 15) / 16 * 16, row = 2 * (wide ? g->width * e : (g->width * e + 30) / 16 * 16);
+    // (floats one by one want a few registers more: 32 columns a thread where twelve warps are enough then and two rows fit; rows too long
+    // for a ring, of over 11604 floats, or 11608 that start on 16 bytes, are read from global memory by one form, of 48)
+    const bool rings = factors + NORM_TEAM_BYTES + 2 * row <= NORM_SMEM;
+    const int most_cols = V == 1 && rings && g->width <= 12 * 32 * 32 ? 32 : 48, warps = (g->width + 32 * most_cols - 1) / (32 * most_cols);
     p.tpr = 32 * warps;
     p.nv = (g->width + V * p.tpr - 1) / (V * p.tpr);
     // (the instantiations)
@@ -119,12 +122,11 @@ NormPlan norm_bwd_plan(const hf_norm_shape* g, bool wide, int sms) {
     p.teams = norm_bwd_warps(V * p.nv) / warps;
     const long long most = (rows + 2 * n - 1) / (2 * n);
     if (p.teams > most) p.teams = most < 1 ? 1 : (int)most;
-    const int factors = (g->width * 4 + 4 + 15) / 16 * 16, row = 2 * (wide ? g->width * e : (g->width * e + 30) / 16 * 16);
     auto fit = [&] { return (NORM_SMEM - factors - p.teams * NORM_TEAM_BYTES) / (p.teams * row); };
     while (p.teams > 1 && fit() < 2) --p.teams;
     p.stages = fit();
     if (p.stages > 4) p.stages = 4;
-    if (p.stages < 2) p.stages = 0;             // (rows too long for rings)
+    if (!rings) p.stages = 0;
     p.smem = factors + p.teams * (NORM_TEAM_BYTES + p.stages * row);
     const int join = p.teams * 2 * V * p.nv * p.tpr * 4;
     if (join > p.smem) p.smem = join;
@@ -225,7 +227,7 @@ hf_status launch_norm_bwd(const Device* d, const NormParams& p, const NormPlan& 
 }
 template <typename T>
 hf_status launch_norm_bwd_of(const Device* d, const NormParams& p, const NormPlan& n, cudaStream_t st) {
-    if constexpr (sizeof(T) == 4)           // (rows of over 14300 floats are too long for a ring of two)
+    if constexpr (sizeof(T) == 4)
         if (!n.stages) return n.wide ? launch_norm_bwd<T, 4, 12, false>(d, p, n, st) : launch_norm_bwd<T, 1, 48, false, false>(d, p, n, st);
     if (!n.wide) {
         constexpr int P = 4 / sizeof(T);
