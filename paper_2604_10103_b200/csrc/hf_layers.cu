@@ -312,6 +312,8 @@ hf_status hf_layer_norm(const hf_norm_shape* g, const void* x, const void* weigh
 hf_status hf_layer_norm_workspace(const hf_norm_shape* g, size_t* bytes) {
     HFL_TRY(norm_check(g));
     if (!bytes) return fail(HF_ERR_INVALID_ARG, "bytes is null");
+    *bytes = 0;
+    if (g->rows == 0) return HF_OK;             // (and there may be no groups to share the multiprocessors among)
     const Device* d;
     HFL_TRY(current_device(&d));
     // (the alignment of the tensors, which the shape does not say, changes the number of thread blocks)

@@ -80,3 +80,25 @@ def test_the_plan_is_that_of_the_kernel_launched(rules, type, wide):
             row = width * e if wide else (width * e + 30) // 16 * 16
             assert smem <= SMEM and smem >= (width * 4 + 4 + 15) // 16 * 16 + teams * (team_bytes + stages * 2 * row), at
             assert smem >= teams * 2 * V * NV * tpr * 4, at
+
+
+@pytest.mark.parametrize("per_group", [0, 1, 4])
+def test_no_rows_need_no_workspace(per_group):
+    """The empty batch of a modulated norm has no groups to share the multiprocessors among."""
+    from paper_2604_10103_b200 import binding as hf, build
+    build.build()
+    s = hf.hf_norm_shape(type=0, param_type=0, width=64, rows=0, x_stride=64, y_stride=64, dx_stride=64, rows_per_group=per_group, param_stride=64,
+                         weight_offset=1.0, eps=1e-6)
+    n = C.c_size_t(1)
+    assert hf.lib().hf_layer_norm_workspace(C.byref(s), C.byref(n)) == 0 and n.value == 0
+
+
+@pytest.mark.gpu
+def test_gradients_of_no_rows_in_groups():
+    import torch
+    from paper_2604_10103_b200 import layers
+    for dtype in (torch.bfloat16, torch.float32):
+        e, w = torch.empty(0, 64, device="cuda", dtype=dtype), torch.empty(0, 64, device="cuda", dtype=dtype)
+        y, mean, rstd = layers.layer_norm(e, w, w, weight_offset=1.0, rows_per_group=4)
+        dx, dw, db = layers.layer_norm_backward(e, e, mean, rstd, w, weight_offset=1.0, rows_per_group=4)
+        assert y.shape == dx.shape == (0, 64) and dw.shape == db.shape == (0, 64)
