@@ -84,7 +84,8 @@ hf_status norm_check(const hf_norm_shape* g) {
     return HF_OK;
 }
 int norm_groups(const hf_norm_shape* g) {
-    return g->rows_per_group ? (int)((g->rows + g->rows_per_group - 1) / g->rows_per_group) : 1;
+    if (g->rows_per_group == 0) return 1;
+    return g->rows == 0 ? 0 : (int)((g->rows - 1) / g->rows_per_group + 1);       // (rows_per_group may be any 64-bit number)
 }
 // Whether every row of a tensor and every group of the parameters starts on 16 bytes.
 bool norm_wide(const hf_norm_shape* g, const void* const* rows, const long long* strides, int n, const void* w, const void* b) {

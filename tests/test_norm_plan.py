@@ -102,3 +102,26 @@ def test_gradients_of_no_rows_in_groups():
         y, mean, rstd = layers.layer_norm(e, w, w, weight_offset=1.0, rows_per_group=4)
         dx, dw, db = layers.layer_norm_backward(e, e, mean, rstd, w, weight_offset=1.0, rows_per_group=4)
         assert y.shape == dx.shape == (0, 64) and dw.shape == db.shape == (0, 64)
+
+
+def test_groups_longer_than_any_number_of_rows(rules):
+    """One group, however many rows it might hold."""
+    for per_group in (1, 4, 2 ** 31, 2 ** 63 - 2, 2 ** 63 - 1):
+        for rows in (1, 2, 500, 2 ** 31 - 1):
+            if per_group == 1 and rows > 500:
+                continue
+            _, groups, _, _, teams, blocks, _, smem, *_ = rules(0, True, 64, rows, per_group)
+            assert groups == -(-rows // per_group) and teams >= 1 and blocks >= 1 and 0 < smem <= SMEM, (per_group, rows)
+
+
+@pytest.mark.gpu
+def test_one_group_of_any_number_of_rows():
+    import torch
+    from paper_2604_10103_b200 import layers
+    for rows, width in ((5, 64), (4000, 1455)):          # (a few rows, and many that walk through rings)
+        x, w, dy = (torch.randn(n, width, device="cuda").bfloat16() for n in (rows, 1, rows))
+        ref = layers.layer_norm(x, w, w)
+        refb = layers.layer_norm_backward(dy, x, ref[1], ref[2], w)
+        got = layers.layer_norm(x, w, w, rows_per_group=2 ** 63 - 1)
+        gotb = layers.layer_norm_backward(dy, x, ref[1], ref[2], w, rows_per_group=2 ** 63 - 1)
+        assert all(torch.equal(p, q) for p, q in zip(ref + refb, got + gotb))
