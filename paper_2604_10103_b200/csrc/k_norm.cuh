@@ -335,13 +335,14 @@ k_norm_bwd(const NormParams p) {
         if (p.w) { norm_params<T, 1, false>(p.w, p.params_f32, g * p.param_stride, c, a, false); a[0] += p.weight_offset; }
         s_a[V == 8 ? (c >> 2 & 1) * (p.width / 2) + (c >> 3) * 4 + (c & 3) : c] = a[0];
     }
+    if (V == 2 && t == 0 && team == 0) s_a[p.width] = 0.f;              // (the other half of an odd row's last pair: it meets a zero of dy)
     __syncthreads();
     auto load_factors = [&](int col, float (&a)[V]) {
         if constexpr (V == 8) {
             const float4 lo = *reinterpret_cast<const float4*>(s_a + col / 2), hi = *reinterpret_cast<const float4*>(s_a + p.width / 2 + col / 2);
             a[0] = lo.x; a[1] = lo.y; a[2] = lo.z; a[3] = lo.w; a[4] = hi.x; a[5] = hi.y; a[6] = hi.z; a[7] = hi.w;
         } else if constexpr (V == 2) {
-            const float2 v = *reinterpret_cast<const float2*>(s_a + col);           // (one float of padding)
+            const float2 v = *reinterpret_cast<const float2*>(s_a + col);
             a[0] = v.x; a[1] = v.y;
         } else
             to_floats(load_vec<float, V>(s_a + col), a);
