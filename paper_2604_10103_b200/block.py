@@ -83,6 +83,12 @@ class _Attention(torch.autograd.Function):
         return dq + dq_hist, dk, dv, None, None
 
 
+def _bf16(name, t):
+    """The attention takes bare pointers: a type that it would misread is refused here."""
+    if t.dtype is not torch.bfloat16:
+        raise ValueError(f"{name} is {t.dtype}: the hybrid attention takes bfloat16")
+
+
 class DenoiserBlock(torch.nn.Module):
     """One layer.  w: an `inputs.Workload` (batch, heads, head_dim, frames); high x wide tokens a frame; context: the `binding.Context`
     that holds the layer's cache and state."""
@@ -91,6 +97,8 @@ class DenoiserBlock(torch.nn.Module):
         super().__init__()
         if high * wide != w.tokens_per_frame:
             raise ValueError(f"{high} x {wide} tokens are not a frame of {w.tokens_per_frame}")
+        if dtype is not torch.bfloat16:
+            raise ValueError(f"the weights are {dtype}: the hybrid attention takes bfloat16")
         self.w, self.context, self.layer, self.act, self.eps = w, context, layer, act, eps
         width = w.heads * w.head_dim
         hidden = hidden or (8 * width // 3 + 63) // 64 * 64
@@ -115,8 +123,11 @@ class DenoiserBlock(torch.nn.Module):
     def _heads(self, x, shift, scale, pos, eps):
         B, T, width = x.shape
         frame = self.w.tokens_per_frame
+        _bf16("x", x)
         h = _Norm.apply(x, scale.reshape(-1, width), shift.reshape(-1, width), frame, eps)
-        return _HeadsRope.apply(torch.nn.functional.linear(h, self.w_qkv), self.w.heads, pos, (self.cos, self.sin, self.extents, self.pairs))
+        qkv = torch.nn.functional.linear(h, self.w_qkv)
+        _bf16("the projection", qkv)            # (autocast may have changed its type)
+        return _HeadsRope.apply(qkv, self.w.heads, pos, (self.cos, self.sin, self.extents, self.pairs))
 
     def forward(self, x, mod, pos):
         """x [batch, tokens of a chunk, width]; mod [batch, frames of the chunk, 6, width]: shift, scale, gate of the attention half, then of the
