@@ -166,7 +166,7 @@ class Context:
     """Owns one hf_ctx.  Methods mirror the C entry points one to one."""
 
     def __init__(self, cfg: hf_config, device: int = 0):
-        self.cfg = cfg
+        self.cfg, self.device = cfg, device
         self._h = C.c_void_p()
         _check(lib().hf_create(C.byref(cfg), device, C.byref(self._h)))
 

@@ -99,6 +99,9 @@ class DenoiserBlock(torch.nn.Module):
             raise ValueError(f"{high} x {wide} tokens are not a frame of {w.tokens_per_frame}")
         if dtype is not torch.bfloat16:
             raise ValueError(f"the weights are {dtype}: the hybrid attention takes bfloat16")
+        c = context.cfg
+        if (c.batch, c.heads, c.head_dim, c.tokens_per_frame * c.chunk_frames) != (w.batch, w.heads, w.head_dim, w.chunk_tokens):
+            raise ValueError("the context's batch, heads, head_dim or tokens of a chunk are not the workload's")
         self.w, self.context, self.layer, self.act, self.eps = w, context, layer, act, eps
         width = w.heads * w.head_dim
         hidden = hidden or (8 * width // 3 + 63) // 64 * 64
@@ -120,11 +123,15 @@ class DenoiserBlock(torch.nn.Module):
         pos[:, 0] += first_frame
         return pos
 
-    def _heads(self, x, shift, scale, pos, eps):
-        B, T, width = x.shape
-        frame = self.w.tokens_per_frame
+    def _heads(self, x, mod, pos):
+        taken = [self.w.batch, self.w.chunk_tokens, self.w.heads * self.w.head_dim]
+        if list(x.shape) != taken:              # (the attention reads and writes as much, whatever it is given)
+            raise ValueError(f"x is {list(x.shape)}: {taken} is taken")
         _bf16("x", x)
-        h = _Norm.apply(x, scale.reshape(-1, width), shift.reshape(-1, width), frame, eps)
+        if x.get_device() != self.context.device:
+            raise ValueError(f"x is on {x.device}, the context on device {self.context.device}")
+        width, frame = x.shape[-1], self.w.tokens_per_frame
+        h = _Norm.apply(x, mod[:, :, 1].reshape(-1, width), mod[:, :, 0].reshape(-1, width), frame, self.eps)
         qkv = torch.nn.functional.linear(h, self.w_qkv)
         _bf16("the projection", qkv)            # (autocast may have changed its type)
         return _HeadsRope.apply(qkv, self.w.heads, pos, (self.cos, self.sin, self.extents, self.pairs))
@@ -132,8 +139,8 @@ class DenoiserBlock(torch.nn.Module):
     def forward(self, x, mod, pos):
         """x [batch, tokens of a chunk, width]; mod [batch, frames of the chunk, 6, width]: shift, scale, gate of the attention half, then of the
         feed-forward's; pos: `positions` of the chunk's first frame."""
-        B, T, width = x.shape
-        q, k, v = self._heads(x, mod[:, :, 0], mod[:, :, 1], pos, self.eps)
+        q, k, v = self._heads(x, mod, pos)
+        width = x.shape[-1]
         if torch.is_grad_enabled() and q.requires_grad:
             o = _Attention.apply(q, k, v, self.context, self.layer)
         else:
@@ -151,7 +158,7 @@ class DenoiserBlock(torch.nn.Module):
     @torch.no_grad()
     def commit(self, x, mod, pos):
         """The finished chunk's keys and values go into the layer's cache (and the oldest chunk into its state)."""
-        _, k, v = self._heads(x, mod[:, :, 0], mod[:, :, 1], pos, self.eps)
+        _, k, v = self._heads(x, mod, pos)
         self.context.hf_kv_append(self.layer, k, v)
 
 

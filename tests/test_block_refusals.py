@@ -29,3 +29,31 @@ def test_types_that_the_attention_does_not_take(dtype):
     for call in (b.forward, b.commit):
         with pytest.raises(ValueError, match="bfloat16"):
             call(x, mod, b.positions(0))
+
+
+@pytest.mark.parametrize("kw", [dict(batch=1), dict(batch=3), dict(tokens=W.chunk_tokens - 32), dict(tokens=W.chunk_tokens + 32), dict(tokens=1), dict(width=64),
+                                dict(width=192)])
+def test_chunks_of_other_sizes_than_the_context(kw):
+    """The attention reads and writes batch x heads x tokens of its context, whatever lies behind the pointers."""
+    b = build()
+    x, mod = chunk(**{k: v for k, v in kw.items() if k != "tokens"}, tokens=kw.get("tokens", W.chunk_tokens))
+    for call in (b.forward, b.commit):
+        with pytest.raises(ValueError, match=r"x is \[.*\]: \[2, 64, 128\] is taken"):
+            call(x, mod, b.positions(0))
+    for bad in (x[0], x[None]):
+        with pytest.raises(ValueError, match="is taken"):
+            b(bad, mod, b.positions(0))
+
+
+@pytest.mark.parametrize("kw", [dict(batch=1), dict(heads=3), dict(heads=1, head_dim=128), dict(tokens_per_frame=2 * HIGH * WIDE), dict(chunk_frames=4)])
+def test_a_context_of_another_workload(kw):
+    context = types.SimpleNamespace(cfg=hf.make_config(W.with_(**kw)), device=0)
+    with pytest.raises(ValueError, match="context"):
+        bl.DenoiserBlock(W, HIGH, WIDE, context, device="cpu")
+
+
+def test_tensors_on_another_device_than_the_context():
+    b = build()
+    x, mod = chunk()
+    with pytest.raises(ValueError, match="x is on cpu"):
+        b(x, mod, b.positions(0))
