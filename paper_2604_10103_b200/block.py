@@ -91,7 +91,8 @@ def _bf16(name, t):
 
 class DenoiserBlock(torch.nn.Module):
     """One layer.  w: an `inputs.Workload` (batch, heads, head_dim, frames); high x wide tokens a frame; context: the `binding.Context`
-    that holds the layer's cache and state."""
+    that holds the layer's cache and state; last_frame: the last frame of the stream in the time table (8 bytes a frame and pair: a million
+    frames of a head of 128 take 176 MB; a longer stream starts anew at frame 0, after `hf_reset`)."""
 
     def __init__(self, w, high, wide, context, layer=0, hidden=None, act="silu", last_frame=255, eps=1e-6, device="cuda", dtype=torch.bfloat16):
         super().__init__()
@@ -119,6 +120,9 @@ class DenoiserBlock(torch.nn.Module):
         self.register_buffer("pos", torch.stack([g.reshape(-1) for g in grid], dim=1).to(torch.int32).to(device))
 
     def positions(self, first_frame):
+        """Positions of the chunk whose first frame is the stream's frame `first_frame` (from 0)."""
+        if not 0 <= first_frame <= self.extents[0] - self.w.chunk_frames:
+            raise ValueError(f"frames {first_frame} .. {first_frame + self.w.chunk_frames - 1} are not in the time table: last_frame is {self.extents[0] - 1}")
         pos = self.pos.clone()
         pos[:, 0] += first_frame
         return pos

@@ -57,3 +57,13 @@ def test_tensors_on_another_device_than_the_context():
     x, mod = chunk()
     with pytest.raises(ValueError, match="x is on cpu"):
         b(x, mod, b.positions(0))
+
+
+def test_frames_outside_the_time_table():
+    """On the device a position outside its table is taken as 0; where the frame is a Python number it is refused."""
+    b = build(last_frame=20)
+    assert b.positions(0)[:, 0].max() == 1 and b.positions(19)[:, 0].max() == 20
+    for first in (-1, 20, 21, 255, 2 ** 40):
+        with pytest.raises(ValueError, match="last_frame"):
+            b.positions(first)
+    assert build(last_frame=70000).positions(69999)[:, 0].max() == 70000
