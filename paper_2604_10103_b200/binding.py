@@ -163,10 +163,13 @@ def make_config(w, merge: int = HF_MERGE_PER_HEAD, swa_kernel: int = HF_SWA_AUTO
 
 
 class Context:
-    """Owns one hf_ctx.  Methods mirror the C entry points one to one."""
+    """Owns one hf_ctx.  Methods mirror the C entry points one to one.  Counted for callers that come back to a layer (a backward pass): per
+    layer `selections`, the calls that made a block selection, and `changes`, those that changed its cache, state or parameters (a graph's
+    replays are not seen)."""
 
     def __init__(self, cfg: hf_config, device: int = 0):
         self.cfg, self.device = cfg, device
+        self.selections, self.changes = [0] * cfg.layers, [0] * cfg.layers
         self._h = C.c_void_p()
         _check(lib().hf_create(C.byref(cfg), device, C.byref(self._h)))
 
@@ -181,22 +184,36 @@ class Context:
         except Exception:
             pass
 
+    def _changes(self, first=0, n=None):
+        last = len(self.changes) if n is None else min(first + n, len(self.changes))
+        for i in range(max(first, 0), last):            # (the library refuses layers that it does not have)
+            self.changes[i] += 1
+
+    def _selects(self, layer):
+        if 0 <= layer < len(self.selections):
+            self.selections[layer] += 1
+
     # -- C ABI, one to one
     def hf_reset(self, layer=-1):
+        self._changes(max(layer, 0), 1 if layer >= 0 else None)
         _check(lib().hf_reset(self._h, layer, _stream()))
 
     def hf_set_merge_weights(self, layer, W, bias=None):
+        self._changes(layer, 1)
         _check(lib().hf_set_merge_weights(self._h, layer, _ptr(W), _ptr(bias), _stream()))
 
     def hf_set_rope(self, cos_q=None, sin_q=None, cos_k=None, sin_k=None):
         """float32 CUDA tensors [T_c, d/2] (or None) -- see include/hf.h."""
+        self._changes()
         _check(lib().hf_set_rope(self._h, _ptr(cos_q), _ptr(sin_q), _ptr(cos_k), _ptr(sin_k), _stream()))
 
     def hf_set_temporal_rope(self, t0, first_pair, n_pairs, cos_tab, sin_tab):
         """float32 CUDA tensors [t0 + 1, n_pairs] -- see include/hf.h."""
+        self._changes()
         _check(lib().hf_set_temporal_rope(self._h, t0, first_pair, n_pairs, _ptr(cos_tab), _ptr(sin_tab), _stream()))
 
     def hf_kv_append(self, layer, k, v):
+        self._changes(layer, 1)
         _check(lib().hf_kv_append(self._h, layer, _ptr(k), _ptr(v), _stream()))
 
     def hf_kv_append_layers(self, first_layer, ks, vs):
@@ -204,16 +221,20 @@ class Context:
         n = len(ks)
         ka = (C.c_void_p * n)(*[t.data_ptr() for t in ks])
         va = (C.c_void_p * n)(*[t.data_ptr() for t in vs])
+        self._changes(first_layer, n)
         _check(lib().hf_kv_append_layers(self._h, first_layer, n, ka, va, _stream()))
 
     def hf_state_absorb_layers(self, first_layer, n_layers, k_ev, v_ev, n_tokens):
         """k_ev, v_ev: bf16 CUDA tensors [n_layers, B, H, n_tokens, d]."""
+        self._changes(first_layer, n_layers)
         _check(lib().hf_state_absorb_layers(self._h, first_layer, n_layers, _ptr(k_ev), _ptr(v_ev), n_tokens, _stream()))
 
     def hf_state_absorb(self, layer, k_ev, v_ev, n_tokens):
+        self._changes(layer, 1)
         _check(lib().hf_state_absorb(self._h, layer, _ptr(k_ev), _ptr(v_ev), n_tokens, _stream()))
 
     def hf_block_select(self, layer, q, k_cur, mask_out=None, idx_out=None, scores_out=None):
+        self._selects(layer)
         _check(lib().hf_block_select(self._h, layer, _ptr(q), _ptr(k_cur), _ptr(mask_out), _ptr(idx_out),
                                      _ptr(scores_out), _stream()))
 
@@ -239,13 +260,16 @@ class Context:
         _check(lib().hf_linear_attn(self._h, layer, _ptr(q), _ptr(o_hist), _stream()))
 
     def hf_hybrid_forward(self, layer, q, k, v, o):
+        self._selects(layer)
         _check(lib().hf_hybrid_forward(self._h, layer, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _stream()))
 
     def hf_hybrid_forward_host(self, layer, q, k, v, o):
         """q, k, v, o: CPU tensors (pinned recommended)."""
+        self._selects(layer)
         _check(lib().hf_hybrid_forward_host(self._h, layer, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _stream()))
 
     def hf_kv_append_host(self, layer, k, v):
+        self._changes(layer, 1)
         _check(lib().hf_kv_append_host(self._h, layer, _ptr(k), _ptr(v), _stream()))
 
     def hf_get_state(self, layer, S=None, z=None):
@@ -262,6 +286,7 @@ class Context:
 
     def hf_state_import(self, image):
         """image: contiguous numpy uint8 array written by hf_state_export."""
+        self._changes()
         _check(lib().hf_state_import(self._h, C.c_void_p(image.ctypes.data), image.nbytes))
 
     def hf_query(self, layer, what) -> int:

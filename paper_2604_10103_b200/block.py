@@ -59,7 +59,8 @@ class _GatedFF(torch.autograd.Function):
 
 class _Attention(torch.autograd.Function):
     """The hybrid attention of one layer for the step with gradient: its selection is held fixed, the cached chunks and the state get no
-    gradient (Alg. 1).  The context must keep this layer's cache and selection until the backward pass."""
+    gradient (Alg. 1).  The context must keep this layer's cache and state until the backward pass, which refuses others; a selection that
+    has replaced this one's in between is made anew (the same q, k and cache: the same selection)."""
 
     @staticmethod
     def forward(ctx, q, k, v, context, layer):
@@ -69,17 +70,23 @@ class _Attention(torch.autograd.Function):
         context.hf_sparse_swa(layer, q, k, v, o, lse=lse)
         context.hf_linear_attn(layer, q, o_hist)
         ctx.save_for_backward(q, k, v, o, lse)
-        ctx.context, ctx.layer = context, layer
+        ctx.context, ctx.layer, ctx.selection, ctx.change = context, layer, context.selections[layer], context.changes[layer]
         return o + o_hist
 
     @staticmethod
     def backward(ctx, g):
         q, k, v, o, lse = ctx.saved_tensors
+        context, layer = ctx.context, ctx.layer
+        if context.changes[layer] != ctx.change:
+            raise RuntimeError(f"the cache or state of layer {layer} has changed since the forward pass")
+        if context.selections[layer] != ctx.selection:
+            context.hf_block_select(layer, q, k)
+            ctx.selection = context.selections[layer]
         g = g.contiguous()
         dq, dq_hist, dk, dv = (torch.empty_like(q) for _ in range(4))
-        ctx.context.hf_sparse_swa_backward_dq(ctx.layer, q, k, v, o, lse, g, dq)
-        ctx.context.hf_sparse_swa_backward_dkv(ctx.layer, q, k, v, o, lse, g, dk, dv)
-        ctx.context.hf_linear_attn_backward_dq(ctx.layer, q, g, dq_hist)
+        context.hf_sparse_swa_backward_dq(layer, q, k, v, o, lse, g, dq)
+        context.hf_sparse_swa_backward_dkv(layer, q, k, v, o, lse, g, dk, dv)
+        context.hf_linear_attn_backward_dq(layer, q, g, dq_hist)
         return dq + dq_hist, dk, dv, None, None
 
 

@@ -31,3 +31,50 @@ def test_autocast_to_another_type_is_refused():
             call(x, mod, b.positions(0))
     with torch.autocast("cuda", dtype=torch.bfloat16):
         assert torch.equal(b(x, mod, b.positions(0)), ref)
+
+
+def gradients(b, xs, mods, between=None, order=None):
+    """The chunks' gradients, all forward passes before the first backward pass."""
+    xs, ys = [x.clone().requires_grad_() for x in xs], []
+    b.zero_grad(set_to_none=True)
+    for x, mod in zip(xs, mods):
+        ys.append(b(x, mod, b.positions(4)))
+    if between:
+        between()
+    for i in order or range(len(xs)):
+        ys[i].float().square().sum().backward()
+    return [x.grad for x in xs] + [p.grad for p in b.parameters()]
+
+
+def test_forward_passes_of_one_layer_before_the_first_backward_pass():
+    """Each gradient is that of its own selection, whichever was made last."""
+    w, ctx, b = build()
+    with torch.no_grad():
+        x, mod = chunk(w, 0)
+        b.commit(x, mod, b.positions(0))
+    (x1, m1), (x2, m2) = chunk(w, 1), chunk(w, 2)
+    alone = [gradients(b, [x], [m]) for x, m in ((x1, m1), (x2, m2))]
+    both = gradients(b, [x1, x2], [m1, m2])
+    assert torch.equal(both[0], alone[0][0]) and torch.equal(both[1], alone[1][0])
+    back = gradients(b, [x1, x2], [m1, m2], order=[1, 0])
+    assert torch.equal(back[0], alone[0][0]) and torch.equal(back[1], alone[1][0])
+
+    def another():
+        with torch.no_grad():
+            b(x2, m2, b.positions(4))
+    assert all(torch.equal(p, q) for p, q in zip(gradients(b, [x1], [m1], another), alone[0]))
+
+
+def test_a_cache_or_state_that_has_changed_before_the_backward_pass():
+    w, ctx, b = build()
+    x, mod = chunk(w, 1)
+    k = torch.randn(w.batch, w.heads, 64, w.head_dim, device="cuda").bfloat16()
+
+    def commit():
+        with torch.no_grad():
+            b.commit(x, mod, b.positions(0))
+    for between in (commit, lambda: ctx.hf_state_absorb(0, k, k, 64), lambda: ctx.hf_reset(0), lambda: ctx.hf_reset(),
+                    lambda: ctx.hf_state_import(ctx.hf_state_export())):
+        with pytest.raises(RuntimeError, match="has changed since the forward pass"):
+            gradients(b, [x], [mod], between)
+    gradients(b, [x], [mod])
