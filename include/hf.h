@@ -382,7 +382,8 @@ hf_status hf_rope_axes(const hf_rope_shape* shape, const hf_rope_tensor* tensors
 /* Gated feed-forward:  g = x Wg^T,  u = x Wu^T,  h = act(g) u,  y = h Wd^T.   act: silu(g) = g / (1 + e^-g), or the tanh form of gelu.
  *   x [rows, width], Wg, Wu [hidden, width], Wd [out_width, hidden], y [rows, out_width]: bf16 or f16, weights contiguous.
  *   gate, up [rows, hidden] contiguous: g and u for the backward pass, rounded to the type, or both NULL.
- * h is rounded to the type between the two products (the tensor cores take 16-bit operands), from g and u in float32.
+ * h is rounded to the type between the two products (the tensor cores take 16-bit operands), from g and u in float32.  With f16 that also
+ * bounds h: act(g) u beyond 65504 becomes infinite, and its row of y infinite or NaN, where float32 would hold it; bf16 has float32's range.
  * width, hidden, out_width: multiples of 8; strides too; pointers 16-byte aligned. */
 enum { HF_ACT_SILU = 0, HF_ACT_GELU_TANH = 1 };
 typedef struct {
@@ -396,7 +397,8 @@ hf_status hf_gated_ff_workspace(const hf_ff_shape* shape, int backward, size_t* 
 hf_status hf_gated_ff(const hf_ff_shape* shape, const void* x, const void* w_gate, const void* w_up, const void* w_down, void* y,
                       void* gate, void* up, void* workspace, void* stream);
 /* dh = dy Wd,  dg = dh u act'(g),  du = dh act(g),   dx = dg Wg + du Wu,  dWg = dg^T x,  dWu = du^T x,  dWd = dy^T h  (h from g and u again;
- * dg, du and h rounded to the type).  gate, up: what the forward returned.  dx [rows, width], dWg, dWu, dWd: the type, contiguous, written.
+ * dg, du and h rounded to the type: with f16 dg and du below 6.1e-5 lose bits, and below 3e-8 all of them, so small gradients want a
+ * scaled dy, as f16 training has it).  gate, up: what the forward returned.  dx [rows, width], dWg, dWu, dWd: the type, contiguous, written.
  * dx, and the three weights' gradients together, may be NULL (not formed). */
 hf_status hf_gated_ff_backward(const hf_ff_shape* shape, const void* dy, const void* x, const void* w_gate, const void* w_up,
                                const void* w_down, const void* gate, const void* up, void* dx, void* dw_gate, void* dw_up,

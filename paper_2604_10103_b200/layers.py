@@ -297,7 +297,7 @@ def _ff_workspace(dev, shape, backward):
 def gated_ff(x, w_gate, w_up, w_down, act="silu", save=False):
     """y = (act(x w_gate^T) * (x w_up^T)) w_down^T.  x bf16 or f16 [..., width], rows with one common stride; w_gate, w_up [hidden, width],
     w_down [out_width, hidden] contiguous; act "silu" or "gelu_tanh".  save: returns (y, gate, up), the last two [rows, hidden] for
-    `gated_ff_backward`; otherwise y alone."""
+    `gated_ff_backward`; otherwise y alone.  act * up is rounded to x's type between the products: in float16 it ends at 65504."""
     dev, t, rows, width, hidden, out_width, stride = _ff_operands(x, w_gate, w_up, w_down, act)
     y = _empty_like(x) if out_width == width == stride else x.new_empty(x.shape[:-1] + (out_width,))
     gate = x.new_empty(rows, hidden) if save else None
@@ -312,7 +312,8 @@ def gated_ff(x, w_gate, w_up, w_down, act="silu", save=False):
 
 
 def gated_ff_backward(dy, x, w_gate, w_up, w_down, gate, up, act="silu"):
-    """Gradients of `gated_ff`: (dx, dw_gate, dw_up, dw_down) in x's type.  gate, up: as the forward returned them."""
+    """Gradients of `gated_ff`: (dx, dw_gate, dw_up, dw_down) in x's type.  gate, up: as the forward returned them.  The projections' gradients
+    are rounded to x's type on the way: in float16 dy wants a scale that keeps them above 6e-5."""
     dev, t, rows, width, hidden, out_width, stride = _ff_operands(x, w_gate, w_up, w_down, act)
     _like("dy", dy, dev, x.shape[:-1] + (out_width,), x.dtype)
     _dense("gate", gate, dev, (rows, hidden), x.dtype)
