@@ -2,6 +2,9 @@
 gated feed-forward, forward and backward.  Each is one call of the library (include/hf.h) on the current stream; outputs and workspaces
 come from torch's allocator.  There is no fallback: a tensor the library does not take raises.
 
+Where gradients are recorded and an input needs one, `layer_norm`, `rope_axes`, `split_heads_rope` and `gated_ff` are part of torch's graph,
+their backward passes the `*_backward` calls below (which may also be called by hand); a second derivative raises.
+
 The short calls are bound by the host, so the way to the library is kept short: the shapes are packed as the bytes of the C structures,
 tensors are asked for nothing twice, and outputs come from the cheapest of torch's ways to make one (empty_like and new_empty with plain
 numbers take 1.4 us, torch.empty with a type and a device 2.4, a view 1.1).
@@ -12,6 +15,7 @@ import functools
 import struct
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as hf
 
@@ -26,6 +30,7 @@ _FF = struct.Struct("@2iq3i2q").pack                        # hf_ff_shape
 _F32, _I32 = torch.float32, torch.int32
 _empty_like, _empty_strided = torch.empty_like, torch.empty_strided
 _lib, _stream, _check = hf.lib, hf._stream, hf._check
+_recording = torch.is_grad_enabled
 
 
 try:
@@ -127,6 +132,8 @@ def layer_norm(x, weight=None, bias=None, eps=1e-6, weight_offset=0.0, rows_per_
     """y = (x - mean) * rstd * (weight_offset + weight) + bias over the last axis; returns (y, mean, rstd), the last two float32 [rows].
     x: bf16, f16 or f32 [..., width], rows with one common stride.  weight, bias: [width] or [1, width]; with rows_per_group > 0
     [groups, width], row r of x taking row r // rows_per_group (slices of a modulation tensor are fine); x's type or float32; or None."""
+    if _recording() and (x.requires_grad or weight is not None and weight.requires_grad or bias is not None and bias.requires_grad):
+        return _LayerNorm.apply(x, weight, bias, eps, weight_offset, rows_per_group)
     dev = _current("x", x)
     rows, width, stride = _rows("x", x)
     t = _norm_type(x, width)
@@ -170,6 +177,25 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, weight_offset=0.0, rows_
     return dx, dw, db
 
 
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps, weight_offset, rows_per_group):
+        y, mean, rstd = layer_norm(x, weight, bias, eps, weight_offset, rows_per_group)
+        ctx.save_for_backward(x, weight, mean, rstd)
+        ctx.bias, ctx.args = None if bias is None else (bias.shape, bias.dtype), (weight_offset, rows_per_group)
+        ctx.mark_non_differentiable(mean, rstd)
+        ctx.set_materialize_grads(False)
+        return y, mean, rstd
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, _mean, _rstd):
+        x, weight, mean, rstd = ctx.saved_tensors
+        dx, dw, db = layer_norm_backward(dy.contiguous(), x, mean, rstd, weight, *ctx.args)
+        return (dx, None if weight is None else dw.view(weight.shape).to(weight.dtype),
+                None if ctx.bias is None else db.view(ctx.bias[0]).to(ctx.bias[1]), None, None, None)
+
+
 # ------------------------------------------------------------------------------------------------ rotary positions
 def _rope(x, B, T, d, tensors, n, pos, tables, pairing, inverse, dev):
     """tensors: the bytes of n hf_rope_tensor."""
@@ -205,6 +231,10 @@ def rope_axes(x, pos, tables, out=None, pairing="adjacent", inverse=False):
     """x [batch, tokens, heads, head_dim] (any strides, features contiguous) turned by its tokens' positions.  pos: int32 [tokens, axes]
     or [batch, tokens, axes]; tables: (cos, sin, extents, pairs per axis) as `rope.axis_tables` forms cos and sin, on the device.
     out: a tensor of x's shape and type with strides of its own, or x itself; None: a new one.  inverse: the backward pass."""
+    if _recording() and (x.requires_grad or out is not None and out.requires_grad):
+        if out is not None:
+            _fail("out is not taken where gradients are recorded")
+        return _RopeAxes.apply(x, pos, tables, pairing, inverse)
     dev = _current("x", x)
     if x.dim() != 4:
         _fail("x is [batch, tokens, heads, head_dim]")
@@ -224,6 +254,8 @@ def rope_axes(x, pos, tables, out=None, pairing="adjacent", inverse=False):
 def split_heads_rope(qkv, heads, kv_heads, pos, tables, pairing="adjacent"):
     """Rows of a fused projection [batch, tokens, (heads + 2 kv_heads) * head_dim] (row stride free) -> q, k, v [batch, heads, tokens, head_dim]
     as the hybrid attention takes them, q and k turned by their positions, in one launch."""
+    if _recording() and qkv.requires_grad:
+        return _SplitHeadsRope.apply(qkv, heads, kv_heads, pos, tables, pairing)
     dev = _current("qkv", qkv)
     if qkv.dim() != 3:
         _fail("qkv is [batch, tokens, (heads + 2 kv_heads) * head_dim]")
@@ -268,6 +300,44 @@ def split_heads_rope_backward(dq, dk, dv, pos, tables, pairing="adjacent"):
     return out
 
 
+def _features_dense(t):
+    """t with the features of a head contiguous; its other axes may lie as they do."""
+    return t if t.stride(-1) == 1 else t.contiguous()
+
+
+class _RopeAxes(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, pos, tables, pairing, inverse):
+        cos, sin, *sizes = tables
+        ctx.save_for_backward(pos, cos, sin)
+        ctx.args = sizes, pairing, inverse
+        return rope_axes(x, pos, tables, None, pairing, inverse)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        pos, cos, sin = ctx.saved_tensors
+        sizes, pairing, inverse = ctx.args
+        return rope_axes(_features_dense(dy), pos, (cos, sin, *sizes), None, pairing, not inverse), None, None, None, None
+
+
+class _SplitHeadsRope(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, qkv, heads, kv_heads, pos, tables, pairing):
+        cos, sin, *sizes = tables
+        ctx.save_for_backward(pos, cos, sin)
+        ctx.args = sizes, pairing
+        return split_heads_rope(qkv, heads, kv_heads, pos, tables, pairing)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dq, dk, dv):
+        pos, cos, sin = ctx.saved_tensors
+        sizes, pairing = ctx.args
+        return (split_heads_rope_backward(_features_dense(dq), _features_dense(dk), _features_dense(dv), pos, (cos, sin, *sizes), pairing),
+                None, None, None, None, None)
+
+
 # ------------------------------------------------------------------------------------------------ gated feed-forward
 def _ff_operands(x, w_gate, w_up, w_down, act):
     """(device, type, rows, width, hidden, out_width, row stride of x) of checked operands."""
@@ -298,6 +368,8 @@ def gated_ff(x, w_gate, w_up, w_down, act="silu", save=False):
     """y = (act(x w_gate^T) * (x w_up^T)) w_down^T.  x bf16 or f16 [..., width], rows with one common stride; w_gate, w_up [hidden, width],
     w_down [out_width, hidden] contiguous; act "silu" or "gelu_tanh".  save: returns (y, gate, up), the last two [rows, hidden] for
     `gated_ff_backward`; otherwise y alone.  act * up is rounded to x's type between the products: in float16 it ends at 65504."""
+    if _recording() and (x.requires_grad or w_gate.requires_grad or w_up.requires_grad or w_down.requires_grad):
+        return _GatedFF.apply(x, w_gate, w_up, w_down, act, save)
     dev, t, rows, width, hidden, out_width, stride = _ff_operands(x, w_gate, w_up, w_down, act)
     y = _empty_like(x) if out_width == width == stride else x.new_empty(x.shape[:-1] + (out_width,))
     gate = x.new_empty(rows, hidden) if save else None
@@ -328,3 +400,21 @@ def gated_ff_backward(dy, x, w_gate, w_up, w_down, gate, up, act="silu"):
     if status:
         _check(status)
     return dx, dwg, dwu, dwd
+
+
+class _GatedFF(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w_gate, w_up, w_down, act, save):
+        y, gate, up = gated_ff(x, w_gate, w_up, w_down, act, True)
+        ctx.save_for_backward(x, w_gate, w_up, w_down, gate, up)
+        ctx.act = act
+        if not save:
+            return y
+        ctx.mark_non_differentiable(gate, up)
+        ctx.set_materialize_grads(False)
+        return y, gate, up
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, *_):
+        return *gated_ff_backward(dy.contiguous(), *ctx.saved_tensors, ctx.act), None, None
