@@ -9,52 +9,12 @@ library, and the plain projections are torch's.  `python -m paper_2604_10103_b20
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as hf
 from . import inputs as gen
 from . import layers
 from . import rope
-
-
-class _Norm(torch.autograd.Function):
-    """Layer norm with scale and shift per group of rows: y = xhat (1 + scale_g) + shift_g."""
-
-    @staticmethod
-    def forward(ctx, x, scale, shift, rows_per_group, eps):
-        y, mean, rstd = layers.layer_norm(x, scale, shift, eps=eps, weight_offset=1.0, rows_per_group=rows_per_group)
-        ctx.save_for_backward(x, scale, mean, rstd)
-        ctx.rows_per_group = rows_per_group
-        return y
-
-    @staticmethod
-    def backward(ctx, dy):
-        x, scale, mean, rstd = ctx.saved_tensors
-        dx, dscale, dshift = layers.layer_norm_backward(dy.contiguous(), x, mean, rstd, scale, weight_offset=1.0, rows_per_group=ctx.rows_per_group)
-        return dx, dscale.to(scale.dtype), dshift.to(scale.dtype), None, None
-
-
-class _HeadsRope(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, qkv, heads, pos, tables):
-        ctx.pos, ctx.tables = pos, tables
-        return layers.split_heads_rope(qkv, heads, heads, pos, tables)
-
-    @staticmethod
-    def backward(ctx, dq, dk, dv):
-        return layers.split_heads_rope_backward(dq, dk, dv, ctx.pos, ctx.tables), None, None, None
-
-
-class _GatedFF(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, x, w_gate, w_up, w_down, act):
-        y, gate, up = layers.gated_ff(x, w_gate, w_up, w_down, act=act, save=True)
-        ctx.save_for_backward(x, w_gate, w_up, w_down, gate, up)
-        ctx.act = act
-        return y
-
-    @staticmethod
-    def backward(ctx, dy):
-        return layers.gated_ff_backward(dy.contiguous(), *ctx.saved_tensors, act=ctx.act) + (None,)
 
 
 class _Attention(torch.autograd.Function):
@@ -74,6 +34,7 @@ class _Attention(torch.autograd.Function):
         return o + o_hist
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g):
         q, k, v, o, lse = ctx.saved_tensors
         context, layer = ctx.context, ctx.layer
@@ -134,6 +95,12 @@ class DenoiserBlock(torch.nn.Module):
         pos[:, 0] += first_frame
         return pos
 
+    def _norm(self, x, scale, shift):
+        """xhat (1 + scale) + shift, one row of scale and shift [batch, frames, width] for the tokens of a frame."""
+        width = x.shape[-1]
+        return layers.layer_norm(x, scale.reshape(-1, width), shift.reshape(-1, width), eps=self.eps, weight_offset=1.0,
+                                 rows_per_group=self.w.tokens_per_frame)[0]
+
     def _heads(self, x, mod, pos):
         taken = [self.w.batch, self.w.chunk_tokens, self.w.heads * self.w.head_dim]
         if list(x.shape) != taken:              # (the attention reads and writes as much, whatever it is given)
@@ -141,17 +108,15 @@ class DenoiserBlock(torch.nn.Module):
         _bf16("x", x)
         if x.get_device() != self.context.device:
             raise ValueError(f"x is on {x.device}, the context on device {self.context.device}")
-        width, frame = x.shape[-1], self.w.tokens_per_frame
-        h = _Norm.apply(x, mod[:, :, 1].reshape(-1, width), mod[:, :, 0].reshape(-1, width), frame, self.eps)
+        h = self._norm(x, mod[:, :, 1], mod[:, :, 0])
         qkv = torch.nn.functional.linear(h, self.w_qkv)
         _bf16("the projection", qkv)            # (autocast may have changed its type)
-        return _HeadsRope.apply(qkv, self.w.heads, pos, (self.cos, self.sin, self.extents, self.pairs))
+        return layers.split_heads_rope(qkv, self.w.heads, self.w.heads, pos, (self.cos, self.sin, self.extents, self.pairs))
 
     def forward(self, x, mod, pos):
         """x [batch, tokens of a chunk, width]; mod [batch, frames of the chunk, 6, width]: shift, scale, gate of the attention half, then of the
         feed-forward's; pos: `positions` of the chunk's first frame."""
         q, k, v = self._heads(x, mod, pos)
-        width = x.shape[-1]
         if torch.is_grad_enabled() and q.requires_grad:
             o = _Attention.apply(q, k, v, self.context, self.layer)
         else:
@@ -159,11 +124,8 @@ class DenoiserBlock(torch.nn.Module):
             self.context.hf_hybrid_forward(self.layer, q, k, v, o)
         per_token = mod.repeat_interleave(self.w.tokens_per_frame, dim=1)
         x = x + per_token[:, :, 2] * torch.nn.functional.linear(o.transpose(1, 2).flatten(2), self.w_out)
-        h = _Norm.apply(x, mod[:, :, 4].reshape(-1, width), mod[:, :, 3].reshape(-1, width), self.w.tokens_per_frame, self.eps)
-        if torch.is_grad_enabled():
-            y = _GatedFF.apply(h, self.w_gate, self.w_up, self.w_down, self.act)
-        else:
-            y = layers.gated_ff(h, self.w_gate, self.w_up, self.w_down, act=self.act)
+        h = self._norm(x, mod[:, :, 4], mod[:, :, 3])
+        y = layers.gated_ff(h, self.w_gate, self.w_up, self.w_down, act=self.act)
         return x + per_token[:, :, 5] * y
 
     @torch.no_grad()

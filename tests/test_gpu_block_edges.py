@@ -78,3 +78,31 @@ def test_a_cache_or_state_that_has_changed_before_the_backward_pass():
         with pytest.raises(RuntimeError, match="has changed since the forward pass"):
             gradients(b, [x], [mod], between)
     gradients(b, [x], [mod])
+
+
+def test_second_derivatives_are_refused():
+    w, ctx, b = build()
+    x, mod = chunk(w, 1)
+    x.requires_grad_()
+    g, = torch.autograd.grad(b(x, mod, b.positions(0)).float().square().sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        g.float().square().sum().backward()
+
+
+def test_the_attention_alone_refuses_a_second_derivative():
+    from paper_2604_10103_b200 import block as bl
+    w, ctx, b = build()
+    q, k, v = (torch.randn(w.batch, w.heads, w.chunk_tokens, w.head_dim, device="cuda").bfloat16().requires_grad_() for _ in range(3))
+    g, = torch.autograd.grad(bl._Attention.apply(q, k, v, ctx, 0).float().square().sum(), q, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        g.float().square().sum().backward()
+
+
+def test_positions_that_change_before_the_backward_pass_are_seen():
+    w, ctx, b = build()
+    x, mod = chunk(w, 1)
+    pos = b.positions(0)
+    y = b(x.requires_grad_(), mod, pos)
+    pos += 1
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.float().sum().backward()
