@@ -146,6 +146,24 @@ k_norm(const NormParams p) {
     }
 }
 
+// A row that a bulk copy brings has not come yet.  The wait is bounded like every wait: a row that never comes leaves garbage, and the flag.  Returns
+// whether the thread has lost a row; it then waits for no other and asks for no more copies.
+__device__ __noinline__ bool norm_wait_slow(uint32_t bar, uint32_t phase, bool lost, int* dev_status, int where) {
+    if (lost) return true;
+    const long long t0 = clock64();
+    while (clock64() - t0 < tc5::WAIT_LIMIT_CYCLES)
+        if (tc5::mbar_try_wait(bar, phase)) return false;
+    atomicOr(dev_status, HF_DEV_TIMEOUT_FLAG);
+    atomicExch(dev_status + 1, where);
+    return true;
+}
+// Copies in flight land before their memory is used for something else, or the thread block leaves.
+__device__ __forceinline__ void norm_drain(bool lost) {
+    if (!lost) return;
+    const long long t0 = clock64();
+    while (clock64() - t0 < 400000) {}
+}
+
 // The same for many rows: thread blocks stay, one a multiprocessor, and their teams of tpr threads walk the rows of a group (the factors and
 // shifts of the group in shared memory), each with a ring of `stages` rows in shared memory that bulk copies fill: as k_norm_bwd does,
 // which see.  A row's stage is free as soon as its elements are in the team's registers.
@@ -200,20 +218,13 @@ k_norm_rows(const NormParams p) {
     };
     int stage = 0, buf = 0;
     uint32_t phase = 0;
+    bool lost = false;
     for (long long r0 = first; r0 < g1; r0 += step, buf ^= 1) {         // (the teams walk in step)
         const long long row = r0 + team;
         const bool on = row < g1;
         const T* gx = static_cast<const T*>(p.x) + row * p.x_stride;
         const Row<T, V, WIDE> x(s_ring + stage * slot_bytes, WIDE ? 0 : (uint32_t)(reinterpret_cast<uintptr_t>(gx) & 15));
-        // bounded like every wait: a row that never came would leave garbage, and the flag
-        if (on && !tc5::mbar_try_wait(bar + 8 * stage, phase)) {
-            const long long t0 = clock64();
-            while (!tc5::mbar_try_wait(bar + 8 * stage, phase) && clock64() - t0 < tc5::WAIT_LIMIT_CYCLES) {}
-            if (clock64() - t0 >= tc5::WAIT_LIMIT_CYCLES) {
-                atomicOr(p.dev_status, HF_DEV_TIMEOUT_FLAG);
-                atomicExch(p.dev_status + 1, 92);
-            }
-        }
+        if (on && !tc5::mbar_try_wait(bar + 8 * stage, phase)) lost = norm_wait_slow(bar + 8 * stage, phase, lost, p.dev_status, 92);
         Vec<T, V> xv[NV];
         float s[V];
 #pragma unroll
@@ -239,7 +250,7 @@ k_norm_rows(const NormParams p) {
             for (int w = 0; w < warps; ++w) sum += own[w];
         }
         // (every thread of the team has its elements)
-        if (t == 0 && on && row + p.stages * step < g1) load(row + p.stages * step, stage);
+        if (t == 0 && on && !lost && row + p.stages * step < g1) load(row + p.stages * step, stage);
         if (++stage == p.stages) { stage = 0; phase ^= 1; }
         const float mean = sum * inv;
 #pragma unroll
@@ -285,6 +296,7 @@ k_norm_rows(const NormParams p) {
             if (in) put_floats<T, V, WIDE>(y + col, f, col + 1 < p.width);
         }
     }
+    norm_drain(lost);
 }
 
 // grid groups x thread blocks per group, block (tpr, teams): a team of tpr threads shares a row, each thread V NV columns of it, the same
@@ -356,7 +368,8 @@ k_norm_bwd(const NormParams p) {
     if (first + team < g1) { mean_next = p.mean[first + team]; rstd_next = p.rstd[first + team]; }
     int stage = 0, buf = 0;
     uint32_t phase = 0;
-    long long before = -1;                              // the row before, whose stage is read no more once the team has met
+    bool lost = false;
+    long long before = g1;                              // the row before (at first none), whose stage is read no more once the team has met
     int before_stage = 0;
     for (long long r0 = first; r0 < g1; r0 += step, buf ^= 1) {         // (the teams walk in step)
         const long long row = r0 + team;
@@ -368,17 +381,7 @@ k_norm_bwd(const NormParams p) {
         const uint8_t* slot_x = s_ring + 2 * stage * slot_bytes;
         const Row<T, V, WIDE> x = RING ? Row<T, V, WIDE>(slot_x, WIDE ? 0 : (uint32_t)(reinterpret_cast<uintptr_t>(gx) & 15)) : Row<T, V, WIDE>(gx);
         const Row<T, V, WIDE> dy = RING ? Row<T, V, WIDE>(slot_x + slot_bytes, WIDE ? 0 : (uint32_t)(reinterpret_cast<uintptr_t>(gd) & 15)) : Row<T, V, WIDE>(gd);
-        if constexpr (RING) {
-            // bounded like every wait: a row that never came would leave garbage, and the flag
-            if (on && !tc5::mbar_try_wait(bar + 8 * stage, phase)) {
-                const long long t0 = clock64();
-                while (!tc5::mbar_try_wait(bar + 8 * stage, phase) && clock64() - t0 < tc5::WAIT_LIMIT_CYCLES) {}
-                if (clock64() - t0 >= tc5::WAIT_LIMIT_CYCLES) {
-                    atomicOr(p.dev_status, HF_DEV_TIMEOUT_FLAG);
-                    atomicExch(p.dev_status + 1, 91);
-                }
-            }
-        }
+        if (RING && on && !tc5::mbar_try_wait(bar + 8 * stage, phase)) lost = norm_wait_slow(bar + 8 * stage, phase, lost, p.dev_status, 91);
         float s1[V], s2[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) { s1[j] = 0.f; s2[j] = 0.f; }
@@ -412,7 +415,7 @@ k_norm_bwd(const NormParams p) {
             for (int w = 0; w < warps; ++w) { const float2 o = own[w]; m1 += o.x; m2 += o.y; }
         }
         if constexpr (RING) {                           // (behind the sums every thread of the team has left the row before)
-            if (t == 0 && before >= 0 && before + p.stages * step < g1) load(before + p.stages * step, before_stage);
+            if (t == 0 && !lost && before + p.stages * step < g1) load(before + p.stages * step, before_stage);
             before = row; before_stage = stage;
             if (++stage == p.stages) { stage = 0; phase ^= 1; }
         }
@@ -437,6 +440,7 @@ k_norm_bwd(const NormParams p) {
             if (in) put_floats<T, V, WIDE>(dx + col, xf, two);
         }
     }
+    norm_drain(lost);
     if (p.dw == nullptr && p.db == nullptr) return;
     // the teams' sums: all to shared memory, then added column by column
     const int cols = V * NV * tpr;
