@@ -374,7 +374,7 @@ k_norm_bwd(const NormParams p) {
     for (long long r0 = first; r0 < g1; r0 += step, buf ^= 1) {         // (the teams walk in step)
         const long long row = r0 + team;
         const bool on = row < g1;
-        const float rstd = rstd_next, neg = -mean_next * rstd;          // xhat = x rstd + neg
+        const float rstd = rstd_next, neg = -mean_next;                 // xhat = (x + neg) rstd: an offset of the row costs its gradients nothing
         if (row + step < g1) { mean_next = p.mean[row + step]; rstd_next = p.rstd[row + step]; }
         const T* gx = static_cast<const T*>(p.x) + row * p.x_stride;
         const T* gd = static_cast<const T*>(p.dy) + row * p.y_stride;
@@ -397,7 +397,8 @@ k_norm_bwd(const NormParams p) {
                 dy.get(col, d, two);
                 load_factors(col, a);
                 if constexpr (!WIDE) { if (!in) d[0] = 0.f; }
-                vfma(xf, xf, rstd, neg);
+                vadd(xf, neg);
+                vmul(xf, rstd);
                 vmul(gh, d, a);
                 vfma(accw[i], d, xf, accw[i]);
                 vadd(accb[i], d);
@@ -421,7 +422,7 @@ k_norm_bwd(const NormParams p) {
         }
         if (!on || p.y == nullptr) continue;
         // dx = rstd gh - rstd m1 - xhat rstd m2
-        const float c1 = -m1 * inv * rstd, c2 = -m2 * inv * rstd;
+        const float c1 = -m1 * inv * rstd, c2 = -m2 * inv * rstd * rstd;
         T* dx = static_cast<T*>(p.y) + row * p.dx_stride;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -433,7 +434,7 @@ k_norm_bwd(const NormParams p) {
             x.get(col, xf, two);
             dy.get(col, d, two);
             load_factors(col, a);
-            vfma(xf, xf, rstd, neg);
+            vadd(xf, neg);
             vmul(d, d, a);
             vfma(xf, xf, c2, c1);
             vfma(xf, d, rstd, xf);

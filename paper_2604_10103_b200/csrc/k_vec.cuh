@@ -148,7 +148,7 @@ __device__ __forceinline__ void stay_packed(Vec<T, V>& v) {
     }
 }
 
-// Element-wise arithmetic on V floats, two an instruction where V is even: r = a b + c, r = a b, r += b.
+// Element-wise arithmetic on V floats, two an instruction where V is even: r = a b + c, r = a b, r *= b, r += b.
 template <int V> __device__ __forceinline__ void vfma(float (&r)[V], const float (&a)[V], const float (&b)[V], const float (&c)[V]) {
     if constexpr (V % 2 == 0) {
 #pragma unroll
@@ -208,6 +208,18 @@ template <int V> __device__ __forceinline__ void vadd(float (&r)[V], const float
 #pragma unroll
         for (int i = 0; i < V; ++i) r[i] += b[i];
     }
+}
+template <int V> __device__ __forceinline__ void vadd(float (&r)[V], float b) {
+    float v[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = b;
+    vadd(r, v);
+}
+template <int V> __device__ __forceinline__ void vmul(float (&r)[V], float b) {
+    float v[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = b;
+    vmul(r, r, v);
 }
 template <int V> __device__ __forceinline__ float vsum(const float (&a)[V]) {
     float s = a[0];
