@@ -252,7 +252,10 @@ k_norm_rows(const NormParams p) {
         // (every thread of the team has its elements)
         if (t == 0 && on && !lost && row + p.stages * step < g1) load(row + p.stages * step, stage);
         if (++stage == p.stages) { stage = 0; phase ^= 1; }
-        const float mean = sum * inv;
+        // (a quotient that float32 holds comes out exactly, so that the mean of a row of one value is that value: the product with the
+        // rounded reciprocal, refined once by its residual, which the fused multiply-add forms exactly)
+        float mean = sum * inv;
+        if (fabsf(mean) < INFINITY) mean = fmaf(fmaf(-mean, (float)p.width, sum), inv, mean);
 #pragma unroll
         for (int j = 0; j < V; ++j) s[j] = 0.f;
 #pragma unroll
