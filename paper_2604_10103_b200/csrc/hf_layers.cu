@@ -400,10 +400,12 @@ hf_status hf_rope_axes(const hf_rope_shape* g, const hf_rope_tensor* tensors, in
             if (!stride_ok(v, e)) wide = false;
         if (!aligned(t.x, 16) || !aligned(t.y, 16)) wide = false;
         p.t[p.n_tensors++] = {t.x, t.y, s[0], s[1], s[2], s[3], s[4], s[5], t.heads, t.rotate};
+        if (t.heads > 0x7ffffff0 - p.total_heads) return fail(HF_ERR_SHAPE, "the tensors have more than 2^31 heads together");
         p.total_heads += t.heads;
     }
     if (p.total_heads == 0) return HF_OK;
-    if ((long long)g->batch * g->tokens * (g->head_dim / 2) / 256 > 0x7ffffff0LL) return fail(HF_ERR_SHAPE, "too many tokens");
+    // (thread blocks of 256 threads; a thread takes at least two features)
+    if ((long long)g->batch * g->tokens > 0x7ffffff0LL * 256 / (g->head_dim / 2)) return fail(HF_ERR_SHAPE, "too many tokens");
     const Device* d;
     HFL_TRY(current_device(&d));
     p.cos_tab = cos_tab; p.sin_tab = sin_tab; p.pos = pos; p.pos_batch = g->batch > 1 ? g->pos_batch : 0;
