@@ -134,7 +134,11 @@ template <int ACT, bool SLOPE> __device__ __forceinline__ float2 ff_act2(float2 
     if constexpr (SLOPE) {
         const float2 q = ffma2(p, make_float2(-1.f, -1.f), one);
         if constexpr (ACT == HF_ACT_SILU) *slope = ffma2(a, q, p);
-        else *slope = ffma2(fmul2(a, q), ffma2(fmul2(g, g), make_float2(3.f * FF_GELU_B * FF_GELU_2A, 3.f * FF_GELU_B * FF_GELU_2A), make_float2(FF_GELU_2A, FF_GELU_2A)), p);
+        else {
+            // (a q is 0 long before the square of the gate overflows, which it may not make a NaN of)
+            const float2 gg = fmul2(g, g), s = make_float2(fminf(gg.x, 1e30f), fminf(gg.y, 1e30f));
+            *slope = ffma2(fmul2(a, q), ffma2(s, make_float2(3.f * FF_GELU_B * FF_GELU_2A, 3.f * FF_GELU_B * FF_GELU_2A), make_float2(FF_GELU_2A, FF_GELU_2A)), p);
+        }
     }
     return a;
 }
