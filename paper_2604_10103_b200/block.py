@@ -60,7 +60,8 @@ def _bf16(name, t):
 class DenoiserBlock(torch.nn.Module):
     """One layer.  w: an `inputs.Workload` (batch, heads, head_dim, frames); high x wide tokens a frame; context: the `binding.Context`
     that holds the layer's cache and state; last_frame: the last frame of the stream in the time table (8 bytes a frame and pair: a million
-    frames of a head of 128 take 176 MB; a longer stream starts anew at frame 0, after `hf_reset`)."""
+    frames of a head of 128 take 176 MB).  A stream without an end has its time from the context: with `hf_set_temporal_rope` for the pairs
+    0 .. pairs[0] - 1 the library turns and re-indexes them, and the positions given here are 0 on the time axis (no gradient then)."""
 
     def __init__(self, w, high, wide, context, layer=0, hidden=None, act="silu", last_frame=255, eps=1e-6, device="cuda", dtype=torch.bfloat16):
         super().__init__()

@@ -106,3 +106,30 @@ def test_positions_that_change_before_the_backward_pass_are_seen():
     pos += 1
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         y.float().sum().backward()
+
+
+def test_time_from_the_context():
+    """The relative temporal rotation of the library in place of the time axis: the same angles between queries and keys, so the same attention (all
+    blocks kept, nothing in the history).  q and k are rounded once more on the way (U each, and the keys of the cache); the rest is the same."""
+    import numpy as np
+    from tests import layer_forms as lf
+
+    def stream(own):
+        w, ctx, b = build(keep=1000, window=3)
+        if not own:
+            n, t0 = b.pairs[0], 40
+            th = np.arange(t0 + 1)[:, None] * 10000.0 ** (-np.arange(n) / n)[None, :]
+            ctx.hf_set_temporal_rope(t0, 0, n, torch.from_numpy(np.cos(th).astype(np.float32)).cuda(), torch.from_numpy(np.sin(th).astype(np.float32)).cuda())
+        out = []
+        with torch.no_grad():
+            for i in range(3):
+                x, mod = chunk(w, i)
+                pos = b.positions(i * w.chunk_frames)
+                if not own:
+                    pos[:, 0] = 0
+                out.append(b(x, mod, pos))
+                b.commit(x, mod, pos)
+        assert ctx.hf_get_device_status() == (0, 0)
+        return out
+    for got, ref in zip(stream(False), stream(True)):
+        assert lf.rel(got, lf.f64(ref)) < 3 * lf.U[torch.bfloat16]
