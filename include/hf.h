@@ -338,7 +338,8 @@ typedef struct {
 } hf_norm_shape;
 
 /* weight, bias, mean, rstd may be NULL (no factor, no shift; not written).  mean, rstd float [rows].  y may be x.  Pointers are aligned to
- * their element, and rows may start anywhere; rows that all start on 16 bytes, with a width of a multiple of 16 bytes, are the fastest. */
+ * their element, and rows may start anywhere; rows that all start on 16 bytes, with a width of a multiple of 16 bytes, are the fastest.  Of others
+ * the whole 16-byte units that hold a row are read (up to 15 bytes in front of it and behind it, whose values do not matter). */
 hf_status hf_layer_norm(const hf_norm_shape* shape, const void* x, const void* weight, const void* bias, void* y, float* mean,
                         float* rstd, void* stream);
 

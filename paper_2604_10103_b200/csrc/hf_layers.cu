@@ -98,7 +98,7 @@ bool norm_wide(const hf_norm_shape* g, const void* const* rows, const long long*
 }
 
 // Backward: threads a row, teams of them, thread blocks.  A team has as few warps as its columns' sums fit in (48 columns a thread; 32760 rows
-// of 1536 bf16: 59 us, with 24 columns and two warps a team 64, with 16 and three 69).  A thread block has up to twelve warps, fewer where
+// of 1536 bf16, when that was measured: 59 us, with 24 columns and two warps a team 64, with 16 and three 69).  A thread block has up to twelve warps, fewer where
 // there are not two rows a team for every multiprocessor or two rows of each team do not fit in shared memory.  The number of thread
 // blocks depends on the shape and its alignment alone, as the workspace does.
 NormPlan norm_bwd_plan(const hf_norm_shape* g, bool wide, int sms) {
@@ -172,7 +172,7 @@ hf_status launch_norm_of(const NormParams& p, bool wide, cudaStream_t st) {
 // Many rows (k_norm_rows): as norm_bwd_plan, with 24 warps a thread block, and no sums over rows to hold.  us, this / a thread block's rows at
 // once (k_norm): 28213 x 1456 bf16 34 / 40, 8000 rows 16.6 / 17.6, 4680 x 1536 10.3 / 9 (so from two rows a team on); rows that do not
 // start on 16 bytes, where the copies also align them: 28213 x 1455 61 / 125, 4000 rows 17 / 19, 600 rows 7.5 / 7.2, 300 rows 7.5 / 6.8,
-// 600 x 6001 10 / 16 (so from four rows a multiprocessor on).  Floats on 16 bytes: 28213 x 1536 69 / 58 (never).
+// 600 x 6001 10 / 16 (so from four rows a multiprocessor on).  Floats on 16 bytes: 28213 x 1536 69 / 56 (never).
 template <typename T, int V, int NV, bool WIDE>
 hf_status launch_norm_rows(const Device* d, const NormParams& p, const NormPlan& n, cudaStream_t st) {
     struct Key {};

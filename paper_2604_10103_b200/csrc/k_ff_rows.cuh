@@ -3,7 +3,7 @@
 //   GATED  h = act(x Wg^T) (x Wu^T): a thread block owns 8 hidden features; the 16 rows of an MMA are their 8 rows of Wg and 8 of Wu
 //   else   y = h Wd^T: 8 rows of Wd, the MMA's other 8 rows stay zero (finer units keep more multiprocessors reading)
 // The 8 columns of an MMA are 8 rows of x.  The warps of a thread block split the contraction, and their sums meet in shared memory, in
-// order.  A contraction index may be permuted if both operands are: lane (g, t) holds the 16 bytes at 32 j + 8 t of row g, and its four words
+// order.  Sums are float32; h is rounded once between the products, as the tiled kernels round it.  A contraction index may be permuted if both operands are: lane (g, t) holds the 16 bytes at 32 j + 8 t of row g, and its four words
 // serve as the two k-steps' fragments, so every load is 16 bytes.  The second product's weights are on their way before the first
 // kernel has finished.  Width 1536, hidden 4096 (37.7 MB of weights, 5.8 us at the measured copy rate): one row 10.5 us for both kernels (3.6 TB/s:
 // two launches, and latency at their ends), 8 rows 11.2, 16 rows 13.7.

@@ -3,9 +3,11 @@
 //   y = xhat a + b_g,  a = weight_offset + w_g,  g = the row's group
 //   gh = dy a,  dx = rstd (gh - mean(gh) - xhat mean(gh xhat)),  dw_g = sum over the group's rows of dy xhat,  db_g = sum of dy
 // All sums are float32.  A row stays in registers between its sums, so x (and dy) are read once; the variance is the mean of the squared
-// differences from the mean, not a difference of two large sums.  Memory bounds the long calls (backward of 32760 x 1536 bf16 59 us, 5.1 TB/s:
-// the main kernel 55, the partials' sums 3; forward of 28213 x 1456 34 us, 4.8 TB/s), the loads' latency the short ones (4680 x 1536 forward 9 us,
-// one round of thread blocks).
+// differences from the mean, not a difference of two large sums, and the backward pass forms x - mean before it scales it, so a row's offset
+// costs neither pass its accuracy.  Memory bounds the long calls (backward of 32760 x 1536 bf16 60.7 us, 5.0 TB/s: the main kernel 57, the partials'
+// sums 3; forward of 28213 x 1456 34.5 us, 4.8 TB/s), the loads' latency the short ones (4680 x 1536 forward 9.5 us, one round of thread blocks).
+// 16-bit rows that do not start on 16 bytes (28213 x 1455 bf16: 61 us forward, 130 backward) come out of shared memory a word and a shift a pair
+// on every pass, and leave as words or, where a row starts in the middle of one, element by element.
 #pragma once
 #include "k_vec.cuh"
 #include "tc5_common.cuh"
