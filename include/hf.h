@@ -405,6 +405,56 @@ hf_status hf_gated_ff_backward(const hf_ff_shape* shape, const void* dy, const v
                                const void* w_down, const void* gate, const void* up, void* dx, void* dw_gate, void* dw_up,
                                void* dw_down, void* workspace, void* stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * A training step's end: the norm of all gradients, and AdamW, each over many tensors at once.  As the calls above: current device, caller's
+ * stream, captured like any other work. */
+
+/* out[0] = the 2-norm of all tensors together; out[1] = min(1, max_norm / out[0]), the factor that brings it to max_norm at most (1 for a norm of
+ * 0; NaN where the norm is not finite, which hf_adamw takes as a step to leave out).  Squares are formed in float32, so a value beyond 1.8e19
+ * counts as not finite; they are summed in double, in a fixed order.  Tensors are contiguous.  out: device, two floats. */
+typedef struct {
+    const void* p;
+    int64_t n;                   /* elements                */
+    int type;                    /* HF_BF16 | HF_F16 | HF_F32 */
+} hf_gradient;
+hf_status hf_gradient_norm_workspace(int n_tensors, size_t* bytes);
+hf_status hf_gradient_norm(const hf_gradient* tensors, int n_tensors, float max_norm, float* out, void* workspace, void* stream);
+
+/* One step of AdamW, t = *step + 1 of each tensor, afterwards counted there:
+ *   g = factor grad,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   p = p - lr ((m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay p)
+ * in float32; a bf16 parameter is rounded once, from its float32 master where it has one (the master is what the step starts from; p is then
+ * only written).  state_bits 32: m, v float.  8: m e4m3, v e5m2 (one byte an element, values times the scale of their block of 256 elements),
+ * scales [ceil(n / 256)][2] float for m and v, rounded up or down at random, up with the probability of what is cut off, by a hash of seed, t
+ * and the element's place (256 first_block + its index): give every tensor blocks of its own.  A value that is not finite spoils its block of 256.
+ * factor: device float, or NULL (1); where it is not finite the call changes nothing.  lr_at: device float that stands for lr, or NULL, so that a
+ * captured step follows a schedule.  Pointers are aligned to their element, scales to 8 bytes; tensors whose pointers are all 16-byte aligned are
+ * the fastest.  Two calls on the same tensors or the same counter must not run at the same time. */
+typedef struct {
+    int param_type;              /* HF_BF16 | HF_F32                    */
+    int grad_type;               /* the parameters' type, or HF_F32     */
+    int state_bits;              /* 32 | 8                              */
+    uint32_t seed;
+    double beta1, beta2;         /* in [0, 1)                           */
+    double eps;
+    const float* factor;
+    int32_t* counter;            /* device, 0 before the first call; left 0 */
+} hf_adamw_step;
+typedef struct {
+    void* p;
+    const void* g;
+    float* master;               /* of bf16 parameters: NULL for all tensors of the call, or for none */
+    void* m;
+    void* v;
+    float* scales;               /* state_bits 8                        */
+    int32_t* step;               /* device: steps taken before (counted for a tensor of no elements too, where it is given) */
+    const float* lr_at;
+    int64_t n;                   /* elements, up to 2^43                */
+    int64_t first_block;
+    double lr, weight_decay;
+} hf_adamw_tensor;
+hf_status hf_adamw(const hf_adamw_step* step, const hf_adamw_tensor* tensors, int n_tensors, void* stream);
+
 /* Synchronises the current device and reports the status word of the calls without a context, as hf_get_device_status does for a
  * context's: flag 1 a bounded wait ran out (HF_ERR_DEVICE_TIMEOUT), flag 2 a position outside its table (HF_ERR_INVALID_ARG).  Clears it. */
 hf_status hf_layers_status(int* flags, int* detail);

@@ -33,7 +33,7 @@ EXPORTS = [
     "hf_status_string", "hf_last_error", "hf_state_absorb_noalloc", "hf_set_rope", "hf_state_export", "hf_state_import",
     "hf_sparse_swa_merged", "hf_slow_path_units", "hf_selftest_wait_limit", "hf_kv_append_layers", "hf_state_absorb_layers", "hf_set_temporal_rope", "hf_sparse_swa_backward_dq", "hf_sparse_swa_backward_dkv", "hf_linear_attn_backward_dq",
     "hf_layer_norm", "hf_layer_norm_workspace", "hf_layer_norm_backward", "hf_rope_axes", "hf_gated_ff_workspace", "hf_gated_ff",
-    "hf_gated_ff_backward", "hf_layers_status",
+    "hf_gated_ff_backward", "hf_layers_status", "hf_gradient_norm_workspace", "hf_gradient_norm", "hf_adamw",
 ]
 
 
@@ -63,6 +63,21 @@ class hf_rope_tensor(C.Structure):
 class hf_ff_shape(C.Structure):
     _fields_ = [("type", C.c_int), ("act", C.c_int), ("rows", C.c_int64), ("width", C.c_int), ("hidden", C.c_int),
                 ("out_width", C.c_int), ("x_stride", C.c_int64), ("y_stride", C.c_int64)]
+
+
+class hf_gradient(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("n", C.c_int64), ("type", C.c_int)]
+
+
+class hf_adamw_step(C.Structure):
+    _fields_ = [("param_type", C.c_int), ("grad_type", C.c_int), ("state_bits", C.c_int), ("seed", C.c_uint32), ("beta1", C.c_double),
+                ("beta2", C.c_double), ("eps", C.c_double), ("factor", C.c_void_p), ("counter", C.c_void_p)]
+
+
+class hf_adamw_tensor(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("g", C.c_void_p), ("master", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("scales", C.c_void_p),
+                ("step", C.c_void_p), ("lr_at", C.c_void_p), ("n", C.c_int64), ("first_block", C.c_int64), ("lr", C.c_double),
+                ("weight_decay", C.c_double)]
 
 
 class HFError(RuntimeError):
@@ -122,6 +137,9 @@ def lib() -> C.CDLL:
     L.hf_gated_ff_workspace.argtypes = [vp, ip, C.POINTER(C.c_size_t)]
     L.hf_gated_ff.argtypes = [vp] * 10
     L.hf_gated_ff_backward.argtypes = [vp] * 14
+    L.hf_gradient_norm_workspace.argtypes = [ip, C.POINTER(C.c_size_t)]
+    L.hf_gradient_norm.argtypes = [vp, ip, C.c_float, vp, vp, vp]
+    L.hf_adamw.argtypes = [vp, vp, ip, vp]
     L.hf_layers_status.argtypes = [C.POINTER(ip), C.POINTER(ip)]
     L.hf_status_string.argtypes = [ip]
     L.hf_status_string.restype = C.c_char_p
@@ -363,6 +381,22 @@ def hf_gated_ff(shape, x, w_gate, w_up, w_down, y, gate, up, workspace):
 def hf_gated_ff_backward(shape, dy, x, w_gate, w_up, w_down, gate, up, dx, dw_gate, dw_up, dw_down, workspace):
     _call(lib().hf_gated_ff_backward, shape, _ptr(dy), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(gate), _ptr(up), _ptr(dx),
           _ptr(dw_gate), _ptr(dw_up), _ptr(dw_down), _ptr(workspace))
+
+
+def hf_gradient_norm_workspace(n_tensors) -> int:
+    n = C.c_size_t()
+    _check(lib().hf_gradient_norm_workspace(n_tensors, C.byref(n)))
+    return n.value
+
+
+def hf_gradient_norm(tensors, n_tensors, max_norm, out, workspace):
+    """tensors: a ctypes array of hf_gradient, or its bytes."""
+    _check(lib().hf_gradient_norm(tensors, n_tensors, max_norm, _ptr(out), _ptr(workspace), _stream()))
+
+
+def hf_adamw(step, tensors, n_tensors):
+    """step: an hf_adamw_step, or its bytes; tensors: a ctypes array of hf_adamw_tensor, or its bytes."""
+    _call(lib().hf_adamw, step, tensors, n_tensors)
 
 
 def hf_layers_status():

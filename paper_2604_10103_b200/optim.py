@@ -1,0 +1,225 @@
+"""The end of a training step on torch CUDA tensors: the norm of all gradients, and AdamW over many tensors at once, in one launch each (two for the
+norm).  As in `layers`: calls of the library (include/hf.h) on the current device and stream, no fallback, what the library does not take raises.
+
+    optimizer = optim.AdamW(block.parameters(), lr=1e-4, state_bits=8)
+    loss.backward()
+    norm, factor = optim.gradient_norm([p.grad for p in block.parameters()], max_norm=1.0)
+    optimizer.step(grad_factor=factor)          # (a norm that is not finite leaves the step out; nothing waits for the device)
+"""
+from __future__ import annotations
+
+import functools
+import struct
+
+import numpy as np
+import torch
+
+from . import binding as hf
+from .layers import _TYPES, _check, _current, _fail, _here, _lib, _stream
+
+_F32, _BF16 = torch.float32, torch.bfloat16
+_BLOCK = 256                                                # elements that share a scale; tensors start at multiples of it in the state's buffers
+_STEP = struct.Struct("@3iI3d2P").pack                      # hf_adamw_step
+
+
+@functools.lru_cache(maxsize=256)
+def _norm_plan(dev, n):
+    return struct.Struct("@" + "Pqi4x" * n).pack, hf.hf_gradient_norm_workspace(n) // 8
+
+
+def gradient_norm(tensors, max_norm=float("inf")):
+    """(norm, factor), two float32 scalars on the device: the 2-norm of all tensors together (bf16, f16 or f32, contiguous, on the current device),
+    and min(1, max_norm / norm), which `AdamW.step` takes as its factor; NaN where the norm is not finite."""
+    tensors = list(tensors)
+    if not tensors:
+        _fail("no tensors")
+    dev = _current("tensors[0]", tensors[0])
+    rows = []
+    for i, t in enumerate(tensors):
+        kind = _TYPES.get(t.dtype)
+        if kind is None:
+            _fail(f"tensors[{i}] is {t.dtype}: bfloat16, float16 and float32 are taken")
+        if t.get_device() != dev:
+            _here(f"tensors[{i}]", t, dev)
+        if not t.is_contiguous():
+            _fail(f"tensors[{i}] has to be contiguous")
+        rows += (t.data_ptr(), t.numel(), kind)
+    n = len(tensors)
+    pack, doubles = _norm_plan(dev, n)
+    out = torch.empty(2, dtype=_F32, device=tensors[0].device)
+    ws = torch.empty(doubles, dtype=torch.float64, device=out.device)
+    status = _lib().hf_gradient_norm(pack(*rows), n, max_norm, out.data_ptr(), ws.data_ptr(), _stream())
+    if status:
+        _check(status)
+    return out.unbind()
+
+
+class AdamW(torch.optim.Optimizer):
+    """AdamW over bf16 and float32 parameters (contiguous, on the current device), all tensors in one launch.
+
+    state_bits 32: moments in float32.  8: the first in e4m3, the second in e5m2, with a float32 scale for each block of 256 elements, rounded up
+    or down at random by a hash of `seed`, step and place: a repeated run gives the same bits.  master_weights: a bf16 parameter has a float32
+    master, from which the step starts (without one, changes below half a step of bf16 are lost); a parameter that is written from outside takes
+    effect with `masters_from_parameters`.  lr may be a float32 tensor of one element on the device, which a captured step reads anew.
+
+    The state lies in `buffers` (m, v, scales, master, steps), each kind in one tensor, a parameter's part at the next multiple of 256 elements;
+    `state[p]` has a parameter's views.  All groups are given at construction.  A parameter without a gradient is left out of the step, and of its
+    count of steps."""
+
+    def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, state_bits=32, master_weights=True, seed=0):
+        if state_bits not in (8, 32):
+            _fail(f"state_bits {state_bits!r}: 8 and 32 are taken")
+        self._made = False
+        super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay))
+        self.state_bits, self.seed = state_bits, int(seed) & 0xffffffff
+        self._params = [p for g in self.param_groups for p in g["params"]]
+        dev, starts, at, master_at = None, [], 0, []
+        masters = 0
+        for i, p in enumerate(self._params):
+            dev = _current(f"parameter {i}", p)
+            if p.dtype is not _F32 and p.dtype is not _BF16:
+                _fail(f"parameter {i} is {p.dtype}: bfloat16 and float32 are taken")
+            if not p.is_contiguous():
+                _fail(f"parameter {i} has to be contiguous")
+            size = -(-p.numel() // _BLOCK) * _BLOCK
+            starts.append(at)
+            at += size
+            master_at.append(masters if master_weights and p.dtype is _BF16 else None)
+            if master_at[-1] is not None:
+                masters += size
+
+        def zeros(shape, dtype):
+            return torch.zeros(shape, dtype=dtype, device=self._params[0].device)
+        small = state_bits == 8
+        self.buffers = dict(m=zeros(at, torch.float8_e4m3fn if small else _F32), v=zeros(at, torch.float8_e5m2 if small else _F32),
+                            scales=zeros((at // _BLOCK, 2), _F32) if small else None, master=zeros(masters, _F32) if masters else None,
+                            steps=zeros(len(self._params) + 1, torch.int32))             # (the last: the library's counter)
+        for i, (p, a, ma) in enumerate(zip(self._params, starts, master_at)):
+            n = p.numel()
+            s = self.state[p] = dict(step=self.buffers["steps"][i], m=self.buffers["m"][a:a + n].view(p.shape), v=self.buffers["v"][a:a + n].view(p.shape))
+            if small:
+                s["scales"] = self.buffers["scales"][a // _BLOCK:-(-(a + n) // _BLOCK)]
+            if ma is not None:
+                s["master"] = self.buffers["master"][ma:ma + n].view(p.shape)
+        self._device, self._first_block = dev, [a // _BLOCK for a in starts]
+        self._plan, self._planned = None, None
+        self.masters_from_parameters()
+        self._made = True
+
+    def add_param_group(self, group):
+        if self._made:
+            _fail("all groups are given at construction: the state lies in one piece")
+        super().add_param_group(group)
+
+    @torch.no_grad()
+    def masters_from_parameters(self):
+        """The masters of the parameters as they are now (after weights were loaded)."""
+        for p in self._params:
+            master = self.state[p].get("master")
+            if master is not None:
+                master.copy_(p)
+
+    def _rows(self, params):
+        """The library's table of these parameters, without their gradients: int64 [n, 12], doubles in the last two columns."""
+        row = {}
+        for g in self.param_groups:
+            lr = g["lr"]
+            for p in g["params"]:
+                row[p] = (lr.data_ptr() if isinstance(lr, torch.Tensor) else 0, 0.0 if isinstance(lr, torch.Tensor) else float(lr), float(g["weight_decay"]))
+        table = np.zeros((len(params), 12), np.int64)
+        index = {p: i for i, p in enumerate(self._params)}
+        for r, p in zip(table, params):
+            s = self.state[p]
+            r[2:10] = [s["master"].data_ptr() if "master" in s else 0, s["m"].data_ptr(), s["v"].data_ptr(), s["scales"].data_ptr() if "scales" in s else 0,
+                       s["step"].data_ptr(), row[p][0], p.numel(), self._first_block[index[p]]]
+            r[10:].view(np.float64)[:] = row[p][1:]
+        return table
+
+    def _launches(self, params):
+        """The calls that a step over these parameters takes: those of one type, with or without masters, with the same betas and eps, together."""
+        of = {p: (g["betas"], g["eps"]) for g in self.param_groups for p in g["params"]}
+        kinds = {}
+        for p in params:
+            kinds.setdefault((p.dtype, p.grad.dtype, "master" in self.state[p], *of[p]), []).append(p)
+        counter = self.buffers["steps"].data_ptr() + 4 * len(self._params)
+        launches = []
+        for (dtype, grad_dtype, _, betas, eps), some in kinds.items():
+            table = self._rows(some)
+
+            def step(factor, head=(_TYPES[dtype], _TYPES[grad_dtype], self.state_bits, self.seed, *map(float, betas), float(eps))):
+                return _STEP(*head, factor, counter)
+            launches.append((some, dtype, grad_dtype, table, table.ctypes.data, step))
+        return launches
+
+    def _settings(self):
+        """What the tables were made from, and step for step may change."""
+        seen = []
+        for g in self.param_groups:
+            lr = g["lr"]
+            if isinstance(lr, torch.Tensor):
+                if lr.dtype is not _F32 or lr.numel() != 1:
+                    _fail("lr is a number, or a float32 tensor of one element")
+                if lr.get_device() != self._device:
+                    _here("lr", lr, self._device)
+                lr = ("at", lr.data_ptr())
+            seen.append((lr, g["weight_decay"], g["betas"], g["eps"]))
+        return seen
+
+    @torch.no_grad()
+    def step(self, closure=None, grad_factor=None):
+        """One step.  grad_factor: a float32 tensor of one element on the device (as `gradient_norm` returns it), by which the gradients are
+        multiplied; where it is not finite nothing is changed."""
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        factor = 0
+        if grad_factor is not None:
+            if grad_factor.dtype is not _F32 or grad_factor.numel() != 1:
+                _fail("grad_factor is a float32 tensor of one element")
+            if grad_factor.get_device() != self._device:
+                _here("grad_factor", grad_factor, self._device)
+            factor = grad_factor.data_ptr()
+        _current("the first parameter", self._params[0])
+        settings = self._settings()
+        some = [p for p in self._params if p.grad is not None]
+        if len(some) == len(self._params):
+            launches = self._plan if settings == self._planned else None
+            if launches is not None and any(p.grad.dtype is not kind for ps, _, kind, *_ in launches for p in ps):
+                launches = None
+            if launches is None:
+                launches = self._plan = self._launches(some)
+                self._planned = settings
+        else:
+            launches = self._launches(some)
+        for params, dtype, grad_dtype, table, at, step in launches:
+            grads = [p.grad for p in params]
+            for p, g in zip(params, grads):
+                if p.dtype is not dtype or p.get_device() != self._device or not p.is_contiguous():
+                    _fail("a parameter's type, device or layout is not what it was at construction")
+                if g.get_device() != self._device or not g.is_contiguous() or g.shape != p.shape:
+                    _fail(f"a gradient of {tuple(g.shape)} on {g.device} for a parameter of {tuple(p.shape)}: the same, contiguous, is taken")
+            table[:, 0] = [p.data_ptr() for p in params]
+            table[:, 1] = [g.data_ptr() for g in grads]
+            status = _lib().hf_adamw(step(factor), at, len(params), _stream())
+            if status:
+                _check(status)
+        return loss
+
+    @torch.no_grad()
+    def load_state_dict(self, state_dict):
+        """Into the state as it lies: the same parameters, state_bits and masters are taken, and refused before anything is changed otherwise."""
+        saved = state_dict["param_groups"]
+        if [len(g["params"]) for g in saved] != [len(g["params"]) for g in self.param_groups]:
+            _fail("the groups' numbers of parameters differ")
+        ids = [i for g in saved for i in g["params"]]
+        for i, p in zip(ids, self._params):
+            mine, theirs = self.state[p], state_dict["state"].get(i, {})
+            if mine.keys() != theirs.keys() or any(mine[k].shape != theirs[k].shape or mine[k].dtype != theirs[k].dtype for k in mine):
+                _fail(f"the state of parameter {i} is of another shape, type or kind")
+        for i, p in zip(ids, self._params):
+            for k, t in self.state[p].items():
+                t.copy_(state_dict["state"][i][k])
+        for mine, theirs in zip(self.param_groups, saved):
+            mine.update({k: v for k, v in theirs.items() if k != "params"})
+        self._plan = self._planned = None
