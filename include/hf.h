@@ -380,6 +380,41 @@ typedef struct {
 hf_status hf_rope_axes(const hf_rope_shape* shape, const hf_rope_tensor* tensors, int n_tensors, const float* cos_tab,
                        const float* sin_tab, const int32_t* pos, void* stream);
 
+/* Norms of q and k, their rotation and the split into heads in one pass.  rows [batch, tokens, (heads + 2 kv_heads) head_dim], a fused projection's: q's
+ * heads, then k's, then v's.  With r = 1 / sqrt(mean x^2 + eps), the mean over a head (HF_NORM_OVER_HEAD) or over all of q's (of k's) heads of the
+ * token (HF_NORM_OVER_WIDTH):   q = R (x r q_weight),  k = R (x r k_weight),  v as it is;   R as hf_rope_axes turns a head (axes, pairs,
+ * extent, pairing, tables and positions as there, a position outside its table too).
+ *   q_weight  [head_dim], or [heads head_dim] with HF_NORM_OVER_WIDTH (k_weight: kv_heads); NULL: 1
+ *   heads     q, k, v [batch, heads or kv_heads, tokens, head_dim], features contiguous, other strides free
+ * Pointers are aligned to their element; where all start on 16 bytes, head_dim is a multiple of 8 (and, in halves, the sum of pairs of 4) and
+ * strides are multiples of 16 bytes, the call is the fastest. */
+enum { HF_NORM_OVER_HEAD = 0, HF_NORM_OVER_WIDTH = 1 };
+typedef struct {
+    int type, param_type;                                /* of rows and heads; of the weights: `type` or HF_F32       */
+    int batch, tokens, head_dim;                         /* head_dim even, 2 .. 256                                   */
+    int heads, kv_heads;                                 /* kv_heads <= heads; heads x head_dim, in eights up to a power of two, <= 16384 */
+    int axes;                                            /* 1 .. 4                                                    */
+    int pairs[4], extent[4];
+    int pairing;
+    int over;
+    float eps;                                           /* >= 0                                                      */
+    int64_t pos_batch;
+    int64_t rows_batch, rows_token;                      /* strides of rows                                           */
+    int64_t grad_batch, grad_token;                      /* of their gradient                                         */
+} hf_heads_shape;
+typedef struct {
+    void* p;                                             /* written; backward: read                                   */
+    int64_t batch, token, head;                          /* strides                                                   */
+} hf_heads_tensor;
+hf_status hf_split_heads_norm_rope(const hf_heads_shape* shape, const void* rows, const void* q_weight, const void* k_weight,
+                                   const float* cos_tab, const float* sin_tab, const int32_t* pos, const hf_heads_tensor* heads, void* stream);
+/* With g = R^T dq, xh = x r, gw = g q_weight:  drows = r (gw - xh mean(gw xh)) for q, likewise for k, dv for v;  dq_weight = sum of g xh over the
+ * tokens (with HF_NORM_OVER_HEAD the heads too).  heads: dq, dk, dv.  The weights' gradients are float, written, and may be NULL. */
+hf_status hf_split_heads_norm_rope_workspace(const hf_heads_shape* shape, size_t* bytes);
+hf_status hf_split_heads_norm_rope_backward(const hf_heads_shape* shape, const hf_heads_tensor* heads, const void* rows, const void* q_weight,
+                                            const void* k_weight, const float* cos_tab, const float* sin_tab, const int32_t* pos, void* drows,
+                                            float* dq_weight, float* dk_weight, void* workspace, void* stream);
+
 /* Gated feed-forward:  g = x Wg^T,  u = x Wu^T,  h = act(g) u,  y = h Wd^T.   act: silu(g) = g / (1 + e^-g), or the tanh form of gelu.
  *   x [rows, width], Wg, Wu [hidden, width], Wd [out_width, hidden], y [rows, out_width]: bf16 or f16, weights contiguous.
  *   gate, up [rows, hidden] contiguous: g and u for the backward pass, rounded to the type, or both NULL.

@@ -22,6 +22,7 @@ HF_Z_SUM, HF_Z_FRAME_MEAN = 0, 1
 HF_BF16, HF_F16, HF_F32 = 0, 1, 2
 HF_PAIRS_ADJACENT, HF_PAIRS_HALVES = 0, 1
 HF_ACT_SILU, HF_ACT_GELU_TANH = 0, 1
+HF_NORM_OVER_HEAD, HF_NORM_OVER_WIDTH = 0, 1
 (HF_Q_CACHED_CHUNKS, HF_Q_KEY_BLOCKS, HF_Q_KEPT_BLOCKS, HF_Q_ABSORBED_TOKENS, HF_Q_QUERY_BLOCKS,
  HF_Q_MASK_WORDS, HF_Q_SWA_KERNEL, HF_Q_SINK_CHUNKS) = range(8)
 
@@ -33,7 +34,8 @@ EXPORTS = [
     "hf_status_string", "hf_last_error", "hf_state_absorb_noalloc", "hf_set_rope", "hf_state_export", "hf_state_import",
     "hf_sparse_swa_merged", "hf_slow_path_units", "hf_selftest_wait_limit", "hf_kv_append_layers", "hf_state_absorb_layers", "hf_set_temporal_rope", "hf_sparse_swa_backward_dq", "hf_sparse_swa_backward_dkv", "hf_linear_attn_backward_dq",
     "hf_layer_norm", "hf_layer_norm_workspace", "hf_layer_norm_backward", "hf_rope_axes", "hf_gated_ff_workspace", "hf_gated_ff",
-    "hf_gated_ff_backward", "hf_layers_status", "hf_gradient_norm_workspace", "hf_gradient_norm", "hf_adamw",
+    "hf_gated_ff_backward", "hf_layers_status", "hf_split_heads_norm_rope", "hf_split_heads_norm_rope_workspace", "hf_split_heads_norm_rope_backward",
+    "hf_gradient_norm_workspace", "hf_gradient_norm", "hf_adamw",
 ]
 
 
@@ -63,6 +65,17 @@ class hf_rope_tensor(C.Structure):
 class hf_ff_shape(C.Structure):
     _fields_ = [("type", C.c_int), ("act", C.c_int), ("rows", C.c_int64), ("width", C.c_int), ("hidden", C.c_int),
                 ("out_width", C.c_int), ("x_stride", C.c_int64), ("y_stride", C.c_int64)]
+
+
+class hf_heads_shape(C.Structure):
+    _fields_ = [("type", C.c_int), ("param_type", C.c_int), ("batch", C.c_int), ("tokens", C.c_int), ("head_dim", C.c_int), ("heads", C.c_int),
+                ("kv_heads", C.c_int), ("axes", C.c_int), ("pairs", C.c_int * 4), ("extent", C.c_int * 4), ("pairing", C.c_int), ("over", C.c_int),
+                ("eps", C.c_float), ("pos_batch", C.c_int64), ("rows_batch", C.c_int64), ("rows_token", C.c_int64), ("grad_batch", C.c_int64),
+                ("grad_token", C.c_int64)]
+
+
+class hf_heads_tensor(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("batch", C.c_int64), ("token", C.c_int64), ("head", C.c_int64)]
 
 
 class hf_gradient(C.Structure):
@@ -137,6 +150,9 @@ def lib() -> C.CDLL:
     L.hf_gated_ff_workspace.argtypes = [vp, ip, C.POINTER(C.c_size_t)]
     L.hf_gated_ff.argtypes = [vp] * 10
     L.hf_gated_ff_backward.argtypes = [vp] * 14
+    L.hf_split_heads_norm_rope.argtypes = [vp] * 9
+    L.hf_split_heads_norm_rope_workspace.argtypes = [vp, C.POINTER(C.c_size_t)]
+    L.hf_split_heads_norm_rope_backward.argtypes = [vp] * 13
     L.hf_gradient_norm_workspace.argtypes = [ip, C.POINTER(C.c_size_t)]
     L.hf_gradient_norm.argtypes = [vp, ip, C.c_float, vp, vp, vp]
     L.hf_adamw.argtypes = [vp, vp, ip, vp]
@@ -366,6 +382,22 @@ def hf_layer_norm_backward(shape, dy, x, mean, rstd, weight, dx, dweight, dbias,
 def hf_rope_axes(shape, tensors, n_tensors, cos_tab, sin_tab, pos):
     """tensors: a ctypes array of hf_rope_tensor, or its bytes."""
     _call(lib().hf_rope_axes, shape, tensors, n_tensors, _ptr(cos_tab), _ptr(sin_tab), _ptr(pos))
+
+
+def hf_split_heads_norm_rope(shape, rows, q_weight, k_weight, cos_tab, sin_tab, pos, heads):
+    """heads: a ctypes array of three hf_heads_tensor, or its bytes."""
+    _call(lib().hf_split_heads_norm_rope, shape, _ptr(rows), _ptr(q_weight), _ptr(k_weight), _ptr(cos_tab), _ptr(sin_tab), _ptr(pos), heads)
+
+
+def hf_split_heads_norm_rope_workspace(shape) -> int:
+    n = C.c_size_t()
+    _check(lib().hf_split_heads_norm_rope_workspace(shape, C.byref(n)))
+    return n.value
+
+
+def hf_split_heads_norm_rope_backward(shape, heads, rows, q_weight, k_weight, cos_tab, sin_tab, pos, drows, dq_weight, dk_weight, workspace):
+    _call(lib().hf_split_heads_norm_rope_backward, shape, heads, _ptr(rows), _ptr(q_weight), _ptr(k_weight), _ptr(cos_tab), _ptr(sin_tab), _ptr(pos),
+          _ptr(drows), _ptr(dq_weight), _ptr(dk_weight), _ptr(workspace))
 
 
 def hf_gated_ff_workspace(shape, backward) -> int:

@@ -21,11 +21,14 @@ from . import binding as hf
 
 _TYPES = {torch.bfloat16: hf.HF_BF16, torch.float16: hf.HF_F16, torch.float32: hf.HF_F32}
 _PAIRINGS = {"adjacent": hf.HF_PAIRS_ADJACENT, "halves": hf.HF_PAIRS_HALVES}
+_OVERS = {"head": hf.HF_NORM_OVER_HEAD, "width": hf.HF_NORM_OVER_WIDTH}
 _ACTS = {"silu": hf.HF_ACT_SILU, "gelu_tanh": hf.HF_ACT_GELU_TANH}
 _NORM = struct.Struct("@3i6q2f").pack                       # hf_norm_shape
 _ROPE = struct.Struct("@5i4i4i2iq").pack                    # hf_rope_shape
 _ROPE_TENSOR = struct.Struct("@2P6q2i").pack                # hf_rope_tensor
 _ROPE_TENSORS = struct.Struct("@2P6q2i2P6q2i2P6q2i").pack   # three of them
+_HEADS = struct.Struct("@18if5q").pack                      # hf_heads_shape
+_HEADS_TENSORS = struct.Struct("@P3qP3qP3q").pack           # three hf_heads_tensor
 _FF = struct.Struct("@2iq3i2q").pack                        # hf_ff_shape
 _F32, _I32 = torch.float32, torch.int32
 _empty_like, _empty_strided = torch.empty_like, torch.empty_strided
@@ -335,6 +338,128 @@ class _SplitHeadsRope(torch.autograd.Function):
         pos, cos, sin = ctx.saved_tensors
         sizes, pairing = ctx.args
         return (split_heads_rope_backward(_features_dense(dq), _features_dense(dk), _features_dense(dv), pos, (cos, sin, *sizes), pairing),
+                None, None, None, None, None)
+
+
+# ------------------------------------------------------------------------------------------------ norms of q and k, with the rotation
+def _norm_rope(qkv, heads, kv_heads, q_weight, k_weight, pos, tables, eps, over, pairing, grad_strides):
+    """(device, batch, tokens, head_dim, the packed hf_heads_shape, cos, sin) of checked operands."""
+    dev = _current("qkv", qkv)
+    if qkv.dim() != 3:
+        _fail("qkv is [batch, tokens, (heads + 2 kv_heads) * head_dim]")
+    B, T, W = qkv.shape
+    if heads < 1 or kv_heads < 1 or W % (heads + 2 * kv_heads):
+        _fail(f"{W} columns do not divide into {heads} + 2 x {kv_heads} heads")
+    xb, xt, one = qkv.stride()
+    if one != 1 and W > 1:
+        _fail("qkv: the last axis has to be contiguous")
+    d = W // (heads + 2 * kv_heads)
+    cos, sin, extents, pairs = tables
+    axes = len(pairs)
+    if not (1 <= axes <= 4 and len(extents) == axes):
+        _fail("one to four axes, an extent and a number of pairs for each")
+    if pairing not in _PAIRINGS:
+        _fail(f"pairing {pairing!r} unknown")
+    if over not in _OVERS:
+        _fail(f"over {over!r} unknown")
+    dtype = qkv.dtype
+    if dtype not in _TYPES:
+        _fail(f"qkv is {dtype}: bfloat16, float16 and float32 are taken")
+    n_entries = 0
+    for e, p in zip(extents, pairs):
+        n_entries += e * p
+    if not (cos.dtype is _F32 and sin.dtype is _F32 and cos.get_device() == dev == sin.get_device() and cos.is_contiguous()
+            and sin.is_contiguous() and cos.shape == (n_entries,) == sin.shape):
+        _dense("cos", cos, dev, (n_entries,), _F32)
+        _dense("sin", sin, dev, (n_entries,), _F32)
+    shape = pos.shape
+    if shape != (T, axes) and shape != (1, T, axes) and shape != (B, T, axes):
+        _fail(f"pos has shape {tuple(shape)}: [{T}, {axes}] or [{B}, {T}, {axes}] is taken")
+    if pos.dtype is not _I32 or pos.get_device() != dev or not pos.is_contiguous():
+        _dense("pos", pos, dev, shape, _I32)
+    kind = dtype
+    if q_weight is not None or k_weight is not None:
+        kind = (k_weight if q_weight is None else q_weight).dtype
+        if kind != dtype and kind != _F32:
+            _fail(f"the weights are {kind}: qkv's type or float32 is taken")
+        if q_weight is not None:
+            _dense("q_weight", q_weight, dev, (d if over == "head" else heads * d,), kind)
+        if k_weight is not None:
+            _dense("k_weight", k_weight, dev, (d if over == "head" else kv_heads * d,), kind)
+    rest = (0,) * (4 - axes)
+    return dev, B, T, d, _HEADS(_TYPES[dtype], _TYPES[kind], B, T, d, heads, kv_heads, axes, *pairs, *rest, *extents, *rest, _PAIRINGS[pairing], _OVERS[over],
+                                eps, T * axes if B > 1 and len(shape) == 3 and shape[0] == B else 0, xb, xt, *grad_strides), cos, sin
+
+
+def split_heads_norm_rope(qkv, heads, kv_heads, q_weight, k_weight, pos, tables, eps=1e-6, over="head", pairing="adjacent"):
+    """`split_heads_rope` of a block with norms of q and k, in one launch: before the rotation q and k are multiplied by 1 / sqrt(mean x^2 + eps), the
+    mean over a head (over "head") or over all heads of the token ("width"), and by a weight, [head_dim] or [heads * head_dim] (k: kv_heads), of
+    qkv's type or float32, or None."""
+    if _recording() and (qkv.requires_grad or q_weight is not None and q_weight.requires_grad or k_weight is not None and k_weight.requires_grad):
+        return _SplitHeadsNormRope.apply(qkv, heads, kv_heads, q_weight, k_weight, pos, tables, eps, over, pairing)
+    dev, B, T, d, shape, cos, sin = _norm_rope(qkv, heads, kv_heads, q_weight, k_weight, pos, tables, eps, over, pairing, (0, 0))
+    q = qkv.new_empty(B, heads, T, d)
+    k = qkv.new_empty(B, kv_heads, T, d)
+    v = _empty_like(k)
+    td = T * d
+    status = _lib().hf_split_heads_norm_rope(shape, qkv.data_ptr(), q_weight.data_ptr() if q_weight is not None else None,
+                                             k_weight.data_ptr() if k_weight is not None else None, cos.data_ptr(), sin.data_ptr(), pos.data_ptr(),
+                                             _HEADS_TENSORS(q.data_ptr(), heads * td, d, td, k.data_ptr(), kv_heads * td, d, td, v.data_ptr(), kv_heads * td, d, td),
+                                             _stream())
+    if status:
+        _check(status)
+    return q, k, v
+
+
+@functools.lru_cache(maxsize=256)
+def _norm_rope_workspace(dev, shape):
+    return hf.hf_split_heads_norm_rope_workspace(shape)
+
+
+def split_heads_norm_rope_backward(dq, dk, dv, qkv, q_weight, k_weight, pos, tables, eps=1e-6, over="head", pairing="adjacent"):
+    """Gradients of `split_heads_norm_rope`: (dqkv contiguous, dq_weight, dk_weight float32).  dq, dk, dv: any strides with the features of a head contiguous."""
+    if dq.dim() != 4 or dk.dim() != 4:
+        _fail("dq, dk, dv are [batch, heads, tokens, head_dim]")
+    W = qkv.shape[-1]
+    dev, B, T, d, shape, cos, sin = _norm_rope(qkv, dq.shape[1], dk.shape[1], q_weight, k_weight, pos, tables, eps, over, pairing, (qkv.shape[1] * W, W))
+    H, KV = dq.shape[1], dk.shape[1]
+    _like("dq", dq, dev, (B, H, T, d), qkv.dtype)
+    _like("dk", dk, dev, (B, KV, T, d), qkv.dtype)
+    _like("dv", dv, dev, (B, KV, T, d), qkv.dtype)
+    parts = ()
+    for t in (dq, dk, dv):
+        xb, xh, xt, one = t.stride()
+        if one != 1 and d > 1:
+            _fail("the features of a head have to be contiguous")
+        parts += (t.data_ptr(), xb, xt, xh)
+    out = qkv.new_empty(B, T, W)
+    dqw = _empty_strided((d if over == "head" else H * d,), (1,), dtype=_F32, device=qkv.device)
+    dkw = dqw.new_empty(d if over == "head" else KV * d)
+    ws = dqw.new_empty(_norm_rope_workspace(dev, shape) // 4)
+    status = _lib().hf_split_heads_norm_rope_backward(shape, _HEADS_TENSORS(*parts), qkv.data_ptr(), q_weight.data_ptr() if q_weight is not None else None,
+                                                      k_weight.data_ptr() if k_weight is not None else None, cos.data_ptr(), sin.data_ptr(),
+                                                      pos.data_ptr(), out.data_ptr(), dqw.data_ptr(), dkw.data_ptr(), ws.data_ptr(), _stream())
+    if status:
+        _check(status)
+    return out, dqw, dkw
+
+
+class _SplitHeadsNormRope(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, qkv, heads, kv_heads, q_weight, k_weight, pos, tables, eps, over, pairing):
+        cos, sin, *sizes = tables
+        ctx.save_for_backward(qkv, q_weight, k_weight, pos, cos, sin)
+        ctx.args = sizes, eps, over, pairing
+        return split_heads_norm_rope(qkv, heads, kv_heads, q_weight, k_weight, pos, tables, eps, over, pairing)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dq, dk, dv):
+        qkv, q_weight, k_weight, pos, cos, sin = ctx.saved_tensors
+        sizes, eps, over, pairing = ctx.args
+        dqkv, dqw, dkw = split_heads_norm_rope_backward(_features_dense(dq), _features_dense(dk), _features_dense(dv), qkv, q_weight, k_weight, pos,
+                                                        (cos, sin, *sizes), eps, over, pairing)
+        return (dqkv, None, None, None if q_weight is None else dqw.to(q_weight.dtype), None if k_weight is None else dkw.to(k_weight.dtype),
                 None, None, None, None, None)
 
 
