@@ -421,7 +421,7 @@ hf_status hf_split_heads_norm_rope_backward(const hf_heads_shape* shape, const h
  * h is rounded to the type between the two products (the tensor cores take 16-bit operands), from g and u in float32.  With f16 that also
  * bounds h: act(g) u beyond 65504 becomes infinite, and its row of y infinite or NaN, where float32 would hold it; bf16 has float32's range.
  * width, hidden, out_width: multiples of 8; strides too; pointers 16-byte aligned. */
-enum { HF_ACT_SILU = 0, HF_ACT_GELU_TANH = 1 };
+enum { HF_ACT_SILU = 0, HF_ACT_GELU_TANH = 1, HF_ACT_NONE = 2 };       /* (NONE: hf_linear alone) */
 typedef struct {
     int type;                    /* HF_BF16 | HF_F16 */
     int act;
@@ -439,6 +439,31 @@ hf_status hf_gated_ff(const hf_ff_shape* shape, const void* x, const void* w_gat
 hf_status hf_gated_ff_backward(const hf_ff_shape* shape, const void* dy, const void* x, const void* w_gate, const void* w_up,
                                const void* w_down, const void* gate, const void* up, void* dx, void* dw_gate, void* dw_up,
                                void* dw_down, void* workspace, void* stream);
+
+/* A linear layer with its epilogue:  pre = x W^T + bias,  y = residual + gate_g act(pre),  g = row / rows_per_group (0 for every row when that is 0).
+ *   x [rows, width], W [out_width, width] contiguous, y and residual [rows, out_width]: bf16 or f16.  bias [out_width], gate [groups, out_width],
+ *   rows gate_stride apart: that type or float (param_type).  bias, gate, residual may be NULL; act HF_ACT_NONE: act(pre) = pre.
+ *   pre [rows, out_width] contiguous: for the backward pass, rounded to the type, or NULL.
+ * Sums and the epilogue are float32; y is rounded once.  With gate rows_per_group of the latent frame and residual the stream x, this is the end of either
+ * half of a denoiser block.  width, out_width, strides: multiples of 8; pointers 16-byte aligned.  y may be the residual, with its stride.
+ * workspace may be NULL where hf_linear_workspace says 0 bytes. */
+typedef struct {
+    int type, param_type;        /* HF_BF16 | HF_F16; of bias and gate: `type` or HF_F32 */
+    int act;                     /* HF_ACT_NONE | HF_ACT_SILU | HF_ACT_GELU_TANH         */
+    int width, out_width;        /* up to 2^17       */
+    int64_t rows;                /* up to 2^24       */
+    int64_t x_stride, y_stride, residual_stride;         /* between rows of x, of y or dy, of the residual */
+    int64_t rows_per_group, gate_stride;                 /* (gate_stride: not read with one group)         */
+} hf_linear_shape;
+hf_status hf_linear_workspace(const hf_linear_shape* shape, int backward, size_t* bytes);
+hf_status hf_linear(const hf_linear_shape* shape, const void* x, const void* weight, const void* bias, const void* gate, const void* residual,
+                    void* y, void* pre, void* workspace, void* stream);
+/* dp = dy gate_g act'(pre),  dx = dp W,  dW = dp^T x,  dbias = sum of dp over the rows,  dgate_g = sum of dy act(pre) over the group's rows.  dp is rounded
+ * to the type for the two products, and not for the sums (f16: as hf_gated_ff_backward says of dg).  pre: what the forward returned; not read with
+ * HF_ACT_NONE and without gate.  dx [rows, width], dweight: the type, contiguous; dbias [out_width], dgate [groups, out_width]: float, contiguous;
+ * written, each may be NULL.  (The residual's gradient is dy.) */
+hf_status hf_linear_backward(const hf_linear_shape* shape, const void* dy, const void* x, const void* weight, const void* pre, const void* gate,
+                             void* dx, void* dweight, float* dbias, float* dgate, void* workspace, void* stream);
 
 /* ------------------------------------------------------------------------------------------------------------------
  * A training step's end: the norm of all gradients, and AdamW, each over many tensors at once.  As the calls above: current device, caller's

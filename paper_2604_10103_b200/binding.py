@@ -21,7 +21,7 @@ HF_SWA_AUTO, HF_SWA_MMA, HF_SWA_TCGEN05, HF_SWA_TCGEN05_PINGPONG = 0, 1, 2, 3
 HF_Z_SUM, HF_Z_FRAME_MEAN = 0, 1
 HF_BF16, HF_F16, HF_F32 = 0, 1, 2
 HF_PAIRS_ADJACENT, HF_PAIRS_HALVES = 0, 1
-HF_ACT_SILU, HF_ACT_GELU_TANH = 0, 1
+HF_ACT_SILU, HF_ACT_GELU_TANH, HF_ACT_NONE = 0, 1, 2
 HF_NORM_OVER_HEAD, HF_NORM_OVER_WIDTH = 0, 1
 (HF_Q_CACHED_CHUNKS, HF_Q_KEY_BLOCKS, HF_Q_KEPT_BLOCKS, HF_Q_ABSORBED_TOKENS, HF_Q_QUERY_BLOCKS,
  HF_Q_MASK_WORDS, HF_Q_SWA_KERNEL, HF_Q_SINK_CHUNKS) = range(8)
@@ -34,7 +34,7 @@ EXPORTS = [
     "hf_status_string", "hf_last_error", "hf_state_absorb_noalloc", "hf_set_rope", "hf_state_export", "hf_state_import",
     "hf_sparse_swa_merged", "hf_slow_path_units", "hf_selftest_wait_limit", "hf_kv_append_layers", "hf_state_absorb_layers", "hf_set_temporal_rope", "hf_sparse_swa_backward_dq", "hf_sparse_swa_backward_dkv", "hf_linear_attn_backward_dq",
     "hf_layer_norm", "hf_layer_norm_workspace", "hf_layer_norm_backward", "hf_rope_axes", "hf_gated_ff_workspace", "hf_gated_ff",
-    "hf_gated_ff_backward", "hf_layers_status", "hf_split_heads_norm_rope", "hf_split_heads_norm_rope_workspace", "hf_split_heads_norm_rope_backward",
+    "hf_gated_ff_backward", "hf_layers_status", "hf_linear_workspace", "hf_linear", "hf_linear_backward", "hf_split_heads_norm_rope", "hf_split_heads_norm_rope_workspace", "hf_split_heads_norm_rope_backward",
     "hf_gradient_norm_workspace", "hf_gradient_norm", "hf_adamw",
 ]
 
@@ -76,6 +76,11 @@ class hf_heads_shape(C.Structure):
 
 class hf_heads_tensor(C.Structure):
     _fields_ = [("p", C.c_void_p), ("batch", C.c_int64), ("token", C.c_int64), ("head", C.c_int64)]
+
+
+class hf_linear_shape(C.Structure):
+    _fields_ = [("type", C.c_int), ("param_type", C.c_int), ("act", C.c_int), ("width", C.c_int), ("out_width", C.c_int), ("rows", C.c_int64),
+                ("x_stride", C.c_int64), ("y_stride", C.c_int64), ("residual_stride", C.c_int64), ("rows_per_group", C.c_int64), ("gate_stride", C.c_int64)]
 
 
 class hf_gradient(C.Structure):
@@ -153,6 +158,9 @@ def lib() -> C.CDLL:
     L.hf_split_heads_norm_rope.argtypes = [vp] * 9
     L.hf_split_heads_norm_rope_workspace.argtypes = [vp, C.POINTER(C.c_size_t)]
     L.hf_split_heads_norm_rope_backward.argtypes = [vp] * 13
+    L.hf_linear_workspace.argtypes = [vp, ip, C.POINTER(C.c_size_t)]
+    L.hf_linear.argtypes = [vp] * 10
+    L.hf_linear_backward.argtypes = [vp] * 12
     L.hf_gradient_norm_workspace.argtypes = [ip, C.POINTER(C.c_size_t)]
     L.hf_gradient_norm.argtypes = [vp, ip, C.c_float, vp, vp, vp]
     L.hf_adamw.argtypes = [vp, vp, ip, vp]
@@ -413,6 +421,21 @@ def hf_gated_ff(shape, x, w_gate, w_up, w_down, y, gate, up, workspace):
 def hf_gated_ff_backward(shape, dy, x, w_gate, w_up, w_down, gate, up, dx, dw_gate, dw_up, dw_down, workspace):
     _call(lib().hf_gated_ff_backward, shape, _ptr(dy), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(gate), _ptr(up), _ptr(dx),
           _ptr(dw_gate), _ptr(dw_up), _ptr(dw_down), _ptr(workspace))
+
+
+def hf_linear_workspace(shape, backward) -> int:
+    n = C.c_size_t()
+    _check(lib().hf_linear_workspace(shape, backward, C.byref(n)))
+    return n.value
+
+
+def hf_linear(shape, x, weight, bias, gate, residual, y, pre, workspace):
+    _call(lib().hf_linear, shape, _ptr(x), _ptr(weight), _ptr(bias), _ptr(gate), _ptr(residual), _ptr(y), _ptr(pre), _ptr(workspace))
+
+
+def hf_linear_backward(shape, dy, x, weight, pre, gate, dx, dweight, dbias, dgate, workspace):
+    _call(lib().hf_linear_backward, shape, _ptr(dy), _ptr(x), _ptr(weight), _ptr(pre), _ptr(gate), _ptr(dx), _ptr(dweight), _ptr(dbias), _ptr(dgate),
+          _ptr(workspace))
 
 
 def hf_gradient_norm_workspace(n_tensors) -> int:

@@ -1,8 +1,9 @@
-// Gated feed-forward: host side and the kernels' instantiations.
+// Gated feed-forward and linear layers: host side and the kernels' instantiations.
 #include "hf_layers.h"
 #include <type_traits>
 #include "k_ff_gemm.cuh"
 #include "k_ff_rows.cuh"
+#include "k_linear_bwd.cuh"
 
 #include <cstring>
 
@@ -45,15 +46,16 @@ struct Size { long long rows, cols, contraction; };
 // dx 2x256 321, 1x192 330, 1x256 335, 2x192 345; dW 2x512 278, 2x256 292, (2x256 317, 2x224 334, 1x256 335 before other parts were faster).
 // 1000 rows: dx 2x256/3 82, /2 87, /1 96, 2x128 92, 1x128 96.  300 rows: dx 1x128/4 56.5, 2x128/3 57, 1x64 67.5; y 1x64 30.5, 2x128 31; g, u 1x256
 // 31.9, 2x256 32, 1x128 35, 1x64 41.  77 rows: y 1x64/3 22.4, /4 23, /6 25.6, /1 26.8; dx 1x128/6 38.9, /4 40.9, /12 43.4, 1x64 57.9.
-enum FfCut { FF_CUT_GATED, FF_CUT_Y, FF_CUT_DH, FF_CUT_DX, FF_CUT_DW };
+enum FfCut { FF_CUT_GATED, FF_CUT_Y, FF_CUT_DH, FF_CUT_DX, FF_CUT_DW, FF_CUT_LINEAR };
 Tiling ff_tiling(const Device* d, const Size* s, int n, int segments, FfCut cut) {
-    const bool gated = cut == FF_CUT_GATED, b_mn = cut >= FF_CUT_DH, a_mn = cut == FF_CUT_DW, may_split = cut != FF_CUT_GATED && cut != FF_CUT_DH;
+    const bool gated = cut == FF_CUT_GATED, b_mn = cut >= FF_CUT_DH && cut <= FF_CUT_DW, a_mn = cut == FF_CUT_DW, may_split = cut != FF_CUT_GATED && cut != FF_CUT_DH;
     Tiling best = {1, 64, 1};
     double least = 1e300;
     for (int cg = 1; cg <= 2; ++cg)
         for (int bn = b_mn ? 64 * cg : 64; bn <= (a_mn && cg == 2 ? 512 : 256); bn += gated ? 64 : (b_mn ? 64 * cg : 32)) {
             if (bn > 256 && bn != 512) continue;
             if (cut == FF_CUT_DH && cg == 1 && bn > 128) break;         // (its staging leaves two stages)
+            if (cut == FF_CUT_LINEAR && cg == 1 && bn > 192) break;     // (three)
             const int out = gated ? bn / 2 : bn, slots = cg == 1 ? d->sm_count : d->pairs;
             long long tiles = 0;
             double blocks = 0;
@@ -121,7 +123,7 @@ struct Launch {
         if (p.splits == 1) return HF_OK;
         const long long warps = (long long)p.tile0[p.products] * 4 * CG * (p.bn / 8);
         join.cg = CG;
-        return launch_after(k_ff_join<T>, dim3((unsigned)((warps + 3) / 4)), dim3(128), 0, st, p, join);
+        return launch_after(k_ff_join<T, EPI == FF_LINEAR>, dim3((unsigned)((warps + 3) / 4)), dim3(128), 0, st, p, join);
     }
     template <int EPI, bool A_MN, bool B_MN>
     hf_status run(cudaStream_t st) {
@@ -336,6 +338,190 @@ hf_status hf_gated_ff_backward(const hf_ff_shape* g, const void* dy, const void*
         HFL_TRY(l.mn_major(&l.p.b[0], mx)); l.p.b[1] = l.p.b[0]; HFL_TRY(l.mn_major(&l.p.b[2], h));
         HFL_TRY(l.output(0, {dw_gate, N, K, K})); HFL_TRY(l.output(1, {dw_up, N, K, K})); HFL_TRY(l.output(2, {dw_down, O, N, N}));
         l.product(N, (int)K, M, l.tiling.bn); l.product(N, (int)K, M, l.tiling.bn); l.product(O, (int)N, M, l.tiling.bn);
+        HFL_TRY((l.run<FF_STORE, true, true>(st)));
+    }
+    return HF_OK;
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------------------------------------------------ linear layers
+namespace {
+hf_status linear_check(const hf_linear_shape* g) {
+    if (g == nullptr) return fail(HF_ERR_INVALID_ARG, "shape is null");
+    if (g->type != HF_BF16 && g->type != HF_F16) return fail(HF_ERR_UNSUPPORTED, "type %d: bf16 and f16 are taken", g->type);
+    if (g->param_type != g->type && g->param_type != HF_F32) return fail(HF_ERR_UNSUPPORTED, "param_type %d is neither the type nor HF_F32", g->param_type);
+    if (g->act != HF_ACT_SILU && g->act != HF_ACT_GELU_TANH && g->act != HF_ACT_NONE) return fail(HF_ERR_UNSUPPORTED, "act %d unknown", g->act);
+    if (g->rows < 0 || g->rows > (1 << 24)) return fail(HF_ERR_SHAPE, "rows %lld outside [0, 2^24]", (long long)g->rows);
+    const int w[2] = {g->width, g->out_width};
+    for (int v : w)
+        if (v < 8 || v % 8 || v > (1 << 17)) return fail(HF_ERR_SHAPE, "width and out_width are multiples of 8 up to 2^17: got %d", v);
+    if (g->rows > 1) {
+        if (g->x_stride < g->width || g->y_stride < g->out_width) return fail(HF_ERR_SHAPE, "row strides must be at least the width");
+        if (g->x_stride % 8 || g->y_stride % 8) return fail(HF_ERR_SHAPE, "row strides must be multiples of 8");
+        if (g->x_stride > (1LL << 36) || g->y_stride > (1LL << 36)) return fail(HF_ERR_SHAPE, "row strides too large");
+    }
+    if (g->rows_per_group < 0) return fail(HF_ERR_SHAPE, "rows_per_group must be >= 0");
+    return HF_OK;
+}
+// Rows of a group, no more than there are; groups.
+int linear_group(const hf_linear_shape* g) { return g->rows_per_group > 0 && g->rows_per_group < g->rows ? (int)g->rows_per_group : (int)g->rows; }
+int linear_groups(const hf_linear_shape* g) { return g->rows == 0 ? 0 : (int)((g->rows - 1) / linear_group(g) + 1); }
+hf_status linear_gate(const hf_linear_shape* g, const void* gate) {
+    if (!gate) return HF_OK;
+    HFL_TRY(ff_pointer(gate, "gate"));
+    if (g->rows > linear_group(g) && (g->gate_stride < g->out_width || g->gate_stride % 8 || g->gate_stride > (1LL << 36)))
+        return fail(HF_ERR_SHAPE, "gate_stride must be a multiple of 8, at least out_width");
+    return HF_OK;
+}
+Sizes linear_sizes(const hf_linear_shape* g) { return {{{g->rows, g->out_width, g->width}}}; }
+Sizes linear_dx_sizes(const hf_linear_shape* g) { return {{{g->rows, g->width, g->out_width}}}; }
+Sizes linear_dw_sizes(const hf_linear_shape* g) { return {{{g->out_width, g->width, g->rows}}}; }
+Tiling cut_linear(const Device* d, const hf_linear_shape* g) { return ff_tiling(d, linear_sizes(g).data, 1, 1, FF_CUT_LINEAR); }
+Tiling cut_linear_dx(const Device* d, const hf_linear_shape* g) { return ff_tiling(d, linear_dx_sizes(g).data, 1, 1, FF_CUT_DX); }
+Tiling cut_linear_dw(const Device* d, const hf_linear_shape* g) { return ff_tiling(d, linear_dw_sizes(g).data, 1, 1, FF_CUT_DW); }
+// Thread blocks that share a group's rows: so many that four a multiprocessor are at work, 32 rows each at least.
+int linear_parts(const Device* d, const hf_linear_shape* g) {
+    const long long others = (long long)((g->out_width + 255) / 256) * linear_groups(g), rows = linear_group(g);
+    long long n = others ? (4LL * d->sm_count + others - 1) / others : 1;
+    if (n > (rows + 31) / 32) n = (rows + 31) / 32;
+    return n < 1 ? 1 : (int)n;
+}
+
+template <typename T, int NT>
+hf_status launch_linear_rows(const FfRowsParams& p, int sms, cudaStream_t st) {
+    // 16 features a thread block where that keeps every multiprocessor busy, with half the threads; otherwise 8
+    if (p.features >= 16 * 2 * sms) return launch_after(k_ff_rows<T, NT, true, 0, true>, dim3((p.features + 15) / 16), dim3(256), 0, st, p);
+    return launch_after(k_ff_rows<T, NT, false, 0, true>, dim3((p.features + 7) / 8), dim3(512), 0, st, p);
+}
+template <typename T>
+hf_status launch_linear_bwd(const LinearBwdParams& p, int act, int groups, cudaStream_t st) {
+    const dim3 grid(groups * p.parts, (p.cols + 255) / 256);
+    auto kernel = act == HF_ACT_NONE ? k_linear_bwd<T, HF_ACT_NONE> : (act == HF_ACT_SILU ? k_linear_bwd<T, HF_ACT_SILU> : k_linear_bwd<T, HF_ACT_GELU_TANH>);
+    return launch_after(kernel, grid, dim3(32 * LINEAR_BWD_WARPS), 0, st, p);
+}
+// The backward pass's scratch: dp | the products' partial sums | those of db and dgate.
+struct LinearWorkspace { size_t products, sums, bytes; };
+LinearWorkspace linear_workspace(const Device* d, const hf_linear_shape* g) {
+    const size_t dp = round_up((size_t)g->rows * g->out_width * 2);
+    const size_t x = ff_partial_bytes(cut_linear_dx(d, g), linear_dx_sizes(g).data, 1), w = ff_partial_bytes(cut_linear_dw(d, g), linear_dw_sizes(g).data, 1);
+    const size_t part = round_up((size_t)linear_groups(g) * linear_parts(d, g) * g->out_width * sizeof(float));
+    return {dp, dp + round_up(x > w ? x : w), dp + round_up(x > w ? x : w) + 2 * part};
+}
+}  // namespace
+
+extern "C" {
+
+hf_status hf_linear_workspace(const hf_linear_shape* g, int backward, size_t* bytes) {
+    HFL_TRY(linear_check(g));
+    if (!bytes) return fail(HF_ERR_INVALID_ARG, "bytes is null");
+    *bytes = 0;
+    if (g->rows == 0) return HF_OK;
+    const Device* d;
+    HFL_TRY(ff_device(&d));
+    if (backward) *bytes = linear_workspace(d, g).bytes;
+    else if (g->rows > FF_ROWS_MOST) *bytes = ff_partial_bytes(cut_linear(d, g), linear_sizes(g).data, 1);
+    return HF_OK;
+}
+
+hf_status hf_linear(const hf_linear_shape* g, const void* x, const void* weight, const void* bias, const void* gate, const void* residual, void* y,
+                    void* pre, void* workspace, void* stream) {
+    HFL_TRY(linear_check(g));
+    if (g->rows == 0) return HF_OK;
+    HFL_TRY(ff_pointer(x, "x")); HFL_TRY(ff_pointer(weight, "weight")); HFL_TRY(ff_pointer(y, "y"));
+    if (bias) HFL_TRY(ff_pointer(bias, "bias"));
+    HFL_TRY(linear_gate(g, gate));
+    if (pre) HFL_TRY(ff_pointer(pre, "pre"));
+    if (residual) {
+        HFL_TRY(ff_pointer(residual, "residual"));
+        if (g->rows > 1 && (g->residual_stride < g->out_width || g->residual_stride % 8 || g->residual_stride > (1LL << 36)))
+            return fail(HF_ERR_SHAPE, "residual_stride must be a multiple of 8, at least out_width");
+    }
+    const Device* d;
+    HFL_TRY(ff_device(&d));
+    const cudaStream_t st = (cudaStream_t)stream;
+    const long long M = g->rows, K = g->width, N = g->out_width;
+    const LinearEpilogue e = {bias, gate, residual, pre, y, g->gate_stride, g->residual_stride, g->y_stride, N, linear_group(g), g->param_type == HF_F32, residual != nullptr};
+    if (M <= FF_ROWS_MOST) {
+        FfRowsParams p = {x, weight, weight, nullptr, nullptr, nullptr, g->x_stride, 0, (int)M, (int)K, (int)N, e, g->act};
+        if (g->type == HF_BF16) return M <= 8 ? launch_linear_rows<bf16, 1>(p, d->sm_count, st) : launch_linear_rows<bf16, 2>(p, d->sm_count, st);
+        return M <= 8 ? launch_linear_rows<__half, 1>(p, d->sm_count, st) : launch_linear_rows<__half, 2>(p, d->sm_count, st);
+    }
+    Launch l(d, g->type, g->act, cut_linear(d, g));
+    if (l.tiling.splits > 1) HFL_TRY(ff_pointer(workspace, "workspace"));
+    l.p.partials = static_cast<float*>(workspace);
+    l.p.linear = e;
+    HFL_TRY(l.k_major(&l.p.a[0], {x, M, K, g->x_stride}, 128));
+    HFL_TRY(l.k_major(&l.p.b[0], {weight, N, K, K}, l.p.bn / l.tiling.cg));
+    HFL_TRY(l.output(0, {y, M, N, g->y_stride}));
+    if (pre) { HFL_TRY(l.output(1, {pre, M, N, N})); l.p.save = 1; }
+    if (residual) HFL_TRY(l.box(&l.p.in[0], {residual, M, N, g->residual_stride}));
+    l.product(M, (int)N, K, l.p.bn);
+    return l.run<FF_LINEAR, false, false>(st);
+}
+
+hf_status hf_linear_backward(const hf_linear_shape* g, const void* dy, const void* x, const void* weight, const void* pre, const void* gate, void* dx,
+                             void* dweight, float* dbias, float* dgate, void* workspace, void* stream) {
+    HFL_TRY(linear_check(g));
+    if (dgate && !gate) return fail(HF_ERR_INVALID_ARG, "dgate without gate");
+    if (!aligned(dbias, 4) || !aligned(dgate, 4)) return fail(HF_ERR_INVALID_ARG, "dbias or dgate is not aligned");
+    const cudaStream_t st = (cudaStream_t)stream;
+    const long long M = g->rows, K = g->width, N = g->out_width;
+    if (dweight) HFL_TRY(ff_pointer(dweight, "dweight"));
+    if (M == 0) {               // (no groups either)
+        if (dweight) HFL_CUDA(cudaMemsetAsync(dweight, 0, (size_t)N * K * 2, st));
+        if (dbias) HFL_CUDA(cudaMemsetAsync(dbias, 0, (size_t)N * sizeof(float), st));
+        return HF_OK;
+    }
+    if (!dx && !dweight && !dbias && !dgate) return HF_OK;
+    HFL_TRY(ff_pointer(dy, "dy"));
+    HFL_TRY(linear_gate(g, gate));
+    const bool apart = g->act != HF_ACT_NONE || gate;           // dp is not dy
+    if (apart) HFL_TRY(ff_pointer(pre, "pre"));
+    if (dx) { HFL_TRY(ff_pointer(dx, "dx")); HFL_TRY(ff_pointer(weight, "weight")); }
+    if (dweight) HFL_TRY(ff_pointer(x, "x"));
+    HFL_TRY(ff_pointer(workspace, "workspace"));
+    const Device* d;
+    HFL_TRY(ff_device(&d));
+    const LinearWorkspace w = linear_workspace(d, g);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    const bool elements = apart && (dx || dweight);
+    const Matrix dp = elements ? Matrix{ws, M, N, N} : Matrix{dy, M, N, g->y_stride}, mx = {x, M, K, g->x_stride};
+    if (elements || dbias || dgate) {
+        const int groups = gate ? linear_groups(g) : 1;
+        LinearBwdParams p = {};
+        p.dy = dy; p.pre = apart ? pre : nullptr; p.dp = elements ? ws : nullptr; p.gate = gate;
+        p.dy_stride = g->y_stride; p.gate_stride = g->gate_stride; p.rows = (int)M; p.cols = (int)N; p.params_f32 = g->param_type == HF_F32;
+        p.group = gate ? linear_group(g) : (int)M;
+        hf_linear_shape whole = *g;
+        if (!gate) whole.rows_per_group = 0;
+        p.parts = linear_parts(d, &whole);
+        const size_t part = (size_t)groups * p.parts * N;
+        float* sums = reinterpret_cast<float*>(ws + w.sums);
+        const bool db_sum = dbias && groups * p.parts > 1, dgate_sum = dgate && p.parts > 1;
+        p.db_part = !dbias ? nullptr : (db_sum ? sums : dbias);
+        p.dgate_part = !dgate ? nullptr : (dgate_sum ? sums + round_up(part * sizeof(float)) / sizeof(float) : dgate);
+        HFL_TRY(g->type == HF_BF16 ? launch_linear_bwd<bf16>(p, g->act, groups, st) : launch_linear_bwd<__half>(p, g->act, groups, st));
+        if (db_sum || dgate_sum)
+            HFL_TRY(launch_after(k_linear_sum, dim3((db_sum ? 1 : 0) + (dgate_sum ? groups : 0), (unsigned)((N + 31) / 32)), dim3(32, 32), 0, st, (const float*)p.db_part,
+                                 groups * p.parts, db_sum ? dbias : nullptr, (const float*)p.dgate_part, p.parts, dgate, (int)N));
+    }
+    if (dx) {
+        Launch l(d, g->type, HF_ACT_NONE, cut_linear_dx(d, g));
+        l.p.partials = reinterpret_cast<float*>(ws + w.products);
+        HFL_TRY(l.k_major(&l.p.a[0], dp, 128));
+        HFL_TRY(l.mn_major(&l.p.b[0], {weight, N, K, K}));
+        HFL_TRY(l.output(0, {dx, M, K, K}));
+        l.product(M, (int)K, N, l.p.bn);
+        l.p.early_b = elements || dbias || dgate;       // (a kernel of this call that has waited comes before)
+        HFL_TRY((l.run<FF_STORE, false, true>(st)));
+    }
+    if (dweight) {
+        Launch l(d, g->type, HF_ACT_NONE, cut_linear_dw(d, g));
+        l.p.partials = reinterpret_cast<float*>(ws + w.products);
+        HFL_TRY(l.mn_major(&l.p.a[0], dp)); HFL_TRY(l.mn_major(&l.p.b[0], mx));
+        HFL_TRY(l.output(0, {dweight, N, K, K}));
+        l.product(N, (int)K, M, l.tiling.bn);
         HFL_TRY((l.run<FF_STORE, true, true>(st)));
     }
     return HF_OK;

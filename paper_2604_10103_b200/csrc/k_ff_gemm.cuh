@@ -3,6 +3,7 @@
 //   GATED    g = x Wg^T and u = x Wu^T side by side in one accumulator; h = act(g) u (and g, u)       A, B: contraction contiguous
 //   STORE    the product itself                                                                       (y, dx, dW)
 //   DHIDDEN  dh = dy Wd; dg = dh u act'(g), du = dh act(g), h = act(g) u                               B: columns contiguous
+//   LINEAR   a linear layer's: pre = x W^T + b, y = residual + gate act(pre) (and pre)                 A, B: contraction contiguous
 // An operand whose contraction index is contiguous ("K-major") is a box of 64 contraction elements by its rows; one whose row index is
 // contiguous ("MN-major": Wd in dh, Wg and Wu in dx, everything in dW) is read as it lies too, in boxes of 64 rows by 64 contraction
 // elements: the tensor cores take both, so nothing is transposed in memory.  Elements past an operand's end read as zero.
@@ -27,12 +28,22 @@
 #include "tc5_common.cuh"
 #include "k_vec.cuh"
 
-enum { FF_GATED = 0, FF_STORE = 1, FF_DHIDDEN = 2 };
+enum { FF_GATED = 0, FF_STORE = 1, FF_DHIDDEN = 2, FF_LINEAR = 3 };
+
+// What a linear layer does with its sums.
+struct LinearEpilogue {
+    const void* bias; const void* gate;     // nullptr: none.  gate: a row for each group of `group` rows
+    const void* residual; void* pre; void* y;       // (few rows, and the join of split contractions; tiles have maps)
+    long long gate_stride, residual_stride, y_stride, pre_stride;
+    int group;
+    int params_f32;                         // bias and gate are float32
+    int has_residual;
+};
 
 struct FfGemmParams {
     CUtensorMap a[3], b[3], out[3];     // operands of each product, or of each segment of the contraction; GATED: b = Wg, Wu
                                         // (DHIDDEN: out[0] is a map of dg, du, h as [3, rows, cols])
-    CUtensorMap in[2];                  // DHIDDEN: gate and up [rows, cols]
+    CUtensorMap in[2];                  // DHIDDEN: gate and up [rows, cols]; LINEAR: the residual
     int products;                       // products of this launch, each with tiles of its own ...
     int tile0[4];                       // ... from tile0[i] to tile0[i + 1]
     int rows[3], cols[3];               // of the output
@@ -45,6 +56,7 @@ struct FfGemmParams {
     int act, save;
     int early_b;                        // B may be read before the kernel before this one is done
     int* dev_status;
+    LinearEpilogue linear;
 };
 
 // NB: accumulators of 256 columns a tile.  1: a tile's epilogue runs under the next tile's MMAs; 2 (STORE, long contractions): tiles of 512
@@ -57,8 +69,9 @@ struct FfGemm {
     static constexpr int WARP_TMA = EPI_WARPS, WARP_MMA = EPI_WARPS + 1;
     static constexpr int THREADS = 32 * (EPI_WARPS + 2);
     static constexpr int MAX_STAGES = 8;
-    // per epilogue warp: two boxes of 32 rows x CW columns on their way out; DHIDDEN: two sets of three, two of them in and out
-    static constexpr int BOX = 64 * CW, STAGING = (EPI == FF_DHIDDEN ? 6 : 2) * BOX;
+    // per epilogue warp: two boxes of 32 rows x CW columns on their way out; DHIDDEN: two sets of three, two of them in and out; LINEAR: two sets of
+    // two, the residual in and y out, and pre
+    static constexpr int BOX = 64 * CW, SET = EPI == FF_DHIDDEN ? 3 : (EPI == FF_LINEAR ? 2 : 1), STAGING = 2 * SET * BOX;
     static constexpr int BAR_BYTES = 384;
     static constexpr int SMEM_MAX = 232448;
     // bn: columns of an accumulator; NB bn / CG columns of B in each thread block (in boxes of 64 where the operand is MN-major)
@@ -129,6 +142,10 @@ constexpr float FF_GELU_2A = 1.5957691216057308f, FF_GELU_B = 0.044715f, FF_LOG2
 // Two elements at a time (packed float32 arithmetic): a and, where asked for, a'.
 template <int ACT, bool SLOPE> __device__ __forceinline__ float2 ff_act2(float2 g, float2* slope) {
     const float2 one = make_float2(1.f, 1.f);
+    if constexpr (ACT == HF_ACT_NONE) {
+        if constexpr (SLOPE) *slope = one;
+        return g;
+    }
     // - log2(e) times the exponent
     float2 x;
     if constexpr (ACT == HF_ACT_SILU) x = fmul2(g, make_float2(-FF_LOG2E, -FF_LOG2E));
@@ -167,6 +184,23 @@ template <typename T, int ACT> __device__ __forceinline__ void ff_hidden_row(con
         g[j] = pack2<T>(dg.x, dg.y);
         u[j] = pack2<T>(du.x, du.y);
         h[j] = pack2<T>(o.x, o.y);
+    }
+}
+
+// Eight parameters of a linear layer, of T or float32, as floats.
+template <typename T> __device__ __forceinline__ void linear_params(const void* base, bool f32, long long at, float (&f)[8]) {
+    if (f32) to_floats(load_vec<float, 8>(static_cast<const float*>(base) + at), f);
+    else to_floats(load_vec<T, 8>(static_cast<const T*>(base) + at), f);
+}
+// Sums of eight neighbouring columns -> pre and y of that row (bias, gate, residual as floats).
+template <int ACT> __device__ __forceinline__ void linear_eight(float (&v)[8], float (&pre)[8], const float (&bias)[8], const float (&gate)[8], const float (&residual)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) {
+        const float2 s = fadd2(make_float2(v[j], v[j + 1]), make_float2(bias[j], bias[j + 1]));
+        pre[j] = s.x; pre[j + 1] = s.y;
+        const float2 a = ff_act2<ACT, false>(s, nullptr);
+        const float2 o = ffma2(a, make_float2(gate[j], gate[j + 1]), make_float2(residual[j], residual[j + 1]));
+        v[j] = o.x; v[j + 1] = o.y;
     }
 }
 
@@ -246,7 +280,7 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
     if (threadIdx.x == 0) {
         for (int s = 0; s < stages; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_free + 8 * s, 1); }
         for (int s = 0; s < 2; ++s) { mbar_init(bar_acc + 8 * s, 1); mbar_init(bar_acc_free + 8 * s, C::EPI_WARPS * CG); }
-        if (EPI == FF_DHIDDEN)
+        if (EPI == FF_DHIDDEN || EPI == FF_LINEAR)
             for (int s = 0; s < 2 * C::EPI_WARPS; ++s) mbar_init(bar_in + 8 * s, 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
@@ -389,16 +423,18 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
                     if (in_t < n_tiles) in_tile = ff_tile(p, in_t, CG * C::BM, bn_out);
                     continue;
                 }
-                const uint32_t b = in_bar + 8 * in_set, to = staging + in_set * 3 * C::BOX;
-                mbar_expect_tx(b, 2 * C::BOX);
+                const uint32_t b = in_bar + 8 * in_set, to = staging + in_set * C::SET * C::BOX;
+                mbar_expect_tx(b, (EPI == FF_DHIDDEN ? 2 : 1) * C::BOX);
                 tma_load_2d(to, &p.in[0], col, row, b);
-                tma_load_2d(to + C::BOX, &p.in[1], col, row, b);
+                if (EPI == FF_DHIDDEN) tma_load_2d(to + C::BOX, &p.in[1], col, row, b);
                 in_set ^= 1;
                 in_c += 2;
                 return;
             }
         };
-        if (EPI == FF_DHIDDEN && lane == 0) { pdl_wait(); ask(); }
+        const bool asks = EPI == FF_DHIDDEN || (EPI == FF_LINEAR && p.linear.has_residual && p.splits == 1);
+        if (EPI == FF_LINEAR || (asks && lane == 0)) pdl_wait();        // (LINEAR: all lanes read the parameters)
+        if (asks && lane == 0) ask();
         for (int t = tile_first; t < n_tiles; t += tile_step) {
             const FfTile tile = ff_tile(p, t, CG * C::BM, bn_out);
             if (!mbar_wait_warp<true>(bar_acc + 8 * acc, acc_phase, abort_flag, p.dev_status, 84)) break;
@@ -415,17 +451,87 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
                 const uint32_t at = lane_base + (acc + h2) * acc_stride + in;
                 uint32_t r[32], o[16];
                 tmem_ld32(at, r);
-                if constexpr (EPI == FF_STORE) {
-                    tmem_wait_ld();
+                if constexpr (EPI == FF_STORE || EPI == FF_LINEAR) {
+                    if (EPI == FF_STORE || p.splits > 1) tmem_wait_ld();
                     if (p.splits > 1) {             // [tile][split][32 rows][32 columns]: column by column, so that a warp's stores are whole lines
                         float* to = p.partials + ((((size_t)tile.index * p.splits + tile.split) * CG + rank) * 4 + quad) * 32 * p.bn + c * 1024 + lane;
 #pragma unroll
                         for (int j = 0; j < 32; ++j) to[32 * j] = __uint_as_float(r[j]);
                         continue;
                     }
+                }
+                if constexpr (EPI == FF_STORE) {
 #pragma unroll
                     for (int j = 0; j < 16; ++j) o[j] = pack2<T>(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
                     out.put(&p.out[tile.product], o, col, row, lane);
+                } else if constexpr (EPI == FF_LINEAR) {
+                    // the parameters on their way beside the sums and the residual's box
+                    const LinearEpilogue& e = p.linear;
+                    float bias[4][8], gate[4][8];
+                    const long long gate_at = e.gate ? (long long)((uint32_t)min(row + lane, p.rows[0] - 1) / (uint32_t)e.group) * e.gate_stride : 0;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) { bias[q][j] = 0.f; gate[q][j] = 1.f; }
+                        if (col + 8 * q < cols) {
+                            if (e.bias) linear_params<T>(e.bias, e.params_f32, col + 8 * q, bias[q]);
+                            if (e.gate) linear_params<T>(e.gate, e.params_f32, gate_at + col + 8 * q, gate[q]);
+                        }
+                    }
+                    uint32_t before[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) before[j] = 0u;
+                    const int set = use_n & 1;
+                    const uint32_t boxes = staging + set * C::SET * C::BOX;
+                    if (asks) {
+                        ok = mbar_wait_warp<true>(in_bar + 8 * set, (use_n >> 1) & 1, abort_flag, p.dev_status, 87);
+                        ++use_n;
+                        if (!ok) { tmem_wait_ld(); break; }
+                        ff_get_row(boxes, before, lane);
+                        if (lane == 0) {
+                            bulk_wait_read();       // the stores of the step before have read the other set
+                            ask();
+                        }
+                        __syncwarp();
+                    }
+                    tmem_wait_ld();
+                    uint32_t pre_row[16];
+                    auto eight = [&](auto act) {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            float v[8], pre[8], res[8];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(r[8 * q + j]);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const float2 f = unpack2<T>(before[4 * q + j]);
+                                res[2 * j] = f.x; res[2 * j + 1] = f.y;
+                            }
+                            linear_eight<decltype(act)::value>(v, pre, bias[q], gate[q], res);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                pre_row[4 * q + j] = pack2<T>(pre[2 * j], pre[2 * j + 1]);
+                                o[4 * q + j] = pack2<T>(v[2 * j], v[2 * j + 1]);
+                            }
+                        }
+                    };
+                    if (p.act == HF_ACT_NONE) eight(std::integral_constant<int, HF_ACT_NONE>());
+                    else if (p.act == HF_ACT_SILU) eight(std::integral_constant<int, HF_ACT_SILU>());
+                    else eight(std::integral_constant<int, HF_ACT_GELU_TANH>());
+                    if (asks) {
+                        ff_put_row(boxes, o, lane);                     // (each lane's row of y takes the place of its own row of the residual)
+                        if (p.save) ff_put_row(boxes + C::BOX, pre_row, lane);
+                        fence_proxy_async();
+                        __syncwarp();
+                        if (lane == 0) {
+                            tma_store_2d(&p.out[0], boxes, col, row);
+                            if (p.save) tma_store_2d(&p.out[1], boxes + C::BOX, col, row);
+                            bulk_commit();
+                        }
+                    } else {
+                        if (p.save) out.put(&p.out[1], pre_row, col, row, lane);
+                        out.put(&p.out[0], o, col, row, lane);
+                    }
                 } else if constexpr (EPI == FF_GATED) {
                     uint32_t u[32];
                     tmem_ld32(at + bn_out, u);
@@ -444,7 +550,7 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
                 } else {
                     uint32_t u[16], h[16];
                     const int set = use_n & 1;
-                    const uint32_t boxes = staging + set * 3 * C::BOX;
+                    const uint32_t boxes = staging + set * C::SET * C::BOX;
                     ok = mbar_wait_warp<true>(in_bar + 8 * set, (use_n >> 1) & 1, abort_flag, p.dev_status, 85);
                     ++use_n;
                     if (!ok) { tmem_wait_ld(); break; }
@@ -477,7 +583,7 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
             if (++acc == ACCS) { acc = 0; acc_phase ^= 1; }
         }
         if (lane == 0) bulk_wait_all();
-        if (EPI == FF_DHIDDEN && *abort_flag) {         // boxes in flight land before the thread block leaves
+        if ((EPI == FF_DHIDDEN || EPI == FF_LINEAR) && *abort_flag) {         // boxes in flight land before the thread block leaves
             const long long t0 = clock64();
             while (clock64() - t0 < 400000) {}
         }
@@ -491,9 +597,30 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
     }
 }
 
+// The epilogue of eight neighbouring sums of a row, straight from and to memory.
+template <typename T>
+__device__ __forceinline__ void linear_row(const LinearEpilogue& e, int act, int row, int col, float (&v)[8]) {
+    float bias[8], gate[8], residual[8], pre[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) { bias[j] = 0.f; gate[j] = 1.f; residual[j] = 0.f; }
+    if (e.bias) linear_params<T>(e.bias, e.params_f32, col, bias);
+    if (e.gate) linear_params<T>(e.gate, e.params_f32, (long long)((uint32_t)row / (uint32_t)e.group) * e.gate_stride + col, gate);
+    if (e.residual) to_floats(load_vec<T, 8>(static_cast<const T*>(e.residual) + row * e.residual_stride + col), residual);
+    if (act == HF_ACT_NONE) linear_eight<HF_ACT_NONE>(v, pre, bias, gate, residual);
+    else if (act == HF_ACT_SILU) linear_eight<HF_ACT_SILU>(v, pre, bias, gate, residual);
+    else linear_eight<HF_ACT_GELU_TANH>(v, pre, bias, gate, residual);
+    Vec<T, 8> o;
+    from_floats(o, v);
+    store_vec(static_cast<T*>(e.y) + row * e.y_stride + col, o);
+    if (e.pre) {
+        from_floats(o, pre);
+        store_vec(static_cast<T*>(e.pre) + row * e.pre_stride + col, o);
+    }
+}
+
 // out = the sum over the splits of the partials of k_ff_gemm, in order, rounded once.  A warp takes 32 rows x 8 columns.
 struct FfJoinOut { void* out[3]; long long stride[3]; int cg; };
-template <typename T>
+template <typename T, bool LINEAR = false>
 __global__ void __launch_bounds__(128)
 k_ff_join(const __grid_constant__ FfGemmParams p, const FfJoinOut o) {
     const int lane = threadIdx.x & 31, eights = p.bn / 8, units = 4 * o.cg * eights;
@@ -512,6 +639,7 @@ k_ff_join(const __grid_constant__ FfGemmParams p, const FfJoinOut o) {
     for (int s = 0; s < p.splits; ++s, from += step)
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] += from[32 * j];
+    if constexpr (LINEAR) { linear_row<T>(p.linear, p.act, row, col, v); return; }
     T* to = static_cast<T*>(o.out[tile.product]) + (size_t)row * o.stride[tile.product] + col;
     *reinterpret_cast<uint4*>(to) = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
 }

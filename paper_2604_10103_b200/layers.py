@@ -1,9 +1,9 @@
-"""The operators of a denoiser block around the hybrid attention, on torch CUDA tensors: layer norm, rotary positions with several axes,
-gated feed-forward, forward and backward.  Each is one call of the library (include/hf.h) on the current stream; outputs and workspaces
+"""The operators of a denoiser block around the hybrid attention, on torch CUDA tensors: layer norm, rotary positions with several axes (with norms of
+q and k or without), gated feed-forward, linear layers with their epilogue, forward and backward.  Each is one call of the library (include/hf.h) on the current stream; outputs and workspaces
 come from torch's allocator.  There is no fallback: a tensor the library does not take raises.
 
-Where gradients are recorded and an input needs one, `layer_norm`, `rope_axes`, `split_heads_rope` and `gated_ff` are part of torch's graph,
-their backward passes the `*_backward` calls below (which may also be called by hand); a second derivative raises.
+Where gradients are recorded and an input needs one, `layer_norm`, `rope_axes`, `split_heads_rope`, `split_heads_norm_rope`, `gated_ff` and `linear` are part of torch's
+graph, their backward passes the `*_backward` calls below (which may also be called by hand); a second derivative raises.
 
 The short calls are bound by the host, so the way to the library is kept short: the shapes are packed as the bytes of the C structures,
 tensors are asked for nothing twice, and outputs come from the cheapest of torch's ways to make one (empty_like and new_empty with plain
@@ -23,6 +23,7 @@ _TYPES = {torch.bfloat16: hf.HF_BF16, torch.float16: hf.HF_F16, torch.float32: h
 _PAIRINGS = {"adjacent": hf.HF_PAIRS_ADJACENT, "halves": hf.HF_PAIRS_HALVES}
 _OVERS = {"head": hf.HF_NORM_OVER_HEAD, "width": hf.HF_NORM_OVER_WIDTH}
 _ACTS = {"silu": hf.HF_ACT_SILU, "gelu_tanh": hf.HF_ACT_GELU_TANH}
+_LINEAR_ACTS = {None: hf.HF_ACT_NONE, **_ACTS}
 _NORM = struct.Struct("@3i6q2f").pack                       # hf_norm_shape
 _ROPE = struct.Struct("@5i4i4i2iq").pack                    # hf_rope_shape
 _ROPE_TENSOR = struct.Struct("@2P6q2i").pack                # hf_rope_tensor
@@ -30,6 +31,7 @@ _ROPE_TENSORS = struct.Struct("@2P6q2i2P6q2i2P6q2i").pack   # three of them
 _HEADS = struct.Struct("@18if5q").pack                      # hf_heads_shape
 _HEADS_TENSORS = struct.Struct("@P3qP3qP3q").pack           # three hf_heads_tensor
 _FF = struct.Struct("@2iq3i2q").pack                        # hf_ff_shape
+_LINEAR = struct.Struct("@5i6q").pack                       # hf_linear_shape
 _F32, _I32 = torch.float32, torch.int32
 _empty_like, _empty_strided = torch.empty_like, torch.empty_strided
 _lib, _stream, _check = hf.lib, hf._stream, hf._check
@@ -543,3 +545,111 @@ class _GatedFF(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dy, *_):
         return *gated_ff_backward(dy.contiguous(), *ctx.saved_tensors, ctx.act), None, None
+
+
+# ------------------------------------------------------------------------------------------------ linear layers
+def _linear_operands(x, weight, bias, act, gate, rows_per_group):
+    """(device, type, type of the parameters, act, rows, width, out_width, row stride of x, of the gate, rows of a group) of checked operands."""
+    dev = _current("x", x)
+    rows, width, stride = _rows("x", x)
+    dtype = x.dtype
+    if dtype is not torch.bfloat16 and dtype is not torch.float16:
+        _fail(f"x is {dtype}: bfloat16 and float16 are taken")
+    if act not in _LINEAR_ACTS:
+        _fail(f"act {act!r} unknown")
+    if weight.dim() != 2:
+        _fail("weight is a matrix")
+    out_width = weight.shape[0]
+    if not (weight.dtype is dtype and weight.shape == (out_width, width) and weight.get_device() == dev and weight.is_contiguous()):
+        _dense("weight", weight, dev, (out_width, width), dtype)
+    kind, gate_stride, group = dtype, out_width, 0
+    if bias is not None:
+        kind = bias.dtype
+        if kind != dtype and kind != _F32:
+            _fail(f"bias is {kind}: x's type or float32 is taken")
+        _dense("bias", bias, dev, (out_width,), kind)
+    if gate is not None:
+        group = rows_per_group if rows_per_group > 0 else 0
+        gate_kind, gate_stride = _norm_param("gate", gate, dev, dtype, out_width, -(-rows // group) if group else 1)
+        if bias is not None and gate_kind != kind:
+            _fail("bias and gate differ in their type")
+        kind = gate_kind
+    return dev, _TYPES[dtype], _TYPES[kind], _LINEAR_ACTS[act], rows, width, out_width, stride, gate_stride, group
+
+
+@functools.lru_cache(maxsize=256)
+def _linear_workspace(dev, shape, backward):
+    return hf.hf_linear_workspace(shape, backward)
+
+
+def linear(x, weight, bias=None, act=None, gate=None, residual=None, rows_per_group=0, save=False):
+    """y = residual + gate * act(x weight^T + bias).  x bf16 or f16 [..., width], rows with one common stride; weight [out_width, width] contiguous; bias
+    [out_width] of x's type or float32; act None, "silu" or "gelu_tanh"; gate of the bias's types [out_width] or [1, out_width], with rows_per_group
+    > 0 [groups, out_width], row r of x taking row r // rows_per_group (slices of a modulation tensor are fine); residual [..., out_width] of x's
+    type, rows with one common stride.  save: returns (y, pre), pre = x weight^T + bias [rows, out_width] for `linear_backward`."""
+    if _recording() and (x.requires_grad or weight.requires_grad or bias is not None and bias.requires_grad or gate is not None and gate.requires_grad
+                         or residual is not None and residual.requires_grad):
+        return _Linear.apply(x, weight, bias, act, gate, residual, rows_per_group, save)
+    dev, t, pt, a, rows, width, out_width, stride, gate_stride, group = _linear_operands(x, weight, bias, act, gate, rows_per_group)
+    residual_stride = out_width
+    if residual is not None:
+        _like("residual", residual, dev, x.shape[:-1] + (out_width,), x.dtype)
+        residual_stride = _rows("residual", residual)[2]
+    y = _empty_like(x) if out_width == width == stride else x.new_empty(x.shape[:-1] + (out_width,))
+    pre = x.new_empty(rows, out_width) if save else None
+    shape = _LINEAR(t, pt, a, width, out_width, rows, stride, out_width, residual_stride, group, gate_stride)
+    need = _linear_workspace(dev, shape, 0)
+    ws = x.new_empty(need // 2) if need else None
+    status = _lib().hf_linear(shape, x.data_ptr(), weight.data_ptr(), bias.data_ptr() if bias is not None else None,
+                              gate.data_ptr() if gate is not None else None, residual.data_ptr() if residual is not None else None, y.data_ptr(),
+                              pre.data_ptr() if save else None, ws.data_ptr() if need else None, _stream())
+    if status:
+        _check(status)
+    return (y, pre) if save else y
+
+
+def linear_backward(dy, x, weight, pre=None, act=None, gate=None, rows_per_group=0, dx=True, dweight=True, dbias=True, dgate=True):
+    """Gradients of `linear`: (dx, dweight in x's type, dbias float32 [out_width], dgate float32 [groups, out_width]); None for those not asked for (dgate:
+    without a gate).  pre: as the forward returned it, needed with an activation or a gate.  The residual's gradient is dy."""
+    dev, t, pt, a, rows, width, out_width, stride, gate_stride, group = _linear_operands(x, weight, None, act, gate, rows_per_group)
+    _like("dy", dy, dev, x.shape[:-1] + (out_width,), x.dtype)
+    if act is not None or gate is not None:
+        if pre is None:
+            _fail("pre is needed with an activation or a gate")
+        _dense("pre", pre, dev, (rows, out_width), x.dtype)
+    gx = (_empty_like(x) if stride == width else x.new_empty(x.shape)) if dx else None
+    gw = _empty_like(weight) if dweight else None
+    gb = _empty_strided((out_width,), (1,), dtype=_F32, device=x.device) if dbias else None
+    gg = _empty_strided((-(-rows // group) if group else 1, out_width), (out_width, 1), dtype=_F32, device=x.device) if dgate and gate is not None else None
+    shape = _LINEAR(t, pt, a, width, out_width, rows, stride, _rows("dy", dy)[2], out_width, group, gate_stride)
+    ws = x.new_empty(_linear_workspace(dev, shape, 1) // 2)
+    status = _lib().hf_linear_backward(shape, dy.data_ptr(), x.data_ptr(), weight.data_ptr(), pre.data_ptr() if pre is not None else None,
+                                       gate.data_ptr() if gate is not None else None, gx.data_ptr() if dx else None, gw.data_ptr() if dweight else None,
+                                       gb.data_ptr() if dbias else None, gg.data_ptr() if gg is not None else None, ws.data_ptr(), _stream())
+    if status:
+        _check(status)
+    return gx, gw, gb, gg
+
+
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, act, gate, residual, rows_per_group, save):
+        kept = act is not None or gate is not None
+        y, pre = linear(x, weight, bias, act, gate, residual, rows_per_group, True) if save or kept else (linear(x, weight, bias, None, None, residual), None)
+        ctx.save_for_backward(x, weight, gate, pre if kept else None)
+        ctx.args, ctx.bias = (act, rows_per_group), None if bias is None else bias.dtype
+        if not save:
+            return y
+        ctx.mark_non_differentiable(pre)
+        ctx.set_materialize_grads(False)
+        return y, pre
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, *_):
+        x, weight, gate, pre = ctx.saved_tensors
+        act, group = ctx.args
+        need = ctx.needs_input_grad
+        dy = dy.contiguous()
+        dx, dw, db, dg = linear_backward(dy, x, weight, pre, act, gate, group, need[0], need[1], need[2], need[4])
+        return (dx, dw, db.to(ctx.bias) if need[2] else None, None, dg.view(gate.shape).to(gate.dtype) if need[4] else None, dy if need[5] else None, None, None)
