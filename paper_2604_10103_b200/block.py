@@ -3,8 +3,9 @@ attention, output projection; modulated layer norm, gated feed-forward; a gated 
 
 `DenoiserBlock.forward` is one layer of one denoising step of a stream (no gradient), `commit` folds a finished chunk into the layer's cache and
 state, and `forward` under autograd is the step with gradient: every operator between the projections has its backward pass in the
-library, and the plain projections are torch's.  `python -m paper_2604_10103_b200.block` runs a short stream and one training step at the
-832x480 shape on synthetic data and prints their times.
+library, and the plain projections are torch's.  `BiasedBlock` is a block with biases, norms of q and k and a feed-forward of two matrices, whose
+projections are the library's too, with their gates and residuals.  `python -m paper_2604_10103_b200.block` runs a short stream and one training step of
+either at the 832x480 shape on synthetic data, of the second with `optim.gradient_norm` and `optim.AdamW`, and prints their times.
 """
 from __future__ import annotations
 
@@ -14,6 +15,7 @@ from torch.autograd.function import once_differentiable
 from . import binding as hf
 from . import inputs as gen
 from . import layers
+from . import optim
 from . import rope
 
 
@@ -73,13 +75,7 @@ class DenoiserBlock(torch.nn.Module):
         if (c.batch, c.heads, c.head_dim, c.tokens_per_frame * c.chunk_frames) != (w.batch, w.heads, w.head_dim, w.chunk_tokens):
             raise ValueError("the context's batch, heads, head_dim or tokens of a chunk are not the workload's")
         self.w, self.context, self.layer, self.act, self.eps = w, context, layer, act, eps
-        width = w.heads * w.head_dim
-        hidden = hidden or (8 * width // 3 + 63) // 64 * 64
-
-        def matrix(n_out, n_in):
-            return torch.nn.Parameter(torch.randn(n_out, n_in, device=device).mul_(n_in ** -0.5).to(dtype))
-        self.w_qkv, self.w_out = matrix(3 * width, width), matrix(width, width)
-        self.w_gate, self.w_up, self.w_down = matrix(hidden, width), matrix(hidden, width), matrix(width, hidden)
+        self._make_weights(w.heads * w.head_dim, hidden, device, dtype)
         n = w.head_dim // 2
         self.pairs, self.extents = (n - 2 * (n // 3), n // 3, n // 3), (last_frame + 1, high, wide)
         cos, sin = rope.axis_tables(self.extents, self.pairs)
@@ -87,6 +83,15 @@ class DenoiserBlock(torch.nn.Module):
         self.register_buffer("sin", torch.from_numpy(sin).to(device))
         grid = torch.meshgrid(torch.arange(w.chunk_frames), torch.arange(high), torch.arange(wide), indexing="ij")
         self.register_buffer("pos", torch.stack([g.reshape(-1) for g in grid], dim=1).to(torch.int32).to(device))
+
+    @staticmethod
+    def _matrix(n_out, n_in, device, dtype):
+        return torch.nn.Parameter(torch.randn(n_out, n_in, device=device).mul_(n_in ** -0.5).to(dtype))
+
+    def _make_weights(self, width, hidden, *how):
+        hidden = hidden or (8 * width // 3 + 63) // 64 * 64
+        self.w_qkv, self.w_out = self._matrix(3 * width, width, *how), self._matrix(width, width, *how)
+        self.w_gate, self.w_up, self.w_down = self._matrix(hidden, width, *how), self._matrix(hidden, width, *how), self._matrix(width, hidden, *how)
 
     def positions(self, first_frame):
         """Positions of the chunk whose first frame is the stream's frame `first_frame` (from 0)."""
@@ -109,20 +114,25 @@ class DenoiserBlock(torch.nn.Module):
         _bf16("x", x)
         if x.get_device() != self.context.device:
             raise ValueError(f"x is on {x.device}, the context on device {self.context.device}")
-        h = self._norm(x, mod[:, :, 1], mod[:, :, 0])
+        return self._split(self._norm(x, mod[:, :, 1], mod[:, :, 0]), pos, (self.cos, self.sin, self.extents, self.pairs))
+
+    def _split(self, h, pos, tables):
         qkv = torch.nn.functional.linear(h, self.w_qkv)
         _bf16("the projection", qkv)            # (autocast may have changed its type)
-        return layers.split_heads_rope(qkv, self.w.heads, self.w.heads, pos, (self.cos, self.sin, self.extents, self.pairs))
+        return layers.split_heads_rope(qkv, self.w.heads, self.w.heads, pos, tables)
+
+    def _attend(self, x, mod, pos):
+        q, k, v = self._heads(x, mod, pos)
+        if torch.is_grad_enabled() and q.requires_grad:
+            return _Attention.apply(q, k, v, self.context, self.layer)
+        o = torch.empty_like(q)
+        self.context.hf_hybrid_forward(self.layer, q, k, v, o)
+        return o
 
     def forward(self, x, mod, pos):
         """x [batch, tokens of a chunk, width]; mod [batch, frames of the chunk, 6, width]: shift, scale, gate of the attention half, then of the
         feed-forward's; pos: `positions` of the chunk's first frame."""
-        q, k, v = self._heads(x, mod, pos)
-        if torch.is_grad_enabled() and q.requires_grad:
-            o = _Attention.apply(q, k, v, self.context, self.layer)
-        else:
-            o = torch.empty_like(q)
-            self.context.hf_hybrid_forward(self.layer, q, k, v, o)
+        o = self._attend(x, mod, pos)
         per_token = mod.repeat_interleave(self.w.tokens_per_frame, dim=1)
         x = x + per_token[:, :, 2] * torch.nn.functional.linear(o.transpose(1, 2).flatten(2), self.w_out)
         h = self._norm(x, mod[:, :, 4], mod[:, :, 3])
@@ -134,6 +144,46 @@ class DenoiserBlock(torch.nn.Module):
         """The finished chunk's keys and values go into the layer's cache (and the oldest chunk into its state)."""
         _, k, v = self._heads(x, mod, pos)
         self.context.hf_kv_append(self.layer, k, v)
+
+
+class BiasedBlock(DenoiserBlock):
+    """A block of the layout of Wan2.1's (without its attention to a prompt): projections with biases, RMS norms of q and k with a weight, over all
+    heads of a token (norm_over "width") or each head ("head"), and a feed-forward of two matrices with biases.  hidden: 4 times the width."""
+
+    def __init__(self, w, high, wide, context, layer=0, hidden=None, act="gelu_tanh", norm_over="width", **kw):
+        if norm_over not in ("width", "head"):
+            raise ValueError(f"norm_over {norm_over!r}: \"width\" and \"head\" are taken")
+        self._norm_over = norm_over             # (before the module's own construction, which calls _make_weights)
+        super().__init__(w, high, wide, context, layer, hidden, act, **kw)
+
+    def _make_weights(self, width, hidden, *how):
+        hidden = hidden or 4 * width
+        device, dtype = how
+
+        def row(n, value):
+            return torch.nn.Parameter(torch.full((n,), value, device=device, dtype=dtype))
+        n = width if self._norm_over == "width" else self.w.head_dim
+        self.w_qkv, self.b_qkv = self._matrix(3 * width, width, *how), row(3 * width, 0.0)
+        self.q_norm, self.k_norm = row(n, 1.0), row(n, 1.0)
+        self.w_out, self.b_out = self._matrix(width, width, *how), row(width, 0.0)
+        self.w_first, self.b_first = self._matrix(hidden, width, *how), row(hidden, 0.0)
+        self.w_second, self.b_second = self._matrix(width, hidden, *how), row(width, 0.0)
+
+    def _split(self, h, pos, tables):
+        heads = self.w.heads
+        qkv = layers.linear(h, self.w_qkv, self.b_qkv)
+        return layers.split_heads_norm_rope(qkv, heads, heads, self.q_norm, self.k_norm, pos, tables, eps=self.eps, over=self._norm_over)
+
+    def _half(self, x, y, weight, bias, gate):
+        """x + gate (y weight^T + bias), one row of the gate [batch, frames, width] for the tokens of a frame."""
+        return layers.linear(y, weight, bias, gate=gate.reshape(-1, x.shape[-1]), residual=x, rows_per_group=self.w.tokens_per_frame)
+
+    def forward(self, x, mod, pos):
+        """As `DenoiserBlock.forward`."""
+        o = self._attend(x, mod, pos)
+        x = self._half(x, o.transpose(1, 2).flatten(2), self.w_out, self.b_out, mod[:, :, 2])
+        h = layers.linear(self._norm(x, mod[:, :, 4], mod[:, :, 3]), self.w_first, self.b_first, act=self.act)
+        return self._half(x, h, self.w_second, self.b_second, mod[:, :, 5])
 
 
 def main():
@@ -171,6 +221,16 @@ def main():
         block.zero_grad(set_to_none=True)
         block(x, mod, pos).float().square().mean().backward()
     print(f"the same with gradient: {timed(step):.3f} ms")
+    block = BiasedBlock(w, 30, 52, context)
+    with torch.no_grad():
+        print(f"a layer with biases, norms of q and k and two matrices of feed-forward: {timed(lambda: block(x, mod, pos)):.3f} ms")
+    optimizer = optim.AdamW(block.parameters(), lr=1e-4)
+
+    def train():
+        step()
+        _, factor = optim.gradient_norm([p.grad for p in block.parameters()], max_norm=1.0)
+        optimizer.step(grad_factor=factor)
+    print(f"the same with gradient: {timed(step):.3f} ms, and a step of AdamW: {timed(train):.3f} ms")
     context.hf_get_device_status()
     hf.hf_layers_status()
 
