@@ -55,12 +55,13 @@ HeadsPlan heads_plan(const hf_heads_shape* g, bool wide) {
     p.threads = 32 * p.warps * p.teams;
     return p;
 }
-// Backward: thread blocks for q, k, v, by what they move (x, dy, dx; v: dy, dx).
+// Backward: thread blocks for q, k, v, by the time that they take (a head of v, which is copied, a quarter of one of q; by what they move it would be two
+// thirds: 161 us instead of 144 for 32760 tokens of 12 + 24 heads of 128).
 void heads_blocks(const hf_heads_shape* g, const HeadsPlan& n, int sms, int (&blocks)[3]) {
-    const long long rows = (long long)g->batch * g->tokens, all = (rows + n.teams - 1) / n.teams, total = (long long)sms * ((n.big ? 512 : 384) / n.threads);
-    const long long part[3] = {3LL * g->heads, 3LL * g->kv_heads, 2LL * g->kv_heads}, sum = part[0] + part[1] + part[2];
-    for (int i = 0; i < 3; ++i) {
-        long long b = (total * part[i] + sum - 1) / sum;
+    const long long rows = (long long)g->batch * g->tokens, all = (rows + n.teams - 1) / n.teams, total = (long long)sms * ((n.big ? 512 : 256) / n.threads);
+    const long long part[3] = {4LL * g->heads, 4LL * g->kv_heads, 1LL * g->kv_heads}, sum = part[0] + part[1] + part[2];
+    for (int i = 0; i < 3; ++i) {           // (rounded down: one thread block too many would wait for the others' end)
+        long long b = total * part[i] / sum;
         if (b > all) b = all;
         blocks[i] = b < 1 ? 1 : (int)b;
     }
@@ -74,8 +75,22 @@ hf_status launch_heads(const Device* d, const HeadsParams& p, const HeadsPlan& n
         k_heads<T, HALVES, WIDE, HB, BIG><<<dim3((unsigned)((rows + n.teams - 1) / n.teams), 3), n.threads, 0, st>>>(p);
     } else {
         struct Key {};
-        if (smem > 48 * 1024) HFL_TRY(allow_shared<Key>(d, k_heads_bwd<T, HALVES, WIDE, HB, BIG>, 16384 * 4));
-        k_heads_bwd<T, HALVES, WIDE, HB, BIG><<<p.blocks[0] + p.blocks[1] + p.blocks[2], n.threads, smem, st>>>(p);
+        const unsigned grid = p.blocks[0] + p.blocks[1] + p.blocks[2];
+        if constexpr (WIDE && !BIG) {
+            constexpr int MOST = 6144 * 4 + 4 * HEADS_SETS * (1024 + 2 * HB * 256 * sizeof(T));  // a row of the weight; four warps' angles and slots
+            smem += n.threads / 32 * HEADS_SETS * (32 * n.lanes + 2 * HB * 256 * (int)sizeof(T));
+            if (p.over_width) {
+                HFL_TRY(allow_shared<Key>(d, k_heads_bwd_ring<T, HALVES, HB, true>, MOST));
+                k_heads_bwd_ring<T, HALVES, HB, true><<<grid, n.threads, smem, st>>>(p);
+            } else {
+                struct HeadKey {};
+                HFL_TRY(allow_shared<HeadKey>(d, k_heads_bwd_ring<T, HALVES, HB, false>, MOST));
+                k_heads_bwd_ring<T, HALVES, HB, false><<<grid, n.threads, smem, st>>>(p);
+            }
+        } else {
+            if (smem > 48 * 1024) HFL_TRY(allow_shared<Key>(d, k_heads_bwd<T, HALVES, WIDE, HB, BIG>, 16384 * 4));
+            k_heads_bwd<T, HALVES, WIDE, HB, BIG><<<grid, n.threads, smem, st>>>(p);
+        }
     }
     HFL_CUDA(cudaGetLastError());
     return HF_OK;
