@@ -27,20 +27,32 @@ hf_status grid_for(const Device* d, F kernel, int threads, unsigned chunks, unsi
     return HF_OK;
 }
 
+// Elements of a chunk: 2048 (a block of 256 for each warp) where that gives every multiprocessor few of them, up to 8192 (what a chunk takes to look up is
+// then spread over four blocks a warp).
+constexpr int MOST_CHUNK = 8192;
+int adamw_chunk(const Device* d, const hf_adamw_tensor* t, int n) {
+    long long all = 0;
+    for (int i = 0; i < n; ++i) all += t[i].n;
+    int chunk = 2048;
+    while (chunk < MOST_CHUNK && all / chunk > 16LL * d->sm_count) chunk *= 2;
+    return chunk;
+}
+
 template <typename P, typename G, bool MASTER, bool BITS8, int CAP>
 hf_status launch_adamw(const Device* d, const hf_adamw_step* g, const hf_adamw_tensor* t, int n, cudaStream_t st) {
     AdamParams<CAP> a;
     a.beta1 = (float)g->beta1; a.beta2 = (float)g->beta2; a.rest1 = (float)(1. - g->beta1); a.rest2 = (float)(1. - g->beta2);
     a.ln1 = std::log(g->beta1); a.ln2 = std::log(g->beta2); a.eps = (float)g->eps; a.seed = g->seed; a.factor = g->factor; a.counter = g->counter;
     a.n_tensors = 0; a.chunks = 0;
+    a.chunk = adamw_chunk(d, t, n);
     for (int i = 0; i < n; ++i) {
         if (t[i].n == 0 && !t[i].step) continue;                        // (a tensor of no elements has its step counted)
         OptimTensor& o = a.t[a.n_tensors++];
         o.p = t[i].p; o.g = t[i].g; o.master = t[i].master; o.m = t[i].m; o.v = t[i].v; o.scales = reinterpret_cast<float2*>(t[i].scales);
         o.step = t[i].step; o.lr_at = t[i].lr_at; o.n = t[i].n; o.first_block = t[i].first_block; o.chunk0 = a.chunks;
         o.lr = (float)t[i].lr; o.decay = (float)t[i].weight_decay;
-        o.wide = aligned(o.p, 16) && aligned(o.g, 16) && aligned(o.master, 16) && aligned(o.m, 16) && aligned(o.v, 16);
-        a.chunks += (unsigned)((t[i].n + OPTIM_CHUNK - 1) / OPTIM_CHUNK);
+        o.wide = aligned(o.p, 8 * sizeof(P)) && aligned(o.g, 8 * sizeof(G)) && aligned(o.master, 32) && aligned(o.m, BITS8 ? 8 : 32) && aligned(o.v, BITS8 ? 8 : 32);
+        a.chunks += (unsigned)((t[i].n + a.chunk - 1) / a.chunk);
     }
     if (a.n_tensors == 0) return HF_OK;
     auto kernel = k_adamw<P, G, MASTER, BITS8, CAP>;
@@ -76,7 +88,7 @@ hf_status adamw_check(const hf_adamw_step* g, const hf_adamw_tensor* t, int n) {
     if (!aligned(g->factor, 4)) return fail(HF_ERR_INVALID_ARG, "factor is not aligned");
     const int pe = element_bytes(g->param_type), ge = element_bytes(g->grad_type), se = g->state_bits == 8 ? 1 : 4;
     bool first = true, master = false, counted = false;
-    long long chunks = 0;
+    long long elements = 0;
     for (int i = 0; i < n; ++i) {
         const hf_adamw_tensor& o = t[i];
         if (o.n < 0) return fail(HF_ERR_SHAPE, "tensor %d: %lld elements", i, (long long)o.n);
@@ -90,8 +102,8 @@ hf_status adamw_check(const hf_adamw_step* g, const hf_adamw_tensor* t, int n) {
         if (o.master && g->param_type == HF_F32) return fail(HF_ERR_INVALID_ARG, "tensor %d: a float32 parameter has no master", i);
         if (first) { first = false; master = o.master != nullptr; }
         else if (master != (o.master != nullptr)) return fail(HF_ERR_INVALID_ARG, "the tensors of a call have masters together or not at all");
-        chunks += (o.n - 1) / OPTIM_CHUNK + 1;
-        if (o.n > (1LL << 43) || chunks > MOST_CHUNKS) return fail(HF_ERR_SHAPE, "more than 2^43 elements");
+        elements += o.n;
+        if (o.n > (1LL << 43) || elements > (1LL << 43)) return fail(HF_ERR_SHAPE, "more than 2^43 elements");
     }
     if (counted && (!g->counter || !aligned(g->counter, 4))) return fail(HF_ERR_INVALID_ARG, "counter is null or not aligned");
     return HF_OK;

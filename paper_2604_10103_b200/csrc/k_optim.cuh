@@ -20,12 +20,13 @@ struct OptimTensor {
     long long first_block;                  // the first block's place in the hash
     unsigned chunk0;                        // chunks of the tensors before
     float lr, decay;
-    int wide;                               // p and g (and the states) take 16-byte accesses
+    int wide;                               // eight elements of each tensor take one access
 };
-constexpr int OPTIM_BLOCK = 256, OPTIM_CHUNK = 8192, OPTIM_WARPS = 8;
+constexpr int OPTIM_BLOCK = 256, OPTIM_WARPS = 8, OPTIM_BLOCKS = 4;
 template <int CAP> struct AdamParams {
     int n_tensors;
     unsigned chunks;
+    int chunk;                              // elements of a chunk: a multiple of a thread block's 2048
     float beta1, beta2, rest1, rest2;       // rest: 1 - beta
     double ln1, ln2;                        // logarithms of the betas
     float eps;
@@ -35,32 +36,39 @@ template <int CAP> struct AdamParams {
     OptimTensor t[CAP];
 };
 
-// Eight neighbours as floats; beyond `left` elements 0.
-template <typename T> __device__ __forceinline__ void optim_load(const T* p, bool wide, int left, float (&f)[8]) {
-    if (wide && left >= 8) to_floats(load_vec<T, 8>(p), f);
+// Eight neighbours as floats; FULL: in one access of 16 or 32 bytes (two of 16 would each touch half of every 32 bytes: 575 us instead of 529 for
+// the four layers' step), otherwise one by one, beyond `left` elements 0.
+template <bool FULL, typename T> __device__ __forceinline__ void optim_load(const T* p, int left, float (&f)[8]) {
+    if constexpr (FULL && sizeof(T) == 4)
+        asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n" : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3]), "=f"(f[4]), "=f"(f[5]),
+                     "=f"(f[6]), "=f"(f[7]) : "l"(p) : "memory");
+    else if constexpr (FULL) to_floats(load_vec<T, 8>(p), f);
     else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) f[j] = j < left ? to_float(p[j]) : 0.f;
     }
 }
-template <typename T> __device__ __forceinline__ void optim_store(T* p, bool wide, int left, const float (&f)[8]) {
-    if (wide && left >= 8) { Vec<T, 8> o; from_floats(o, f); store_vec(p, o); }
+template <bool FULL, typename T> __device__ __forceinline__ void optim_store(T* p, int left, const float (&f)[8]) {
+    if constexpr (FULL && sizeof(T) == 4)
+        asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};\n" ::"l"(p), "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]),
+                     "f"(f[6]), "f"(f[7]) : "memory");
+    else if constexpr (FULL) { Vec<T, 8> o; from_floats(o, f); store_vec(p, o); }
     else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (j < left) p[j] = from_float<T>(f[j]);
     }
 }
-__device__ __forceinline__ uint2 optim_load_codes(const uint8_t* p, bool wide, int left) {
-    if (wide && left >= 8) return *reinterpret_cast<const uint2*>(p);
+template <bool FULL> __device__ __forceinline__ uint2 optim_load_codes(const uint8_t* p, int left) {
+    if constexpr (FULL) return *reinterpret_cast<const uint2*>(p);
     uint32_t w[2] = {0, 0};
 #pragma unroll
     for (int j = 0; j < 8; ++j)
         if (j < left) w[j >> 2] |= (uint32_t)p[j] << 8 * (j & 3);
     return make_uint2(w[0], w[1]);
 }
-__device__ __forceinline__ void optim_store_codes(uint8_t* p, bool wide, int left, uint2 c) {
-    if (wide && left >= 8) { *reinterpret_cast<uint2*>(p) = c; return; }
+template <bool FULL> __device__ __forceinline__ void optim_store_codes(uint8_t* p, int left, uint2 c) {
+    if constexpr (FULL) { *reinterpret_cast<uint2*>(p) = c; return; }
     const uint32_t w[2] = {c.x, c.y};
 #pragma unroll
     for (int j = 0; j < 8; ++j)
@@ -84,8 +92,8 @@ template <bool E5> __device__ __forceinline__ void optim_decode(uint2 c, float s
     const uint32_t w[4] = {c.x & 0xffffu, c.x >> 16, c.y & 0xffffu, c.y >> 16};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const float2 v = optim_decode<E5>(w[j]);
-        f[2 * j] = v.x * scale; f[2 * j + 1] = v.y * scale;
+        const float2 v = fmul2(optim_decode<E5>(w[j]), make_float2(scale, scale));
+        f[2 * j] = v.x; f[2 * j + 1] = v.y;
     }
 }
 // An invertible mix of 32 bits.
@@ -94,26 +102,115 @@ __device__ __forceinline__ uint32_t optim_mix(uint32_t x) {
     x = (x ^ (x >> 15)) * 0x846ca68bu;
     return x ^ (x >> 16);
 }
-// y >= 0 without the last DROP bits of its mantissa, or of numbers below `least`, the type's smallest normal one, as many as there: they are next to it.  Up
-// where what is cut off and 16 random bits of the same weight carry.
-template <int DROP> __device__ __forceinline__ float optim_up_or_down(float y, uint32_t bits16, float least) {
-    const float off = y < least ? least : 0.f;
-    return __uint_as_float((__float_as_uint(y + off) + (bits16 << (DROP - 16))) & ~((1u << DROP) - 1u)) - off;
+// y >= 0, two at a time, without the last DROP bits of its mantissa, or of numbers below `least`, the type's smallest normal one, as many as there: they
+// are next to it.  Up where what is cut off and 16 random bits of the same weight carry.
+template <int DROP> __device__ __forceinline__ float2 optim_up_or_down(float2 y, uint32_t bits0, uint32_t bits1, float least) {
+    const float2 off = make_float2(y.x < least ? least : 0.f, y.y < least ? least : 0.f), z = fadd2(y, off);
+    constexpr uint32_t KEEP = ~((1u << DROP) - 1u);
+    return fadd2(make_float2(__uint_as_float((__float_as_uint(z.x) + (bits0 << (DROP - 16))) & KEEP), __uint_as_float((__float_as_uint(z.y) + (bits1 << (DROP - 16))) & KEEP)),
+                 make_float2(-off.x, -off.y));
+}
+// Two quotients by a block's scale, no more than the type's largest value: products with its reciprocal, corrected by the residual, which the fused
+// multiply-add forms exactly.
+__device__ __forceinline__ float2 optim_quotient(float2 v, float scale, float inv, float most) {
+    const float2 i2 = make_float2(inv, inv), q = fmul2(v, i2), r = ffma2(make_float2(-q.x, -q.y), make_float2(scale, scale), v), o = ffma2(r, i2, q);
+    return make_float2(fminf(o.x, most), fminf(o.y, most));
 }
 // A block's largest value (>= 0, as its bits) to its scale: largest value / the type's, at least the smallest normal float; NaN and infinity stay.
 __device__ __forceinline__ float optim_scale(float largest, float of_type) {
     const float s = largest * (1.f / of_type);
     return s < 1.17549435e-38f ? 1.17549435e-38f : s;
 }
+// The largest of eight, as unsigned numbers.
+__device__ __forceinline__ uint32_t optim_max(const uint32_t (&v)[8]) {
+    return __vimax3_u32(__vimax3_u32(v[0], v[1], v[2]), __vimax3_u32(v[3], v[4], v[5]), max(v[6], v[7]));
+}
+__device__ __forceinline__ float optim_sqrt(float v) {          // (2 ulp; nothing is flushed)
+    float r;
+    asm("sqrt.approx.f32 %0, %1;\n" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float optim_rcp(float v) {           // (1 ulp)
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;\n" : "=f"(r) : "f"(v));
+    return r;
+}
+
+// What a tensor's step takes, the same for all its elements.
+struct OptimStep { float factor, inv1, root2, lr, decay; uint32_t hash; };
+
+// A warp's block of 256 elements from `at` on.
+template <typename P, typename G, bool MASTER, bool BITS8, bool FULL, typename A>
+__device__ __forceinline__ void optim_block(const A& a, const OptimTensor& t, long long at, const OptimStep& s) {
+    const int lane = threadIdx.x & 31;
+    const long long i = at + 8 * lane, block = at / OPTIM_BLOCK;
+    const int left = FULL ? 8 : (int)min(t.n - i, 8LL);         // (may be negative)
+    float p[8], g[8], m[8], v[8];
+    if constexpr (MASTER) optim_load<FULL>(t.master + i, left, p);
+    else optim_load<FULL>(static_cast<const P*>(t.p) + i, left, p);
+    optim_load<FULL>(static_cast<const G*>(t.g) + i, left, g);
+    if constexpr (BITS8) {
+        const uint2 cm = optim_load_codes<FULL>(static_cast<const uint8_t*>(t.m) + i, left), cv = optim_load_codes<FULL>(static_cast<const uint8_t*>(t.v) + i, left);
+        const float2 scale = t.scales[block];
+        optim_decode<false>(cm, scale.x, m);
+        optim_decode<true>(cv, scale.y, v);
+    } else {
+        optim_load<FULL>(static_cast<const float*>(t.m) + i, left, m);
+        optim_load<FULL>(static_cast<const float*>(t.v) + i, left, v);
+    }
+    const float2 factor = make_float2(s.factor, s.factor), beta1 = make_float2(a.beta1, a.beta1), beta2 = make_float2(a.beta2, a.beta2);
+    const float2 rest1 = make_float2(a.rest1, a.rest1), rest2 = make_float2(a.rest2, a.rest2), inv1 = make_float2(s.inv1, s.inv1);
+    const float2 root2 = make_float2(s.root2, s.root2), eps = make_float2(a.eps, a.eps), lr = make_float2(-s.lr, -s.lr), decay = make_float2(s.decay, s.decay);
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) {
+        // (each product and sum of the moments rounded by itself: they have the bits of the formula in elementary steps)
+        const float2 gj = fmul2(make_float2(g[j], g[j + 1]), factor);
+        const float2 mj = fadd2(fmul2(beta1, make_float2(m[j], m[j + 1])), fmul2(rest1, gj));
+        const float2 vj = fadd2(fmul2(beta2, make_float2(v[j], v[j + 1])), fmul2(fmul2(rest2, gj), gj));
+        const float2 den = ffma2(make_float2(optim_sqrt(vj.x), optim_sqrt(vj.y)), root2, eps);
+        const float2 q = fmul2(fmul2(mj, inv1), make_float2(optim_rcp(den.x), optim_rcp(den.y)));
+        const float2 pj = make_float2(p[j], p[j + 1]), o = ffma2(lr, ffma2(decay, pj, q), pj);
+        m[j] = mj.x; m[j + 1] = mj.y; v[j] = vj.x; v[j + 1] = vj.y; p[j] = o.x; p[j + 1] = o.y;
+    }
+    if constexpr (MASTER) optim_store<FULL>(t.master + i, left, p);
+    optim_store<FULL>(static_cast<P*>(t.p) + i, left, p);
+    if constexpr (BITS8) {
+        // (the bits of numbers >= 0 are in their order, infinities and NaN above all: such a scale spoils the block, whatever its codes)
+        uint32_t bm[8], bv[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) { bm[j] = __float_as_uint(m[j]) & 0x7fffffffu; bv[j] = __float_as_uint(v[j]); }
+        const float sm = optim_scale(__uint_as_float(__reduce_max_sync(0xffffffffu, optim_max(bm))), 448.f);
+        const float sv = optim_scale(__uint_as_float(__reduce_max_sync(0xffffffffu, optim_max(bv))), 57344.f);
+        if (lane == 0) t.scales[block] = make_float2(sm, sv);
+        const float im = 1.f / sm, iv = 1.f / sv;
+        const uint32_t h = optim_mix((uint32_t)(t.first_block + block) ^ s.hash) + 8 * lane;
+        uint32_t cm[4], cv[4];
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+            const uint32_t r0 = optim_mix(h + j), r1 = optim_mix(h + j + 1);
+            const float2 ym = optim_quotient(make_float2(__uint_as_float(bm[j]), __uint_as_float(bm[j + 1])), sm, im, 448.f);
+            const float2 yv = optim_quotient(make_float2(v[j], v[j + 1]), sv, iv, 57344.f);
+            const float2 y = optim_up_or_down<20>(ym, r0 & 0xffffu, r1 & 0xffffu, 0x1p-6f), z = optim_up_or_down<21>(yv, r0 >> 16, r1 >> 16, 0x1p-14f);
+            cm[j / 2] = optim_encode<false>(copysignf(y.x, m[j]), copysignf(y.y, m[j + 1]));
+            cv[j / 2] = optim_encode<true>(fmaxf(z.x, v[j] > 0.f ? 0x1p-16f : 0.f), fmaxf(z.y, v[j + 1] > 0.f ? 0x1p-16f : 0.f));
+        }
+        optim_store_codes<FULL>(static_cast<uint8_t*>(t.m) + i, left, make_uint2(cm[0] | cm[1] << 16, cm[2] | cm[3] << 16));
+        optim_store_codes<FULL>(static_cast<uint8_t*>(t.v) + i, left, make_uint2(cv[0] | cv[1] << 16, cv[2] | cv[3] << 16));
+    } else {
+        optim_store<FULL>(static_cast<float*>(t.m) + i, left, m);
+        optim_store<FULL>(static_cast<float*>(t.v) + i, left, v);
+    }
+}
 
 template <typename P, typename G, bool MASTER, bool BITS8, int CAP>
-__global__ void __launch_bounds__(32 * OPTIM_WARPS)
+__global__ void __launch_bounds__(32 * OPTIM_WARPS, OPTIM_BLOCKS)
 k_adamw(const __grid_constant__ AdamParams<CAP> a) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    float factor = 1.f;
+    const int warp = threadIdx.x >> 5;
+    OptimStep s;
+    s.factor = 1.f;
     if (a.factor) {
-        factor = *a.factor;
-        if (!(fabsf(factor) < INFINITY)) return;        // nothing is changed, the number of steps neither
+        s.factor = *a.factor;
+        if (!(fabsf(s.factor) < INFINITY)) return;      // nothing is changed, the number of steps neither
     }
     for (unsigned chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
         int lo = 0, hi = a.n_tensors - 1;               // the last tensor that starts at this chunk or before
@@ -122,77 +219,17 @@ k_adamw(const __grid_constant__ AdamParams<CAP> a) {
             if (a.t[mid].chunk0 <= chunk) lo = mid; else hi = mid - 1;
         }
         const OptimTensor& t = a.t[lo];
-        const bool wide = t.wide;
         const int step = *t.step + 1;
         // 1 - b^t without cancellation (a product of 53 bits, then float32)
-        const float c1 = -expm1f((float)(a.ln1 * step)), c2 = -expm1f((float)(a.ln2 * step));
-        const float inv1 = 1.f / c1, root2 = 1.f / sqrtf(c2);
-        const float lr = t.lr_at ? *t.lr_at : t.lr, decay = t.decay;
-        const long long start = (long long)(chunk - t.chunk0) * OPTIM_CHUNK, end = min(t.n, start + OPTIM_CHUNK);
+        s.inv1 = -1.f / expm1f((float)(a.ln1 * step));
+        s.root2 = 1.f / sqrtf(-expm1f((float)(a.ln2 * step)));
+        s.lr = t.lr_at ? *t.lr_at : t.lr;
+        s.decay = t.decay;
+        s.hash = optim_mix(a.seed + 0x9e3779b9u * (uint32_t)step);
+        const long long start = (long long)(chunk - t.chunk0) * a.chunk, end = min(t.n, start + a.chunk);
         for (long long at = start + warp * OPTIM_BLOCK; at < end; at += OPTIM_WARPS * OPTIM_BLOCK) {
-            const long long i = at + 8 * lane;
-            const int left = (int)min(t.n - i, 8LL);    // (may be negative)
-            float p[8], g[8], m[8], v[8];
-            if constexpr (MASTER) optim_load(t.master + i, wide, left, p);
-            else optim_load(static_cast<const P*>(t.p) + i, wide, left, p);
-            optim_load(static_cast<const G*>(t.g) + i, wide, left, g);
-            const long long block = at / OPTIM_BLOCK;
-            if constexpr (BITS8) {
-                const float2 s = t.scales[block];
-                optim_decode<false>(optim_load_codes(static_cast<const uint8_t*>(t.m) + i, wide, left), s.x, m);
-                optim_decode<true>(optim_load_codes(static_cast<const uint8_t*>(t.v) + i, wide, left), s.y, v);
-            } else {
-                optim_load(static_cast<const float*>(t.m) + i, wide, left, m);
-                optim_load(static_cast<const float*>(t.v) + i, wide, left, v);
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float gj = g[j] * factor;
-                // (each product and sum rounded by itself: the states have the bits of the formula in elementary steps)
-                m[j] = __fadd_rn(__fmul_rn(a.beta1, m[j]), __fmul_rn(a.rest1, gj));
-                v[j] = __fadd_rn(__fmul_rn(a.beta2, v[j]), __fmul_rn(__fmul_rn(a.rest2, gj), gj));
-                const float s = (m[j] * inv1) / fmaf(sqrtf(v[j]), root2, a.eps);
-                p[j] = fmaf(-lr, fmaf(decay, p[j], s), p[j]);
-            }
-            if constexpr (MASTER) optim_store(t.master + i, wide, left, p);
-            optim_store(static_cast<P*>(t.p) + i, wide, left, p);
-            if constexpr (BITS8) {
-                // (the bits of numbers >= 0 are in their order, infinities and NaN above all)
-                uint32_t bm = 0, bv = 0;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const bool on = j < left;
-                    bm = max(bm, on ? __float_as_uint(fabsf(m[j])) : 0u);
-                    bv = max(bv, on ? __float_as_uint(v[j]) & 0x7fffffffu : 0u);
-                }
-                const float sm = optim_scale(__uint_as_float(__reduce_max_sync(0xffffffffu, bm)), 448.f);
-                const float sv = optim_scale(__uint_as_float(__reduce_max_sync(0xffffffffu, bv)), 57344.f);
-                if (lane == 0) t.scales[block] = make_float2(sm, sv);
-                const uint32_t h = optim_mix((uint32_t)(t.first_block + block) ^ optim_mix(a.seed + 0x9e3779b9u * (uint32_t)step));
-                uint32_t cm[4], cv[4];
-#pragma unroll
-                for (int j = 0; j < 8; j += 2) {
-                    float y[2], z[2];
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const uint32_t r = optim_mix(h + 8 * lane + j + k);
-                        float q = fabsf(m[j + k]) / sm;
-                        q = q > 448.f ? 448.f : q;
-                        y[k] = copysignf(optim_up_or_down<20>(q, r & 0xffffu, 0x1p-6f), m[j + k]);
-                        q = v[j + k] / sv;
-                        q = q > 57344.f ? 57344.f : q;
-                        z[k] = optim_up_or_down<21>(q, r >> 16, 0x1p-14f);
-                        if (v[j + k] > 0.f && z[k] < 0x1p-16f) z[k] = 0x1p-16f;
-                    }
-                    cm[j / 2] = optim_encode<false>(y[0], y[1]);
-                    cv[j / 2] = optim_encode<true>(z[0], z[1]);
-                }
-                optim_store_codes(static_cast<uint8_t*>(t.m) + i, wide, left, make_uint2(cm[0] | cm[1] << 16, cm[2] | cm[3] << 16));
-                optim_store_codes(static_cast<uint8_t*>(t.v) + i, wide, left, make_uint2(cv[0] | cv[1] << 16, cv[2] | cv[3] << 16));
-            } else {
-                optim_store(static_cast<float*>(t.m) + i, wide, left, m);
-                optim_store(static_cast<float*>(t.v) + i, wide, left, v);
-            }
+            if (t.wide && at + OPTIM_BLOCK <= t.n) optim_block<P, G, MASTER, BITS8, true>(a, t, at, s);
+            else optim_block<P, G, MASTER, BITS8, false>(a, t, at, s);
         }
     }
     // the last thread block to come here, when all have read the numbers of steps, counts the step

@@ -9,6 +9,7 @@ norm).  As in `layers`: calls of the library (include/hf.h) on the current devic
 from __future__ import annotations
 
 import functools
+import operator
 import struct
 
 import numpy as np
@@ -20,6 +21,9 @@ from .layers import _TYPES, _check, _current, _fail, _here, _lib, _stream
 _F32, _BF16 = torch.float32, torch.bfloat16
 _BLOCK = 256                                                # elements that share a scale; tensors start at multiples of it in the state's buffers
 _STEP = struct.Struct("@3iI3d2P").pack                      # hf_adamw_step
+# (mapped over all tensors: a call of a loop's body takes twice as long)
+_pointer, _numel, _where, _dense = torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.get_device, torch.Tensor.is_contiguous
+_type, _grad, _rate, _of_group = operator.attrgetter("dtype"), operator.attrgetter("grad"), operator.itemgetter("lr"), operator.itemgetter("lr", "weight_decay", "betas", "eps")
 
 
 @functools.lru_cache(maxsize=256)
@@ -34,17 +38,19 @@ def gradient_norm(tensors, max_norm=float("inf")):
     if not tensors:
         _fail("no tensors")
     dev = _current("tensors[0]", tensors[0])
-    rows = []
-    for i, t in enumerate(tensors):
-        kind = _TYPES.get(t.dtype)
-        if kind is None:
-            _fail(f"tensors[{i}] is {t.dtype}: bfloat16, float16 and float32 are taken")
-        if t.get_device() != dev:
-            _here(f"tensors[{i}]", t, dev)
-        if not t.is_contiguous():
-            _fail(f"tensors[{i}] has to be contiguous")
-        rows += (t.data_ptr(), t.numel(), kind)
     n = len(tensors)
+    kinds, here, dense = list(map(_type, tensors)), list(map(_where, tensors)), list(map(_dense, tensors))
+    if here.count(dev) != n or not all(dense):
+        for i, t in enumerate(tensors):
+            _here(f"tensors[{i}]", t, dev)
+            if not dense[i]:
+                _fail(f"tensors[{i}] has to be contiguous")
+    try:
+        kinds = [_TYPES[k] for k in kinds]
+    except KeyError as e:
+        _fail(f"a tensor is {e.args[0]}: bfloat16, float16 and float32 are taken")
+    rows = [0] * (3 * n)
+    rows[0::3], rows[1::3], rows[2::3] = map(_pointer, tensors), map(_numel, tensors), kinds
     pack, doubles = _norm_plan(dev, n)
     out = torch.empty(2, dtype=_F32, device=tensors[0].device)
     ws = torch.empty(doubles, dtype=torch.float64, device=out.device)
@@ -52,6 +58,27 @@ def gradient_norm(tensors, max_norm=float("inf")):
     if status:
         _check(status)
     return out.unbind()
+
+
+class _Launch:
+    """One call of the library: its parameters, and its table."""
+
+    def __init__(self, params, dtype, grad_dtype, device, table, head, counter):
+        self.params, self.dtype, self.grad_dtype, self.device, self.table, self.head, self.counter = params, dtype, grad_dtype, device, table, head, counter
+        self.at, self.sizes, self.p, self.g = table.ctypes.data, [p.numel() for p in params], None, None
+
+    def look(self):
+        """The parameters and gradients as they are now, into the table."""
+        params = self.params
+        grads = list(map(_grad, params))
+        g, p, n = list(map(_pointer, grads)), list(map(_pointer, params)), len(params)
+        for tensors, kind, name in ((grads, self.grad_dtype, "gradient"), (params, self.dtype, "parameter")):
+            if list(map(_numel, tensors)) != self.sizes or list(map(_type, tensors)).count(kind) != n or list(map(_where, tensors)).count(self.device) != n or not all(map(_dense, tensors)):
+                _fail(f"a {name}'s size, type, device or layout is not what it was: {kind}, contiguous, on device {self.device}, of the parameter's size is taken")
+        if p != self.p:
+            self.table[:, 0] = self.p = p
+        if g != self.g:
+            self.table[:, 1] = self.g = g
 
 
 class AdamW(torch.optim.Optimizer):
@@ -142,19 +169,16 @@ class AdamW(torch.optim.Optimizer):
         for p in params:
             kinds.setdefault((p.dtype, p.grad.dtype, "master" in self.state[p], *of[p]), []).append(p)
         counter = self.buffers["steps"].data_ptr() + 4 * len(self._params)
-        launches = []
-        for (dtype, grad_dtype, _, betas, eps), some in kinds.items():
-            table = self._rows(some)
-
-            def step(factor, head=(_TYPES[dtype], _TYPES[grad_dtype], self.state_bits, self.seed, *map(float, betas), float(eps))):
-                return _STEP(*head, factor, counter)
-            launches.append((some, dtype, grad_dtype, table, table.ctypes.data, step))
-        return launches
+        return [_Launch(some, dtype, grad_dtype, self._device, self._rows(some), (_TYPES[dtype], _TYPES[grad_dtype], self.state_bits, self.seed, *map(float, betas), float(eps)),
+                        counter) for (dtype, grad_dtype, _, betas, eps), some in kinds.items()]
 
     def _settings(self):
         """What the tables were made from, and step for step may change."""
+        groups = self.param_groups
+        if torch.Tensor not in map(type, map(_rate, groups)):
+            return list(map(_of_group, groups))
         seen = []
-        for g in self.param_groups:
+        for g in groups:
             lr = g["lr"]
             if isinstance(lr, torch.Tensor):
                 if lr.dtype is not _F32 or lr.numel() != 1:
@@ -165,7 +189,6 @@ class AdamW(torch.optim.Optimizer):
             seen.append((lr, g["weight_decay"], g["betas"], g["eps"]))
         return seen
 
-    @torch.no_grad()
     def step(self, closure=None, grad_factor=None):
         """One step.  grad_factor: a float32 tensor of one element on the device (as `gradient_norm` returns it), by which the gradients are
         multiplied; where it is not finite nothing is changed."""
@@ -182,26 +205,23 @@ class AdamW(torch.optim.Optimizer):
             factor = grad_factor.data_ptr()
         _current("the first parameter", self._params[0])
         settings = self._settings()
-        some = [p for p in self._params if p.grad is not None]
-        if len(some) == len(self._params):
-            launches = self._plan if settings == self._planned else None
-            if launches is not None and any(p.grad.dtype is not kind for ps, _, kind, *_ in launches for p in ps):
+        launches = self._plan if settings == self._planned else None
+        if launches is not None:
+            try:
+                for launch in launches:
+                    launch.look()
+            except TypeError:               # a gradient is missing
                 launches = None
-            if launches is None:
-                launches = self._plan = self._launches(some)
-                self._planned = settings
-        else:
+        if launches is None:
+            some = [p for p in self._params if p.grad is not None]
             launches = self._launches(some)
-        for params, dtype, grad_dtype, table, at, step in launches:
-            grads = [p.grad for p in params]
-            for p, g in zip(params, grads):
-                if p.dtype is not dtype or p.get_device() != self._device or not p.is_contiguous():
-                    _fail("a parameter's type, device or layout is not what it was at construction")
-                if g.get_device() != self._device or not g.is_contiguous() or g.shape != p.shape:
-                    _fail(f"a gradient of {tuple(g.shape)} on {g.device} for a parameter of {tuple(p.shape)}: the same, contiguous, is taken")
-            table[:, 0] = [p.data_ptr() for p in params]
-            table[:, 1] = [g.data_ptr() for g in grads]
-            status = _lib().hf_adamw(step(factor), at, len(params), _stream())
+            for launch in launches:
+                launch.look()
+            if len(some) == len(self._params):
+                self._plan, self._planned = launches, settings
+        stream = _stream()
+        for launch in launches:
+            status = _lib().hf_adamw(_STEP(*launch.head, factor, launch.counter), launch.at, len(launch.params), stream)
             if status:
                 _check(status)
         return loss
