@@ -163,10 +163,12 @@ __device__ __forceinline__ void optim_block(const A& a, const OptimTensor& t, lo
     const float2 root2 = make_float2(s.root2, s.root2), eps = make_float2(a.eps, a.eps), lr = make_float2(-s.lr, -s.lr), decay = make_float2(s.decay, s.decay);
 #pragma unroll
     for (int j = 0; j < 8; j += 2) {
-        // (each product and sum of the moments rounded by itself: they have the bits of the formula in elementary steps)
+        // (each product and sum of the moments rounded by itself: they have the bits of the formula in elementary steps.  The sums are taken one by one:
+        // a packed sum of packed products would become a fused multiply-add.)
         const float2 gj = fmul2(make_float2(g[j], g[j + 1]), factor);
-        const float2 mj = fadd2(fmul2(beta1, make_float2(m[j], m[j + 1])), fmul2(rest1, gj));
-        const float2 vj = fadd2(fmul2(beta2, make_float2(v[j], v[j + 1])), fmul2(fmul2(rest2, gj), gj));
+        const float2 m0 = fmul2(beta1, make_float2(m[j], m[j + 1])), m1 = fmul2(rest1, gj);
+        const float2 v0 = fmul2(beta2, make_float2(v[j], v[j + 1])), v1 = fmul2(fmul2(rest2, gj), gj);
+        const float2 mj = make_float2(__fadd_rn(m0.x, m1.x), __fadd_rn(m0.y, m1.y)), vj = make_float2(__fadd_rn(v0.x, v1.x), __fadd_rn(v0.y, v1.y));
         const float2 den = ffma2(make_float2(optim_sqrt(vj.x), optim_sqrt(vj.y)), root2, eps);
         const float2 q = fmul2(fmul2(mj, inv1), make_float2(optim_rcp(den.x), optim_rcp(den.y)));
         const float2 pj = make_float2(p[j], p[j + 1]), o = ffma2(lr, ffma2(decay, pj, q), pj);
