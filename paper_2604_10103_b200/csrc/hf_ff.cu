@@ -380,10 +380,11 @@ Sizes linear_dw_sizes(const hf_linear_shape* g) { return {{{g->out_width, g->wid
 Tiling cut_linear(const Device* d, const hf_linear_shape* g) { return ff_tiling(d, linear_sizes(g).data, 1, 1, FF_CUT_LINEAR); }
 Tiling cut_linear_dx(const Device* d, const hf_linear_shape* g) { return ff_tiling(d, linear_dx_sizes(g).data, 1, 1, FF_CUT_DX); }
 Tiling cut_linear_dw(const Device* d, const hf_linear_shape* g) { return ff_tiling(d, linear_dw_sizes(g).data, 1, 1, FF_CUT_DW); }
-// Thread blocks that share a group's rows: so many that four a multiprocessor are at work, 32 rows each at least.
+// Thread blocks that share a group's rows: so many that all are at work at a time (one round: the second of 1.35 rounds took as long as the first), 32 rows
+// each at least.
 int linear_parts(const Device* d, const hf_linear_shape* g) {
     const long long others = (long long)((g->out_width + 255) / 256) * linear_groups(g), rows = linear_group(g);
-    long long n = others ? (4LL * d->sm_count + others - 1) / others : 1;
+    long long n = others ? (long long)LINEAR_BWD_BLOCKS * d->sm_count / others : 1;
     if (n > (rows + 31) / 32) n = (rows + 31) / 32;
     return n < 1 ? 1 : (int)n;
 }
@@ -394,18 +395,25 @@ hf_status launch_linear_rows(const FfRowsParams& p, int sms, cudaStream_t st) {
     if (p.features >= 16 * 2 * sms) return launch_after(k_ff_rows<T, NT, true, 0, true>, dim3((p.features + 15) / 16), dim3(256), 0, st, p);
     return launch_after(k_ff_rows<T, NT, false, 0, true>, dim3((p.features + 7) / 8), dim3(512), 0, st, p);
 }
-template <typename T>
+template <typename T, bool GATE>
 hf_status launch_linear_bwd(const LinearBwdParams& p, int act, int groups, cudaStream_t st) {
     const dim3 grid(groups * p.parts, (p.cols + 255) / 256);
-    auto kernel = act == HF_ACT_NONE ? k_linear_bwd<T, HF_ACT_NONE> : (act == HF_ACT_SILU ? k_linear_bwd<T, HF_ACT_SILU> : k_linear_bwd<T, HF_ACT_GELU_TANH>);
+    auto kernel = act == HF_ACT_NONE ? k_linear_bwd<T, HF_ACT_NONE, GATE> : (act == HF_ACT_SILU ? k_linear_bwd<T, HF_ACT_SILU, GATE> : k_linear_bwd<T, HF_ACT_GELU_TANH, GATE>);
     return launch_after(kernel, grid, dim3(32 * LINEAR_BWD_WARPS), 0, st, p);
+}
+template <typename T>
+hf_status launch_linear_bwd(const LinearBwdParams& p, int act, int groups, cudaStream_t st) {
+    return p.gate ? launch_linear_bwd<T, true>(p, act, groups, st) : launch_linear_bwd<T, false>(p, act, groups, st);
 }
 // The backward pass's scratch: dp | the products' partial sums | those of db and dgate.
 struct LinearWorkspace { size_t products, sums, bytes; };
 LinearWorkspace linear_workspace(const Device* d, const hf_linear_shape* g) {
     const size_t dp = round_up((size_t)g->rows * g->out_width * 2);
     const size_t x = ff_partial_bytes(cut_linear_dx(d, g), linear_dx_sizes(g).data, 1), w = ff_partial_bytes(cut_linear_dw(d, g), linear_dw_sizes(g).data, 1);
-    const size_t part = round_up((size_t)linear_groups(g) * linear_parts(d, g) * g->out_width * sizeof(float));
+    hf_linear_shape whole = *g;                 // (without a gate all rows are one group)
+    whole.rows_per_group = 0;
+    const size_t grouped = (size_t)linear_groups(g) * linear_parts(d, g), one = linear_parts(d, &whole);
+    const size_t part = round_up((grouped > one ? grouped : one) * g->out_width * sizeof(float));
     return {dp, dp + round_up(x > w ? x : w), dp + round_up(x > w ? x : w) + 2 * part};
 }
 }  // namespace
