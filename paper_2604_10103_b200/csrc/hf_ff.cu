@@ -56,6 +56,7 @@ Tiling ff_tiling(const Device* d, const Size* s, int n, int segments, FfCut cut)
             if (bn > 256 && bn != 512) continue;
             if (cut == FF_CUT_DH && cg == 1 && bn > 128) break;         // (its staging leaves two stages)
             if (cut == FF_CUT_LINEAR && cg == 1 && bn > 192) break;     // (three)
+            if (cut == FF_CUT_LINEAR && cg == 2 && s[0].rows <= 128) break;     // (the pair's second would have no rows: 77 rows of 1536 to 6144 13.0 us at 2x96, 10.4 at 1x64)
             const int out = gated ? bn / 2 : bn, slots = cg == 1 ? d->sm_count : d->pairs;
             long long tiles = 0;
             double blocks = 0;

@@ -102,8 +102,7 @@ k_ff_rows(const FfRowsParams p) {
             for (int w = 0; w < WARPS; ++w) v += s_sum[w][f >> 3][f & 7][row];
             linear_one<T>(p.linear, p.act, row, col, v);
         }
-        return;
-    }
+    } else
     for (int e = threadIdx.x; e < 64 * NT; e += 32 * WARPS) {
         const int row = e >> 3, f = e & 7, col = blockIdx.x * 8 + f;
         if (row >= p.rows || col >= p.features) continue;
