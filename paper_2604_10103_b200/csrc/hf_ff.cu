@@ -46,6 +46,17 @@ struct Size { long long rows, cols, contraction; };
 // dx 2x256 321, 1x192 330, 1x256 335, 2x192 345; dW 2x512 278, 2x256 292, (2x256 317, 2x224 334, 1x256 335 before other parts were faster).
 // 1000 rows: dx 2x256/3 82, /2 87, /1 96, 2x128 92, 1x128 96.  300 rows: dx 1x128/4 56.5, 2x128/3 57, 1x64 67.5; y 1x64 30.5, 2x128 31; g, u 1x256
 // 31.9, 2x256 32, 1x128 35, 1x64 41.  77 rows: y 1x64/3 22.4, /4 23, /6 25.6, /1 26.8; dx 1x128/6 38.9, /4 40.9, /12 43.4, 1x64 57.9.
+// LINEAR's estimate, of what 13 sizes from 32 x 1536 x 1536 to 32760 x 6144 x 1536 took with seven tilings each (12 % off on average, the fastest of each
+// found): a block of 64 of the contraction takes its MMAs, the loop's own latency, or, with all multiprocessors at work (`busy`), the operands' way out of L2, more so
+// in long calls; then something a round, and the last tile's epilogue.  us, 4680 rows: 1536 to 6144 2x256 67, 2x224 72, 2x192 75, 1x192 86; 6144 to 1536 2x224
+// 69, 1x128 80, 2x256 85; 300 rows of 1536 to 6144: 1x128 10.7, 1x192 13.4, 2x192 13.6; of 6144 to 1536: 1x96/3 16.1, 1x64 19.8, 2x192 27.
+double linear_cycles(int bn, double columns, double rounds, double blocks, double busy) {
+    if (busy > 1) busy = 1;
+    const double mma = 2.67 * bn, loop = 262 + 0.6 * bn, l2 = 1.76 * columns * busy * busy * (1 + 0.36 * (rounds < 5 ? (rounds - 1) / 4 : 1));
+    double block = mma > loop ? mma : loop;
+    if (block < l2) block = l2;
+    return rounds * (blocks * block + 700) + 22.0 * bn;
+}
 enum FfCut { FF_CUT_GATED, FF_CUT_Y, FF_CUT_DH, FF_CUT_DX, FF_CUT_DW, FF_CUT_LINEAR };
 Tiling ff_tiling(const Device* d, const Size* s, int n, int segments, FfCut cut) {
     const bool gated = cut == FF_CUT_GATED, b_mn = cut >= FF_CUT_DH && cut <= FF_CUT_DW, a_mn = cut == FF_CUT_DW, may_split = cut != FF_CUT_GATED && cut != FF_CUT_DH;
@@ -55,7 +66,6 @@ Tiling ff_tiling(const Device* d, const Size* s, int n, int segments, FfCut cut)
         for (int bn = b_mn ? 64 * cg : 64; bn <= (a_mn && cg == 2 ? 512 : 256); bn += gated ? 64 : (b_mn ? 64 * cg : 32)) {
             if (bn > 256 && bn != 512) continue;
             if (cut == FF_CUT_DH && cg == 1 && bn > 128) break;         // (its staging leaves two stages)
-            if (cut == FF_CUT_LINEAR && cg == 1 && bn > 192) break;     // (three)
             if (cut == FF_CUT_LINEAR && cg == 2 && s[0].rows <= 128) break;     // (the pair's second would have no rows: 77 rows of 1536 to 6144 13.0 us at 2x96, 10.4 at 1x64)
             const int out = gated ? bn / 2 : bn, slots = cg == 1 ? d->sm_count : d->pairs;
             long long tiles = 0;
@@ -70,7 +80,9 @@ Tiling ff_tiling(const Device* d, const Size* s, int n, int segments, FfCut cut)
             blocks *= segments;
             for (int k = 1; k <= (may_split && bn <= 256 && tiles < slots ? 16 : 1); ++k) {
                 if (k > 1 && blocks < 4 * k) break;
-                double cost = (double)((tiles * k + slots - 1) / slots) * (blocks / k * block + between);
+                const double rounds = (double)((tiles * k + slots - 1) / slots);
+                double cost = rounds * (blocks / k * block + between);
+                if (cut == FF_CUT_LINEAR) cost = linear_cycles(bn, columns, rounds, blocks / k, (double)(tiles * k) / slots);
                 if (k > 1) cost += 4000.0 + 1200.0 * k + tiles * k * 128.0 * cg * bn * 8.0 / 2300.0;
                 if (cost < least) { least = cost; best = {cg, bn, k}; }
             }
@@ -87,7 +99,7 @@ struct Launch {
     FfJoinOut join = {};
     Launch(const Device* dev, int t, int act, Tiling cut) : d(dev), type(t), tiling(cut) {
         memset(&p, 0, sizeof(p));
-        p.segments = 1; p.act = act; p.dev_status = dev->status; p.bn = cut.bn; p.splits = cut.splits;
+        p.segments = 1; p.a_rows = 128; p.act = act; p.dev_status = dev->status; p.bn = cut.bn; p.splits = cut.splits;
     }
     // Contraction-contiguous (K-major) operand of `tile` rows; row-contiguous (MN-major) operand.
     hf_status k_major(CUtensorMap* m, const Matrix& x, int tile) { return matrix_map(d, m, type, x.p, x.rows, x.cols, x.stride, 64, tile); }
@@ -107,7 +119,8 @@ struct Launch {
     template <typename T, int EPI, bool A_MN, bool B_MN, int CG, int NB = 1>
     hf_status run_t(cudaStream_t st) {
         typedef FfGemm<EPI, CG, NB> C;
-        p.stages = C::stages_for(p.bn);
+        p.set = C::set_boxes(p.linear.has_residual, p.save);
+        p.stages = C::stages_for(p.bn, p.set);
         auto kernel = k_ff_gemm<T, EPI, A_MN, B_MN, CG, NB>;
         struct Key {};
         HFL_TRY(allow_shared<Key>(d, kernel, C::SMEM_MAX));
@@ -119,7 +132,7 @@ struct Launch {
         attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
         attr[1].val.programmaticStreamSerializationAllowed = 1;
         cfg.gridDim = dim3(CG * (tiles < slots ? tiles : slots)); cfg.blockDim = dim3(C::THREADS);
-        cfg.dynamicSmemBytes = C::smem_bytes(p.bn, p.stages); cfg.stream = st; cfg.attrs = attr; cfg.numAttrs = 2;
+        cfg.dynamicSmemBytes = C::smem_bytes(p.bn, p.stages, p.set); cfg.stream = st; cfg.attrs = attr; cfg.numAttrs = 2;
         HFL_CUDA(cudaLaunchKernelEx(&cfg, kernel, p));
         if (p.splits == 1) return HF_OK;
         const long long warps = (long long)p.tile0[p.products] * 4 * CG * (p.bn / 8);
@@ -460,7 +473,8 @@ hf_status hf_linear(const hf_linear_shape* g, const void* x, const void* weight,
     if (l.tiling.splits > 1) HFL_TRY(ff_pointer(workspace, "workspace"));
     l.p.partials = static_cast<float*>(workspace);
     l.p.linear = e;
-    HFL_TRY(l.k_major(&l.p.a[0], {x, M, K, g->x_stride}, 128));
+    if (M < 128) l.p.a_rows = (int)(M + 7) / 8 * 8;             // (rows that are not there are not brought)
+    HFL_TRY(l.k_major(&l.p.a[0], {x, M, K, g->x_stride}, l.p.a_rows));
     HFL_TRY(l.k_major(&l.p.b[0], {weight, N, K, K}, l.p.bn / l.tiling.cg));
     HFL_TRY(l.output(0, {y, M, N, g->y_stride}));
     if (pre) { HFL_TRY(l.output(1, {pre, M, N, N})); l.p.save = 1; }

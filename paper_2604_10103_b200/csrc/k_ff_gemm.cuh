@@ -7,7 +7,7 @@
 // An operand whose contraction index is contiguous ("K-major") is a box of 64 contraction elements by its rows; one whose row index is
 // contiguous ("MN-major": Wd in dh, Wg and Wu in dx, everything in dW) is read as it lies too, in boxes of 64 rows by 64 contraction
 // elements: the tensor cores take both, so nothing is transposed in memory.  Elements past an operand's end read as zero.
-// A thread block is persistent: a loader thread, an MMA thread, and eight epilogue warps that empty one accumulator while the MMAs fill the
+// A thread block is persistent: a loader thread for each operand, an MMA thread, and eight epilogue warps that empty one accumulator while the MMAs fill the
 // other.  CG 2: two thread blocks on neighbouring SMs share a tile of 256 rows (cta_group::2): each holds its 128 rows of A and of the
 // accumulator and half of B, which the tensor cores of both read, so a tile costs a third less operand traffic; the first of the pair
 // issues the MMAs of both.  Every wait is bounded (~1 s) and reports through the status word; the two cluster barriers are reached by every
@@ -53,7 +53,9 @@ struct FfGemmParams {
     float* partials;
     int bn;                             // accumulator columns of a tile: a multiple of 32 (GATED: half of them g, half u)
     int stages;
+    int set;                            // boxes of an epilogue warp's set
     int act, save;
+    int a_rows;                         // rows of A's boxes (contraction contiguous): 128, or what there is in multiples of 8.  (The accumulator's rows behind them are nobody's.)
     int early_b;                        // B may be read before the kernel before this one is done
     int* dev_status;
     LinearEpilogue linear;
@@ -66,19 +68,21 @@ struct FfGemm {
     static constexpr int BM = 128, BK = 64;             // rows of a thread block, contraction of a stage
     static constexpr int A_BYTES = BM * BK * 2;
     static constexpr int EPI_WARPS = 8, CW = 32;        // CW: columns that an epilogue warp takes at a time
-    static constexpr int WARP_TMA = EPI_WARPS, WARP_MMA = EPI_WARPS + 1;
-    static constexpr int THREADS = 32 * (EPI_WARPS + 2);
+    static constexpr int WARP_TMA = EPI_WARPS, WARP_MMA = EPI_WARPS + 1, WARP_TMA_B = EPI_WARPS + 2;
+    static constexpr int THREADS = 32 * (EPI_WARPS + 3);
     static constexpr int MAX_STAGES = 8;
     // per epilogue warp: two boxes of 32 rows x CW columns on their way out; DHIDDEN: two sets of three, two of them in and out; LINEAR: two sets of
     // two, the residual in and y out, and pre
-    static constexpr int BOX = 64 * CW, SET = EPI == FF_DHIDDEN ? 3 : (EPI == FF_LINEAR ? 2 : 1), STAGING = 2 * SET * BOX;
+    static constexpr int BOX = 64 * CW;
+    // (boxes of a set: LINEAR as many as a step has both in it and out of it)
+    __host__ __device__ static constexpr int set_boxes(bool residual, bool save) { return EPI == FF_DHIDDEN ? 3 : (EPI == FF_LINEAR && residual && save ? 2 : 1); }
     static constexpr int BAR_BYTES = 384;
     static constexpr int SMEM_MAX = 232448;
     // bn: columns of an accumulator; NB bn / CG columns of B in each thread block (in boxes of 64 where the operand is MN-major)
     __host__ __device__ static constexpr int stage_bytes(int bn) { return A_BYTES + (NB * bn / CG + 63) / 64 * 64 * BK * 2; }
-    static constexpr int smem_bytes(int bn, int stages) { return stages * stage_bytes(bn) + EPI_WARPS * STAGING + BAR_BYTES + 1024; }
-    static constexpr int stages_for(int bn) {
-        const int n = (SMEM_MAX - EPI_WARPS * STAGING - BAR_BYTES - 1024) / stage_bytes(bn);
+    static constexpr int smem_bytes(int bn, int stages, int set) { return stages * stage_bytes(bn) + EPI_WARPS * 2 * set * BOX + BAR_BYTES + 1024; }
+    static constexpr int stages_for(int bn, int set) {
+        const int n = (SMEM_MAX - EPI_WARPS * 2 * set * BOX - BAR_BYTES - 1024) / stage_bytes(bn);
         return n < MAX_STAGES ? n : MAX_STAGES;
     }
 };
@@ -265,7 +269,7 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
     const uint32_t s_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* s_gen = smem_raw + (s_base - smem_u32(smem_raw));
     const int stage_bytes = C::stage_bytes(p.bn), stages = p.stages;
-    const uint32_t s_staging = s_base + stages * stage_bytes, bar0 = s_staging + C::EPI_WARPS * C::STAGING;
+    const uint32_t s_staging = s_base + stages * stage_bytes, bar0 = s_staging + C::EPI_WARPS * 2 * p.set * C::BOX;
     const uint32_t bar_full = bar0, bar_free = bar0 + 64, bar_acc = bar0 + 128, bar_acc_free = bar0 + 144, bar_in = bar0 + 192;
     uint8_t* bar_gen = s_gen + (bar0 - s_base);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar_gen + 160);
@@ -293,63 +297,62 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
     // The kernel may have been launched while the one before it still runs: only the threads that read global memory themselves wait for
     // that, everything else follows from what they read.  The next kernel may be launched once this one has waited, so that what was
     // written before this one is there for it from the start (early_b).
-    if (warp == C::WARP_TMA) {
-        // ================================================================= loader
+    if (warp == C::WARP_TMA || warp == C::WARP_TMA_B) {
+        // ================================================================= loaders, one of A and one of B: a copy's issue and a barrier's test take 200 cycles
+        // together, which one thread's two copies a block would make the bound of tiles of few columns
+        const bool of_a = warp == C::WARP_TMA;
         if (lane == 0) {
-            bool ok = true;
+            tma_prefetch_map(of_a ? &p.a[0] : &p.b[0]);        // (while the kernel before this one still runs)
+            bool ok = true, waits = of_a || !p.early_b;        // (early_b: B's first blocks are on their way before A's rows are there)
             int s = 0;
             uint32_t phase = 1;                 // (the stages are free at first)
             const int b_boxes = B_MN ? (bn_own + 63) / 64 : 1;
-            const uint32_t bytes = CG * (C::A_BYTES + (B_MN ? b_boxes * 8192 : bn_own * C::BK * 2));        // of the whole tile
-            auto load_a = [&](const FfTile& tile, int k, uint32_t sA, uint32_t full) {
-                const int seg = p.segments > 1 && k >= p.kb[0], i = tile.product + seg;       // (one of the two is always 0)
-                const int kc = (k - seg * p.kb[0]) * C::BK, m0 = tile.m0 + rank * C::BM;
-                if (A_MN) {
-                    ff_load<CG>(sA, &p.a[i], m0, kc, full);
-                    ff_load<CG>(sA + 8192, &p.a[i], m0 + 64, kc, full);
-                } else
-                    ff_load<CG>(sA, &p.a[i], kc, m0, full);
-            };
-            auto load_b = [&](const FfTile& tile, int k, uint32_t sB, uint32_t full) {
-                const int seg = p.segments > 1 && k >= p.kb[0], i = tile.product + seg;
-                const int kc = (k - seg * p.kb[0]) * C::BK, n0 = tile.n0 + (EPI == FF_GATED ? 0 : rank * bn_own);
-                if (EPI == FF_GATED) {
-                    // g's columns in front of u's: the pair's first thread block holds Wg's rows, the second Wu's
-                    ff_load<CG>(sB, &p.b[rank], kc, n0, full);
-                    if (CG == 1) ff_load<CG>(sB + bn_out * C::BK * 2, &p.b[1], kc, n0, full);
-                } else if (B_MN) {
-                    for (int x = 0; x < b_boxes; ++x) ff_load<CG>(sB + x * 8192, &p.b[i], n0 + 64 * x, kc, full);
-                } else
-                    ff_load<CG>(sB, &p.b[i], kc, n0, full);
-            };
-            bool first = true;
+            const uint32_t bytes = CG * (p.a_rows * C::BK * 2 + (B_MN ? b_boxes * 8192 : bn_own * C::BK * 2));      // of the whole tile
             for (int t = tile_first; ok && t < n_tiles; t += tile_step) {
                 const FfTile tile = ff_tile(p, t, CG * C::BM, bn_out);
                 const int k_all = p.kb[tile.product] * p.segments;      // (segments: of the same length)
                 const int k_end = (int)((long long)k_all * (tile.split + 1) / p.splits);
                 int k = (int)((long long)k_all * tile.split / p.splits);
-                if (first) {
-                    first = false;
-                    // weights on their way before the rows of the other operand are there
-                    const int ahead = p.early_b ? min(stages, k_end - k) : 0;
-                    for (int j = 0; j < ahead; ++j) {
-                        if (rank == 0) mbar_expect_tx(bar_full + 8 * j, bytes);
-                        load_b(tile, k + j, s_base + j * stage_bytes + C::A_BYTES, ff_first<CG>(bar_full + 8 * j));
+                // (what does not change from block to block is formed outside)
+                while (ok && k < k_end) {
+                    const int seg = p.segments > 1 && k >= p.kb[0], i = tile.product + seg, stop = p.segments > 1 && !seg ? min(k_end, p.kb[0]) : k_end;
+                    int kc = (k - seg * p.kb[0]) * C::BK;
+                    if (waits) {                // (as late as that: what comes before overlaps with the end of the kernel before this one)
+                        waits = false;
+                        pdl_wait();
+                        if (of_a) pdl_trigger();
                     }
-                    pdl_wait();
-                    pdl_trigger();
-                    for (int j = 0; j < ahead; ++j, ++k) {
-                        load_a(tile, k, s_base + j * stage_bytes, ff_first<CG>(bar_full + 8 * j));
-                        if (++s == stages) { s = 0; phase ^= 1; }
+                    if (of_a) {
+                        const CUtensorMap* map = &p.a[i];
+                        const int m0 = tile.m0 + rank * C::BM;
+                        for (; k < stop; ++k, kc += C::BK) {
+                            if (!(ok = mbar_wait<true>(bar_free + 8 * s, phase, abort_flag, p.dev_status, 81))) break;
+                            const uint32_t to = s_base + s * stage_bytes, full = ff_first<CG>(bar_full + 8 * s);
+                            if (rank == 0) mbar_expect_tx(bar_full + 8 * s, bytes);
+                            if (A_MN) {
+                                ff_load<CG>(to, map, m0, kc, full);
+                                ff_load<CG>(to + 8192, map, m0 + 64, kc, full);
+                            } else
+                                ff_load<CG>(to, map, kc, m0, full);
+                            if (++s == stages) { s = 0; phase ^= 1; }
+                        }
+                    } else {
+                        const CUtensorMap* map = EPI == FF_GATED ? &p.b[rank] : &p.b[i];
+                        const int n0 = tile.n0 + (EPI == FF_GATED ? 0 : rank * bn_own);
+                        for (; k < stop; ++k, kc += C::BK) {
+                            if (!(ok = mbar_wait<true>(bar_free + 8 * s, phase, abort_flag, p.dev_status, 88))) break;
+                            const uint32_t to = s_base + s * stage_bytes + C::A_BYTES, full = ff_first<CG>(bar_full + 8 * s);
+                            if (EPI == FF_GATED) {
+                                // g's columns in front of u's: the pair's first thread block holds Wg's rows, the second Wu's
+                                ff_load<CG>(to, map, kc, n0, full);
+                                if (CG == 1) ff_load<CG>(to + bn_out * C::BK * 2, &p.b[1], kc, n0, full);
+                            } else if (B_MN) {
+                                for (int x = 0; x < b_boxes; ++x) ff_load<CG>(to + x * 8192, map, n0 + 64 * x, kc, full);
+                            } else
+                                ff_load<CG>(to, map, kc, n0, full);
+                            if (++s == stages) { s = 0; phase ^= 1; }
+                        }
                     }
-                }
-                for (; k < k_end; ++k) {
-                    if (!(ok = mbar_wait<true>(bar_free + 8 * s, phase, abort_flag, p.dev_status, 81))) break;
-                    const uint32_t sA = s_base + s * stage_bytes, full = ff_first<CG>(bar_full + 8 * s);
-                    if (rank == 0) mbar_expect_tx(bar_full + 8 * s, bytes);
-                    load_a(tile, k, sA, full);
-                    load_b(tile, k, sA + C::A_BYTES, full);
-                    if (++s == stages) { s = 0; phase ^= 1; }
                 }
             }
             // every stage's MMAs are done before this thread block (whose memory the pair's MMAs read and signal) may leave
@@ -363,7 +366,7 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
             }
         }
     } else if (warp == C::WARP_MMA) {
-        // ================================================================= MMA issuer (warp-uniform, one elected lane issues)
+        // ================================================================= MMA issuer (one elected lane; the warp meets again behind the roles)
         constexpr uint32_t TYPE = std::is_same<T, bf16>::value ? 1u : 0u;
         const uint32_t idesc = (1u << 4) | (TYPE << 7) | (TYPE << 10) | ((A_MN ? 1u : 0u) << 15) | ((B_MN ? 1u : 0u) << 16) |
                                ((uint32_t)(p.bn >> 3) << 17) | ((uint32_t)(CG * C::BM >> 4) << 24);
@@ -371,39 +374,38 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
         const uint64_t db0 = smem_desc_sw128(s_base + C::A_BYTES, B_MN ? 8192 : 16, 1024);
         constexpr int A_STEP = (A_MN ? 2048 : 32) >> 4, B_STEP = (B_MN ? 2048 : 32) >> 4;
         const int b_half = (p.bn / CG * C::BK * 2) >> 4;            // (NB 2: bn / CG is a multiple of 64)
-        bool ok = rank == 0;
-        int s = 0, acc = 0;
-        uint32_t phase = 0, acc_phase = 1;
-        for (int t = tile_first; ok && t < n_tiles; t += tile_step) {
-            const FfTile tile = ff_tile(p, t, CG * C::BM, bn_out);
-            const int k_all = p.kb[tile.product] * p.segments;
-            const int n_kb = (int)((long long)k_all * (tile.split + 1) / p.splits) - (int)((long long)k_all * tile.split / p.splits);
-            if (!(ok = mbar_wait_warp<true>(bar_acc_free + 8 * acc, acc_phase, abort_flag, p.dev_status, 82))) break;
-            fence_after_sync();
-            for (int kb = 0; kb < n_kb; ++kb) {
-                if (!(ok = mbar_wait_warp<true>(bar_full + 8 * s, phase, abort_flag, p.dev_status, 83))) break;
-                fence_after_sync();
-                if (elect_one()) {
+        if (rank == 0 && elect_one()) {
+            bool ok = true;
+            int s = 0, acc = 0;
+            uint32_t phase = 0, acc_phase = 1;
+            for (int t = tile_first; ok && t < n_tiles; t += tile_step) {
+                const FfTile tile = ff_tile(p, t, CG * C::BM, bn_out);
+                const int k_all = p.kb[tile.product] * p.segments;
+                const int n_kb = (int)((long long)k_all * (tile.split + 1) / p.splits) - (int)((long long)k_all * tile.split / p.splits);
+                if (!(ok = mbar_wait<true>(bar_acc_free + 8 * acc, acc_phase, abort_flag, p.dev_status, 82))) break;
+                const uint32_t d = tmem + acc * acc_stride;
+                for (int kb = 0; kb < n_kb; ++kb) {
+                    if (!(ok = mbar_wait<true>(bar_full + 8 * s, phase, abort_flag, p.dev_status, 83))) break;
+                    fence_after_sync();
                     const uint64_t off = (uint64_t)((s * stage_bytes) >> 4);
 #pragma unroll
                     for (int ks = 0; ks < C::BK / 16; ++ks)
 #pragma unroll
                         for (int h = 0; h < NB; ++h)
-                            ff_mma<CG>(tmem + (acc + h) * acc_stride, da0 + off + ks * A_STEP, db0 + off + ks * B_STEP + h * b_half, idesc, kb > 0 || ks > 0);
+                            ff_mma<CG>(d + h * acc_stride, da0 + off + ks * A_STEP, db0 + off + ks * B_STEP + h * b_half, idesc, kb > 0 || ks > 0);
                     ff_commit<CG>(bar_free + 8 * s);
                     if (kb == n_kb - 1) ff_commit<CG>(bar_acc + 8 * acc);
+                    if (++s == stages) { s = 0; phase ^= 1; }
                 }
-                __syncwarp();
-                if (++s == stages) { s = 0; phase ^= 1; }
+                if (++acc == ACCS) { acc = 0; acc_phase ^= 1; }
             }
-            if (++acc == ACCS) { acc = 0; acc_phase ^= 1; }
         }
     } else {
         // ================================================================= epilogue: warps w and w + 4 share the accumulator rows 32 (w & 3) ...
         constexpr int CW = C::CW;
         const int quad = warp & 3, half = warp >> 2;
         const uint32_t lane_base = tmem + ((uint32_t)(quad * 32) << 16);
-        const uint32_t staging = s_staging + warp * C::STAGING;
+        const uint32_t set_bytes = p.set * C::BOX, staging = s_staging + warp * 2 * set_bytes;
         FfOut out = {staging, 0};
         int acc = 0;
         uint32_t acc_phase = 0;
@@ -423,7 +425,7 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
                     if (in_t < n_tiles) in_tile = ff_tile(p, in_t, CG * C::BM, bn_out);
                     continue;
                 }
-                const uint32_t b = in_bar + 8 * in_set, to = staging + in_set * C::SET * C::BOX;
+                const uint32_t b = in_bar + 8 * in_set, to = staging + in_set * set_bytes;
                 mbar_expect_tx(b, (EPI == FF_DHIDDEN ? 2 : 1) * C::BOX);
                 tma_load_2d(to, &p.in[0], col, row, b);
                 if (EPI == FF_DHIDDEN) tma_load_2d(to + C::BOX, &p.in[1], col, row, b);
@@ -433,6 +435,10 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
             }
         };
         const bool asks = EPI == FF_DHIDDEN || (EPI == FF_LINEAR && p.linear.has_residual && p.splits == 1);
+        if (lane == 0) {
+            tma_prefetch_map(&p.out[0]);
+            if (asks) tma_prefetch_map(&p.in[0]);
+        }
         if (EPI == FF_LINEAR || (asks && lane == 0)) pdl_wait();        // (LINEAR: all lanes read the parameters)
         if (asks && lane == 0) ask();
         for (int t = tile_first; t < n_tiles; t += tile_step) {
@@ -482,7 +488,7 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
 #pragma unroll
                     for (int j = 0; j < 16; ++j) before[j] = 0u;
                     const int set = use_n & 1;
-                    const uint32_t boxes = staging + set * C::SET * C::BOX;
+                    const uint32_t boxes = staging + set * set_bytes;
                     if (asks) {
                         ok = mbar_wait_warp<true>(in_bar + 8 * set, (use_n >> 1) & 1, abort_flag, p.dev_status, 87);
                         ++use_n;
@@ -550,7 +556,7 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
                 } else {
                     uint32_t u[16], h[16];
                     const int set = use_n & 1;
-                    const uint32_t boxes = staging + set * C::SET * C::BOX;
+                    const uint32_t boxes = staging + set * set_bytes;
                     ok = mbar_wait_warp<true>(in_bar + 8 * set, (use_n >> 1) & 1, abort_flag, p.dev_status, 85);
                     ++use_n;
                     if (!ok) { tmem_wait_ld(); break; }
