@@ -404,7 +404,7 @@ int linear_parts(const Device* d, const hf_linear_shape* g) {
 }
 
 template <typename T, int NT>
-hf_status launch_linear_rows(const FfRowsParams& p, int sms, cudaStream_t st) {
+hf_status launch_linear_rows(const LinearRowsParams& p, int sms, cudaStream_t st) {
     // 16 features a thread block where that keeps every multiprocessor busy, with half the threads; otherwise 8
     if (p.features >= 16 * 2 * sms) return launch_after(k_ff_rows<T, NT, true, 0, true>, dim3((p.features + 15) / 16), dim3(256), 0, st, p);
     return launch_after(k_ff_rows<T, NT, false, 0, true>, dim3((p.features + 7) / 8), dim3(512), 0, st, p);
@@ -465,7 +465,7 @@ hf_status hf_linear(const hf_linear_shape* g, const void* x, const void* weight,
     const long long M = g->rows, K = g->width, N = g->out_width;
     const LinearEpilogue e = {bias, gate, residual, pre, y, g->gate_stride, g->residual_stride, g->y_stride, N, linear_group(g), g->param_type == HF_F32, residual != nullptr};
     if (M <= FF_ROWS_MOST) {
-        FfRowsParams p = {x, weight, weight, nullptr, nullptr, nullptr, g->x_stride, 0, (int)M, (int)K, (int)N, e, g->act};
+        const LinearRowsParams p = {{x, weight, weight, nullptr, nullptr, nullptr, g->x_stride, 0, (int)M, (int)K, (int)N}, e, g->act};
         if (g->type == HF_BF16) return M <= 8 ? launch_linear_rows<bf16, 1>(p, d->sm_count, st) : launch_linear_rows<bf16, 2>(p, d->sm_count, st);
         return M <= 8 ? launch_linear_rows<__half, 1>(p, d->sm_count, st) : launch_linear_rows<__half, 2>(p, d->sm_count, st);
     }

@@ -191,6 +191,11 @@ template <typename T, int ACT> __device__ __forceinline__ void ff_hidden_row(con
     }
 }
 
+// A kernel's parameters come to a multiprocessor line by line, when they are first read, half a microsecond each: those of the epilogue are asked for while
+// the operands are on their way.
+__device__ __forceinline__ void linear_touch(const LinearEpilogue& e) {
+    asm volatile("" ::"l"(e.bias), "l"(e.y_stride), "r"(e.has_residual));
+}
 // Eight parameters of a linear layer, of T or float32, as floats.
 template <typename T> __device__ __forceinline__ void linear_params(const void* base, bool f32, long long at, float (&f)[8]) {
     if (f32) to_floats(load_vec<float, 8>(static_cast<const float*>(base) + at), f);
@@ -435,6 +440,7 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
             }
         };
         const bool asks = EPI == FF_DHIDDEN || (EPI == FF_LINEAR && p.linear.has_residual && p.splits == 1);
+        if constexpr (EPI == FF_LINEAR) linear_touch(p.linear);
         if (lane == 0) {
             tma_prefetch_map(&p.out[0]);
             if (asks) tma_prefetch_map(&p.in[0]);

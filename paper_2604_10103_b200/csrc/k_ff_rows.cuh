@@ -16,7 +16,9 @@ struct FfRowsParams {
     void* out; void* gate; void* up;                    // h or y; g, u (nullptr: not kept)
     long long x_stride, out_stride;
     int rows, contraction, features;
-    LinearEpilogue linear;                              // LINEAR
+};
+struct LinearRowsParams : FfRowsParams {                // (apart: as part of the feed-forward's they cost its two launches 1.4 us)
+    LinearEpilogue linear;
     int act;
 };
 
@@ -45,12 +47,12 @@ template <typename T> __device__ __forceinline__ void linear_one(const LinearEpi
 // NT: groups of 8 rows of x.  GATED: two products side by side, of two matrices or (LINEAR) of 16 features of one.  ACT: of GATED.
 template <typename T, int NT, bool GATED, int ACT, bool LINEAR = false>
 __global__ void __launch_bounds__(GATED ? 256 : 512, GATED ? 4 : 2)
-k_ff_rows(const FfRowsParams p) {
+k_ff_rows(const std::conditional_t<LINEAR, LinearRowsParams, FfRowsParams> p) {
     constexpr int WARPS = GATED ? 8 : 16, JB = GATED ? 6 : 8, MATS = GATED ? 2 : 1, OWN = LINEAR ? 8 * MATS : 8;
     __shared__ float s_sum[WARPS][MATS][8][8 * NT + 1];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int feature = blockIdx.x * OWN + g, blocks = (p.contraction + 31) / 32;
-    const bool on = feature < p.features, on1 = LINEAR ? feature + 8 < p.features : on;
+    const bool on = feature < p.features, on1 = feature + 8 < p.features;
     const T* w0 = static_cast<const T*>(p.w0) + (size_t)feature * p.contraction + 8 * t;
     const T* w1 = static_cast<const T*>(p.w1) + (size_t)(feature + (LINEAR ? 8 : 0)) * p.contraction + 8 * t;
     const T* x = static_cast<const T*>(p.x) + 8 * t;
@@ -59,8 +61,9 @@ k_ff_rows(const FfRowsParams p) {
     for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i) c[n][i] = 0.f;
-    bool waited = GATED || LINEAR;
-    if (waited) { pdl_wait(); pdl_trigger(); }          // (what the first product reads may be the previous kernel's)
+    constexpr bool FIRST = GATED || LINEAR;
+    if (FIRST) { pdl_wait(); pdl_trigger(); }           // (what the first product reads may be the previous kernel's)
+    bool waited = FIRST;
     for (int j0 = warp * JB; j0 < blocks || !waited; j0 += WARPS * JB) {
         uint4 a0[JB], a1[JB];
 #pragma unroll
@@ -68,9 +71,10 @@ k_ff_rows(const FfRowsParams p) {
             a0[i] = make_uint4(0, 0, 0, 0); a1[i] = a0[i];
             if (on && 32 * (j0 + i) + 8 * t < p.contraction) {
                 a0[i] = *reinterpret_cast<const uint4*>(w0 + 32 * (j0 + i));
-                if (GATED && on1) a1[i] = *reinterpret_cast<const uint4*>(w1 + 32 * (j0 + i));
+                if (GATED && (!LINEAR || on1)) a1[i] = *reinterpret_cast<const uint4*>(w1 + 32 * (j0 + i));
             }
         }
+        if constexpr (LINEAR) linear_touch(p.linear);
         if (!waited) { pdl_wait(); waited = true; }     // h is there; the weights above are no kernel's of this call
 #pragma unroll
         for (int i = 0; i < JB; ++i) {
