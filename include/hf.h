@@ -489,7 +489,7 @@ hf_status hf_gradient_norm(const hf_gradient* tensors, int n_tensors, float max_
  * and the element's place (256 first_block + its index): give every tensor blocks of its own.  A value that is not finite spoils its block of 256.
  * factor: device float, or NULL (1); where it is not finite the call changes nothing.  lr_at: device float that stands for lr, or NULL, so that a
  * captured step follows a schedule.  Pointers are aligned to their element, scales to 8 bytes; tensors whose pointers are all 16-byte aligned are
- * the fastest.  Two calls on the same tensors or the same counter must not run at the same time. */
+ * the fastest.  A tensor is in a call once; two calls on the same tensors or the same counter must not run at the same time. */
 typedef struct {
     int param_type;              /* HF_BF16 | HF_F32                    */
     int grad_type;               /* the parameters' type, or HF_F32     */

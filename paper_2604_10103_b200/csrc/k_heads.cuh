@@ -197,70 +197,103 @@ __device__ __forceinline__ void heads_team_sum(float (&v)[N], int team, int warp
         for (int n = 0; n < N; ++n) v[n] += s[(team * warps + w) * N + n];
 }
 
-// HB: heads of a lane.  Threads of a thread block: at most 128, or 512 (BIG).
+// A token's angles, looked up by the warp's lanes together (pairs lane, lane + 32, ...) into shared memory, cosines and then sines, from where each lane takes its
+// unit's.  One lookup a pair: each lane's own four would be as many again in every slice of heads.
+__device__ __forceinline__ void heads_look_up(const HeadsParams& p, int pairs, int b, int tok, float* s_angles) {
+    const int lane = threadIdx.x & 31;
+    const int* from = p.pos + b * p.pos_batch + (long long)tok * p.axes;
+    for (int pr = lane; pr < pairs; pr += 32) {
+        float c = 1.f, s = 0.f;
+        if (pr < p.n_pairs) {
+            int a = 0;
+            while (a + 1 < p.axes && pr >= p.first[a + 1]) ++a;
+            int at = from[a];
+            if ((unsigned)at >= (unsigned)p.extent[a]) {                // outside the table: no address is formed from it
+                atomicOr(p.dev_status, HF_DEV_BAD_INDEX_FLAG);
+                atomicExch(p.dev_status + 1, tok);
+                at = 0;
+            }
+            const int e = p.tab[a] + at * p.pairs[a] + pr - p.first[a];
+            c = p.cos_tab[e];
+            s = p.sin_tab[e];
+        }
+        s_angles[pr] = c;
+        s_angles[pairs + pr] = s;
+    }
+}
+
+// HB: heads of a lane.  Threads of a thread block: at most 128, or 512 (BIG).  The issue slots bound it with memory (4680 tokens of 12 + 24 heads of 128: 19.0 us): angles
+// looked up by each lane, addresses formed anew for each head and selections for pairs that are not rotated took 21.3.
 template <typename T, bool HALVES, bool WIDE, int HB, bool BIG>
 __global__ void __launch_bounds__(BIG ? 512 : 128)
 k_heads(const __grid_constant__ HeadsParams p) {
     __shared__ float s_sum[16];
+    __shared__ __align__(16) float s_angles[BIG ? 16 : 4][256];
     const int part = blockIdx.y, heads = p.heads[part];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, team = warp / p.warps, team_warp = warp - team * p.warps;
-    const long long row = (long long)blockIdx.x * p.teams + team, rows = (long long)p.batch * p.tokens;
+    const uint32_t row = blockIdx.x * (uint32_t)p.teams + team, rows = (uint32_t)p.batch * (uint32_t)p.tokens;
     const bool live = row < rows;
-    const int b = live ? (int)((uint32_t)row / (uint32_t)p.tokens) : 0, tok = live ? (int)row - b * p.tokens : 0;      // (rows fit 31 bits)
+    const int b = live ? (int)(row / (uint32_t)p.tokens) : 0, tok = live ? (int)(row - b * p.tokens) : 0;
     const HeadsLane<T, HALVES, WIDE> l(p, lane & (p.lanes - 1));
-    const bool on = live && l.on;
     const int per_warp = 32 / p.lanes, slices = p.warps * per_warp, slice = team_warp * per_warp + lane / p.lanes;
     const int before = part == 0 ? 0 : (part == 1 ? p.heads[0] : p.heads[0] + p.heads[1]);
-    const T* x = static_cast<const T*>(p.rows) + b * p.rows_b + tok * p.rows_t + (size_t)before * p.head_dim;
-    T* y = static_cast<T*>(p.t[part].p) + b * p.t[part].b + tok * p.t[part].t;
+    const T* x = static_cast<const T*>(p.rows) + b * p.rows_b + tok * p.rows_t + (before + slice) * p.head_dim;
+    T* y = static_cast<T*>(p.t[part].p) + b * p.t[part].b + tok * p.t[part].t + slice * p.t[part].h;
+    const int x_step = slices * p.head_dim;
+    const long long y_step = slices * p.t[part].h;
+    uint32_t mine = 0;                          // the lane's heads
+#pragma unroll
+    for (int k = 0; k < HB; ++k)
+        if (live && l.on && k * slices + slice < heads) mine |= 1u << k;
     Vec<T, 8> v[HB];
 #pragma unroll
-    for (int k = 0; k < HB; ++k) {
-        const int h = k * slices + slice;
+    for (int k = 0; k < HB; ++k, x += x_step) {
         const float zero[8] = {};
         from_floats(v[k], zero);
-        if (on && h < heads) v[k] = l.load(p, x + (size_t)h * p.head_dim);
+        if (mine >> k & 1) v[k] = l.load(p, x);
     }
     if (part == 2) {
 #pragma unroll
-        for (int k = 0; k < HB; ++k) {
-            const int h = k * slices + slice;
-            if (on && h < heads) l.store(p, y + h * p.t[2].h, v[k]);
-        }
+        for (int k = 0; k < HB; ++k, y += y_step)
+            if (mine >> k & 1) l.store(p, y, v[k]);
         return;
     }
-    const HeadsAngles angles(p, on ? l.unit : 1 << 20, b, tok);
+    const int pairs = 4 * p.lanes;
+    if (live) heads_look_up(p, pairs, b, tok, s_angles[warp]);
     const void* w = p.w[part];
     const int turned = heads_turned(p, l.unit);
+    const bool all_turned = 2 * p.n_pairs == p.head_dim && p.head_dim % 8 == 0;
     float all[1] = {0.f}, own[HB];
 #pragma unroll
     for (int k = 0; k < HB; ++k) {
         float f[8];
         heads_floats<HALVES>(v[k], f);
-        own[k] = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) own[k] = fmaf(f[i], f[i], own[k]);
+        vmul(f, f, f);
+        own[k] = vsum(f);
         all[0] += own[k];
     }
     if (p.over_width) {
         heads_team_sum(all, team, team_warp, p.warps, s_sum);
         all[0] = 1.f / sqrtf(all[0] / (float)(heads * p.head_dim) + p.eps);
     }
-    float f_w[8];
-    if (on && !p.over_width) l.weight(p, w, 0, f_w);
+    __syncwarp();
+    float c[4], s[4], f_w[8];
+    to_floats(load_vec<float, 4>(s_angles[warp] + 4 * l.unit), c);
+    to_floats(load_vec<float, 4>(s_angles[warp] + pairs + 4 * l.unit), s);
+    if (mine && !p.over_width) l.weight(p, w, 0, f_w);
 #pragma unroll
-    for (int k = 0; k < HB; ++k) {
-        const int h = k * slices + slice;
+    for (int k = 0; k < HB; ++k, y += y_step) {
         const float r = p.over_width ? all[0] : 1.f / sqrtf(heads_lanes_sum(own[k], p.lanes) / (float)p.head_dim + p.eps);
-        if (!on || h >= heads) continue;
+        if (!(mine >> k & 1)) continue;
         stay_packed(v[k]);
-        if (p.over_width) l.weight(p, w, h, f_w);
+        if (p.over_width) l.weight(p, w, k * slices + slice, f_w);
         float f[8];
         heads_floats<HALVES>(v[k], f);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = f[i] * r * f_w[i];
-        heads_turn<false>(angles.c, angles.s, turned, f);
-        l.store(p, y + h * p.t[part].h, f);
+        vmul(f, r);
+        vmul(f, f, f_w);
+        if (all_turned) heads_turn<false>(c, s, f);
+        else heads_turn<false>(c, s, turned, f);
+        l.store(p, y, f);
     }
 }
 
@@ -449,12 +482,12 @@ k_heads_bwd_ring(const __grid_constant__ HeadsParams p) {
         if (l.on && k * slices + slice < heads) mine |= 1u << k;
     struct Place { uint32_t row; int b, tok; } at0;
     at0.row = row0; at0.b = row0 < rows ? row0 / (uint32_t)p.tokens : 0; at0.tok = row0 < rows ? row0 - at0.b * p.tokens : 0;
+    const int step_b = (int)(step / (uint32_t)p.tokens), step_tok = (int)(step - step_b * (uint32_t)p.tokens);
     auto after = [&](const Place& a) {          // (past the end: it stays, for nothing)
         Place n = {a.row + step, a.b, a.tok};
         if (n.row < rows) {
-            uint32_t tok = (uint32_t)a.tok + step;
-            while (tok >= (uint32_t)p.tokens) { tok -= p.tokens; ++n.b; }
-            n.tok = (int)tok;
+            n.b += step_b; n.tok += step_tok;
+            if (n.tok >= p.tokens) { n.tok -= p.tokens; ++n.b; }
         }
         return n;
     };

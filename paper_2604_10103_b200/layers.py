@@ -420,8 +420,8 @@ def _norm_rope_workspace(dev, shape):
 
 def split_heads_norm_rope_backward(dq, dk, dv, qkv, q_weight, k_weight, pos, tables, eps=1e-6, over="head", pairing="adjacent"):
     """Gradients of `split_heads_norm_rope`: (dqkv contiguous, dq_weight, dk_weight float32).  dq, dk, dv: any strides with the features of a head contiguous."""
-    if dq.dim() != 4 or dk.dim() != 4:
-        _fail("dq, dk, dv are [batch, heads, tokens, head_dim]")
+    if dq.dim() != 4 or dk.dim() != 4 or qkv.dim() != 3:
+        _fail("dq, dk, dv are [batch, heads, tokens, head_dim], qkv [batch, tokens, (heads + 2 kv_heads) * head_dim]")
     W = qkv.shape[-1]
     dev, B, T, d, shape, cos, sin = _norm_rope(qkv, dq.shape[1], dk.shape[1], q_weight, k_weight, pos, tables, eps, over, pairing, (qkv.shape[1] * W, W))
     H, KV = dq.shape[1], dk.shape[1]

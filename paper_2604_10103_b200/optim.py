@@ -63,9 +63,9 @@ def gradient_norm(tensors, max_norm=float("inf")):
 class _Launch:
     """One call of the library: its parameters, and its table."""
 
-    def __init__(self, params, dtype, grad_dtype, device, table, head, counter):
+    def __init__(self, params, sizes, dtype, grad_dtype, device, table, head, counter):
         self.params, self.dtype, self.grad_dtype, self.device, self.table, self.head, self.counter = params, dtype, grad_dtype, device, table, head, counter
-        self.at, self.sizes, self.p, self.g = table.ctypes.data, [p.numel() for p in params], None, None
+        self.at, self.sizes, self.p, self.g = table.ctypes.data, sizes, None, None
 
     def look(self):
         """The parameters and gradients as they are now, into the table."""
@@ -138,6 +138,9 @@ class AdamW(torch.optim.Optimizer):
             _fail("all groups are given at construction: the state lies in one piece")
         super().add_param_group(group)
 
+    def __getstate__(self):
+        raise TypeError("the state lies in buffers that calls refer to: it is copied and stored by state_dict and load_state_dict")
+
     @torch.no_grad()
     def masters_from_parameters(self):
         """The masters of the parameters as they are now (after weights were loaded)."""
@@ -158,7 +161,7 @@ class AdamW(torch.optim.Optimizer):
         for r, p in zip(table, params):
             s = self.state[p]
             r[2:10] = [s["master"].data_ptr() if "master" in s else 0, s["m"].data_ptr(), s["v"].data_ptr(), s["scales"].data_ptr() if "scales" in s else 0,
-                       s["step"].data_ptr(), row[p][0], p.numel(), self._first_block[index[p]]]
+                       s["step"].data_ptr(), row[p][0], s["m"].numel(), self._first_block[index[p]]]
             r[10:].view(np.float64)[:] = row[p][1:]
         return table
 
@@ -169,7 +172,7 @@ class AdamW(torch.optim.Optimizer):
         for p in params:
             kinds.setdefault((p.dtype, p.grad.dtype, "master" in self.state[p], *of[p]), []).append(p)
         counter = self.buffers["steps"].data_ptr() + 4 * len(self._params)
-        return [_Launch(some, dtype, grad_dtype, self._device, self._rows(some), (_TYPES[dtype], _TYPES[grad_dtype], self.state_bits, self.seed, *map(float, betas), float(eps)),
+        return [_Launch(some, [self.state[p]["m"].numel() for p in some], dtype, grad_dtype, self._device, self._rows(some), (_TYPES[dtype], _TYPES[grad_dtype], self.state_bits, self.seed, *map(float, betas), float(eps)),
                         counter) for (dtype, grad_dtype, _, betas, eps), some in kinds.items()]
 
     def _settings(self):

@@ -122,6 +122,13 @@ def test_many_tokens():
     check(2, 1500, 3, 1, 40, F32, "head", "halves", (8, 4, 4))
 
 
+def test_many_batches_of_few_tokens():
+    """The walk over tokens passes several batches at a step."""
+    for T in (1, 3):
+        check(3001, T, 2, 1, 64, BF, "width", "adjacent", (12, 10, 10))
+        check(1700, T, 2, 2, 64, BF, "head", "halves", (12, 10, 10))
+
+
 @pytest.mark.parametrize("dtype,lead", [(BF, 8), (BF, 1), (F32, 3)])
 @pytest.mark.parametrize("over", ["head", "width"])
 def test_strides(dtype, lead, over):

@@ -313,6 +313,46 @@ def test_state_goes_out_and_comes_back(bits, tmp_path):
         optim.AdamW(other[:1], state_bits=bits).load_state_dict(saved["opt"])
 
 
+def test_a_copy_goes_by_the_state():
+    import copy
+
+    from paper_2604_10103_b200 import optim
+    params, _ = make([(50,)], F32)
+    opt = optim.AdamW(params)
+    with pytest.raises(TypeError, match="state_dict"):
+        copy.deepcopy(opt)
+    with pytest.raises(ValueError, match="construction"):
+        opt.add_param_group(dict(params=[torch.nn.Parameter(torch.zeros(3, device="cuda"))]))
+
+
+def test_what_a_step_refuses():
+    from paper_2604_10103_b200 import optim
+    params, _ = make([(50,), (4, 6)], F32)
+    opt = optim.AdamW(params, lr=0.1)
+    before = [p.detach().clone() for p in params]
+    for factor in (torch.tensor(1.0), torch.ones(2, device="cuda"), torch.tensor(1.0, device="cuda", dtype=torch.float64)):
+        with pytest.raises(ValueError):
+            opt.step(grad_factor=factor)
+    params[1].grad = torch.randn(6, 4, device="cuda").t()
+    with pytest.raises(ValueError, match="gradient"):
+        opt.step()
+    params[1].grad = None
+    params[0].data = torch.zeros(3, device="cuda")
+    params[0].grad = torch.zeros(3, device="cuda")
+    with pytest.raises(ValueError):
+        opt.step()
+    assert torch.equal(params[1].detach(), before[1]) and int(opt.state[params[1]]["step"]) == 0
+    for bad in (torch.nn.Parameter(torch.zeros(3, device="cuda").half()), torch.nn.Parameter(torch.zeros(4, 6, device="cuda").t())):
+        with pytest.raises(ValueError):
+            optim.AdamW([bad])
+    with pytest.raises(ValueError):
+        optim.gradient_norm([torch.zeros(4, 6, device="cuda").t()])
+    with pytest.raises(ValueError):
+        optim.gradient_norm([torch.zeros(4, device="cuda"), torch.zeros(4)])
+    with pytest.raises(ValueError):
+        optim.gradient_norm([torch.zeros(4, device="cuda", dtype=torch.float64)])
+
+
 def test_a_scheduler_drives_it():
     from paper_2604_10103_b200 import optim
     params, _ = make([(50,)], F32)
