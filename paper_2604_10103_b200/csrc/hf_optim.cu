@@ -8,8 +8,8 @@ using namespace hf_layers;
 
 namespace {
 
-// Tensors of a launch: as many as 32,764 bytes of parameters hold, or a table that is sent faster where there are few.
-constexpr int FEW = 32, MOST_ADAM = 300, MOST_NORM = 1200;
+// Tensors of a launch: as many as 32,764 bytes of parameters hold, or of two shorter tables, which are sent faster, where there are fewer (132 gradients: 52 us a call instead of 56).
+constexpr int FEW = 32, SOME_ADAM = 100, MOST_ADAM = 300, SOME_NORM = 160, MOST_NORM = 1200;
 constexpr long long MOST_CHUNKS = 0x7fffffff;
 
 // Thread blocks of a launch: chunks, up to what the multiprocessors hold at a time (KERNEL: a type that stands for the instantiation).
@@ -66,6 +66,7 @@ hf_status launch_adamw(const Device* d, const hf_adamw_step* g, const hf_adamw_t
 template <typename P, typename G, bool MASTER, bool BITS8>
 hf_status run_adamw(const Device* d, const hf_adamw_step* g, const hf_adamw_tensor* t, int n, cudaStream_t st) {
     if (n <= FEW) return launch_adamw<P, G, MASTER, BITS8, FEW>(d, g, t, n, st);
+    if (n <= SOME_ADAM) return launch_adamw<P, G, MASTER, BITS8, SOME_ADAM>(d, g, t, n, st);
     for (int i = 0; i < n; i += MOST_ADAM)
         HFL_TRY((launch_adamw<P, G, MASTER, BITS8, MOST_ADAM>(d, g, t + i, n - i < MOST_ADAM ? n - i : MOST_ADAM, st)));
     return HF_OK;
@@ -179,6 +180,9 @@ hf_status hf_gradient_norm(const hf_gradient* tensors, int n_tensors, float max_
     int all = 0, blocks;
     if (n_tensors <= FEW) {
         HFL_TRY(launch_grad_norm<FEW>(d, tensors, n_tensors, partials, &blocks, st));
+        all = blocks;
+    } else if (n_tensors <= SOME_NORM) {
+        HFL_TRY(launch_grad_norm<SOME_NORM>(d, tensors, n_tensors, partials, &blocks, st));
         all = blocks;
     } else
         for (int i = 0; i < n_tensors; i += MOST_NORM) {

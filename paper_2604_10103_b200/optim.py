@@ -46,7 +46,7 @@ def gradient_norm(tensors, max_norm=float("inf")):
             if not dense[i]:
                 _fail(f"tensors[{i}] has to be contiguous")
     try:
-        kinds = [_TYPES[k] for k in kinds]
+        kinds = [_TYPES[kinds[0]]] * n if kinds.count(kinds[0]) == n else [_TYPES[k] for k in kinds]
     except KeyError as e:
         _fail(f"a tensor is {e.args[0]}: bfloat16, float16 and float32 are taken")
     rows = [0] * (3 * n)
@@ -69,16 +69,21 @@ class _Launch:
 
     def look(self):
         """The parameters and gradients as they are now, into the table."""
-        params = self.params
+        params, n = self.params, len(self.params)
         grads = list(map(_grad, params))
-        g, p, n = list(map(_pointer, grads)), list(map(_pointer, params)), len(params)
-        for tensors, kind, name in ((grads, self.grad_dtype, "gradient"), (params, self.dtype, "parameter")):
-            if list(map(_numel, tensors)) != self.sizes or list(map(_type, tensors)).count(kind) != n or list(map(_where, tensors)).count(self.device) != n or not all(map(_dense, tensors)):
-                _fail(f"a {name}'s size, type, device or layout is not what it was: {kind}, contiguous, on device {self.device}, of the parameter's size is taken")
-        if p != self.p:
+        g, p = list(map(_pointer, grads)), list(map(_pointer, params))
+        if not (list(map(_numel, params)) == self.sizes == list(map(_numel, grads)) and list(map(_type, grads)).count(self.grad_dtype) == n and all(map(_dense, grads))):
+            self._differs()
+        # (what torch holds equal between a parameter and its gradient, and what does not change where a tensor stays, is looked at where one has moved)
+        if p != self.p or g != self.g:
+            if not (list(map(_type, params)).count(self.dtype) == n and all(map(_dense, params)) and {self.device} == set(map(_where, grads)) == set(map(_where, params))):
+                self._differs()
             self.table[:, 0] = self.p = p
-        if g != self.g:
             self.table[:, 1] = self.g = g
+
+    def _differs(self):
+        _fail(f"a parameter's or a gradient's size, type, device or layout is not what it was: {self.dtype}, contiguous, on device {self.device}, the gradient of the "
+              "parameter's size, is taken")
 
 
 class AdamW(torch.optim.Optimizer):
