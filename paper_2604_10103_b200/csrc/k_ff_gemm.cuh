@@ -20,9 +20,10 @@
 // cycles of MMAs for each 64 of the contraction, in which 32 KB are written into and 32 KB read out of each thread block's shared memory:
 // its 128 bytes a cycle.  So tiles of one thread block (96 KB in the same cycles) are slower the longer they run, what an epilogue moves
 // through shared memory stops the MMAs, and dW, whose contraction is long, has tiles of 256 x 512 (a quarter less).  us (TFLOP/s) alone: 4680
-// rows, width 1536, hidden 4096: g, u, h 80 (1470), y 50 (1180: 114 tiles of 256 x 256, 133 of 224, on 74 pairs), dh and its epilogue 73
+// rows, width 1536, hidden 4096: g, u, h 80 (1470), y 47 (1245: 114 tiles of 256 x 256, 133 of 224, on 74 pairs), dh and its epilogue 73
 // (810: 304 tiles, four rounds and eight tiles; see FF_DHIDDEN below), dx 96 (1230), dW 118 (1500); 32760 rows: dh 410 (1005), dx 560 (1470), dW 751
-// (1650).  In a loop the power limit takes a tenth off.
+// (1650).  In a loop the power limit takes a tenth off.  LINEAR, width 1536 to 6144: 4680 rows 67 us (1315), 32760 rows 467 (1325); 6144 to 1536 with gate and
+// residual 72.5 (1218).  Tiles of few columns are bound by the loop's own latency (a barrier's test, a copy's issue, an MMA's): 0.16 us a block of 64.
 #pragma once
 #include <cooperative_groups.h>
 #include "tc5_common.cuh"
@@ -279,7 +280,8 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
     uint8_t* bar_gen = s_gen + (bar0 - s_base);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar_gen + 160);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(bar_gen + 164);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const bool of_a = threadIdx.x >> 5 != C::WARP_TMA_B;                    // (of the two loaders, which are one role)
+    const int warp = of_a ? (int)(threadIdx.x >> 5) : C::WARP_TMA, lane = threadIdx.x & 31;
     const int rank = CG == 1 ? 0 : (int)(blockIdx.x & 1);                   // (clusters are two neighbouring thread blocks)
     const int bn_out = EPI == FF_GATED ? p.bn / 2 : NB * p.bn, bn_own = NB * p.bn / CG;
     constexpr int ACCS = 2 / NB;                        // accumulators (sets of them) in turn
@@ -302,10 +304,9 @@ k_ff_gemm(const __grid_constant__ FfGemmParams p) {
     // The kernel may have been launched while the one before it still runs: only the threads that read global memory themselves wait for
     // that, everything else follows from what they read.  The next kernel may be launched once this one has waited, so that what was
     // written before this one is there for it from the start (early_b).
-    if (warp == C::WARP_TMA || warp == C::WARP_TMA_B) {
+    if (warp == C::WARP_TMA) {
         // ================================================================= loaders, one of A and one of B: a copy's issue and a barrier's test take 200 cycles
         // together, which one thread's two copies a block would make the bound of tiles of few columns
-        const bool of_a = warp == C::WARP_TMA;
         if (lane == 0) {
             tma_prefetch_map(of_a ? &p.a[0] : &p.b[0]);        // (while the kernel before this one still runs)
             bool ok = true, waits = of_a || !p.early_b;        // (early_b: B's first blocks are on their way before A's rows are there)

@@ -18,7 +18,7 @@ struct LinearBwdParams {
 constexpr int LINEAR_BWD_WARPS = 8, LINEAR_BWD_BLOCKS = 3;          // (thread blocks of a multiprocessor)
 
 // grid: (groups x parts) x strips of 256 columns.  GATE: there is one (and its gradient may be asked for).  The arithmetic goes two columns an instruction: one by
-// one, and with the gate's part always formed, it took the issue slots whole (311 us instead of FIGURE_BWD for 32760 rows of 6144 bf16, gelu).
+// one, and with the gate's part always formed, it took the issue slots whole (311 us instead of 196, 6.2 TB/s, for 32760 rows of 6144 bf16, gelu).
 template <typename T, int ACT, bool GATE>
 __global__ void __launch_bounds__(32 * LINEAR_BWD_WARPS, LINEAR_BWD_BLOCKS)
 k_linear_bwd(const LinearBwdParams p) {

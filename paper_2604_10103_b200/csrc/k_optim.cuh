@@ -8,6 +8,8 @@
 // rounded up or down at random, up with the probability of what is cut off: their mean is right.  Rounded to the nearest, v would stand still:
 // a step changes it by a factor of 1 - b2, far less than half the distance of two neighbours.  The random bits are a hash of seed, step and place, so a repeated run gives the same bits.  v is rounded, not its
 // root, since the root's rounding would add its variance to v step after step.  A v > 0 becomes at least the smallest code (its step would be m / eps at 0).
+// 113 M elements, bf16 with masters: 529 us (6.0 TB/s, 92 % of the copy rate); 57 M elements in 8 bits: 182 us (5.0 TB/s: 71 instructions an element, and the loads'
+// latency); the norm of 28 M bf16 elements 8.4 us.
 #pragma once
 #include "k_vec.cuh"
 
