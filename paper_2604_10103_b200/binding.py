@@ -176,6 +176,24 @@ def lib() -> C.CDLL:
     return L
 
 
+_host = None
+
+
+def host() -> C.PyDLL:
+    """Load libhf_host.so (once), which looks over torch tensors for the optimizer's calls.  Raises if it has not been built."""
+    global _host
+    if _host is None:
+        import torch  # noqa: F401  (its libraries come first)
+        path = os.path.join(HERE, "libhf_host.so")
+        if not os.path.exists(path):
+            raise RuntimeError(f"{path} is missing: build it with `python -m paper_2604_10103_b200.build`")
+        h = C.PyDLL(path)
+        h.hf_host_gradients.argtypes = [C.py_object, C.c_int, C.c_void_p]
+        h.hf_host_parameters.argtypes = [C.py_object, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p]
+        _host = h
+    return _host
+
+
 def _check(status: int):
     if status != HF_OK:
         raise HFError(status, lib().hf_last_error().decode())

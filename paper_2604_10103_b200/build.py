@@ -1,13 +1,16 @@
-"""Build libhf.so in-tree with nvcc for sm_100a (cross-compiles without a GPU)."""
+"""Build libhf.so in-tree with nvcc for sm_100a (cross-compiles without a GPU), and libhf_host.so, which looks over torch tensors for the optimizer, with g++."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhf.so")
+HOST_LIB, HOST_SOURCE = os.path.join(HERE, "libhf_host.so"), os.path.join(CSRC, "host_tensors.cpp")
+HEADER = os.path.join(HERE, "..", "include", "hf.h")
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC", "-shared", "-cudart", "static",
@@ -19,27 +22,41 @@ def sources():
 
 
 def _deps():
-    return [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(HERE, "..", "include", "hf.h")]
+    return [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cu", ".cuh", ".h"))] + [HEADER]
+
+
+def _older(lib, deps) -> bool:
+    return not os.path.exists(lib) or any(os.path.getmtime(p) > os.path.getmtime(lib) for p in deps)
 
 
 def stale() -> bool:
-    if not os.path.exists(LIB):
-        return True
-    t = os.path.getmtime(LIB)
-    return any(os.path.getmtime(p) > t for p in _deps())
+    return _older(LIB, _deps()) or _older(HOST_LIB, [HOST_SOURCE, HEADER])
+
+
+def _run(cmd):
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError(f"{cmd[0]} failed:\n" + " ".join(cmd) + "\n" + res.stdout + res.stderr)
+    return res.stderr
+
+
+def _host_command():
+    import torch
+    root = os.path.dirname(torch.__file__)
+    include = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"]]
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+            *("-I" + p for p in include), HOST_SOURCE, "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-o", HOST_LIB]
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile every .cu under csrc/ into libhf.so; returns its path.  Raises on failure."""
-    if not force and not stale():
-        return LIB
-    nvcc = os.environ.get("NVCC", "nvcc")
-    cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + sources() + ["-o", LIB]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        raise RuntimeError("nvcc failed:\n" + " ".join(cmd) + "\n" + res.stdout + res.stderr)
-    if verbose:
-        sys.stderr.write(res.stderr)
+    """Compile every .cu under csrc/ into libhf.so (returns its path), and host_tensors.cpp into libhf_host.so.  Raises on failure."""
+    if force or _older(HOST_LIB, [HOST_SOURCE, HEADER]):
+        _run(_host_command())
+    if force or _older(LIB, _deps()):
+        nvcc = os.environ.get("NVCC", "nvcc")
+        told = _run([nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + sources() + ["-o", LIB])
+        if verbose:
+            sys.stderr.write(told)
     return LIB
 
 

@@ -1,0 +1,55 @@
+// What the optimizer's calls ask of many torch tensors, asked without Python between: 0.01 us a tensor instead of 0.3 (the norm of 132 gradients 17.7 us a
+// call instead of 51, a step over as many parameters 37 instead of 82).  (The one part that knows torch; the
+// library itself does not.)  Called with the interpreter's lock held.  Nothing is thrown through to the caller.
+#include <torch/csrc/autograd/python_variable.h>
+
+#include "../../include/hf.h"
+
+namespace {
+
+int kind_of(const at::Tensor& t) {
+    switch (t.scalar_type()) {
+        case at::kBFloat16: return HF_BF16;
+        case at::kHalf: return HF_F16;
+        case at::kFloat: return HF_F32;
+        default: return -1;
+    }
+}
+bool here(const at::Tensor& t, int device) { return t.layout() == at::kStrided && t.is_cuda() && t.get_device() == device && t.is_contiguous(); }
+
+}  // namespace
+
+extern "C" {
+
+// tensors: a list; rows: one hf_gradient for each.  0, or 1 + the place of the first that is not a contiguous tensor of a known type on the device.
+int hf_host_gradients(PyObject* tensors, int device, hf_gradient* rows) {
+    const Py_ssize_t n = PyList_GET_SIZE(tensors);
+    for (Py_ssize_t i = 0; i < n; ++i) try {
+        PyObject* o = PyList_GET_ITEM(tensors, i);
+        if (!THPVariable_Check(o)) return (int)i + 1;
+        const at::Tensor& t = THPVariable_Unpack(o);
+        const int kind = kind_of(t);
+        if (kind < 0 || !here(t, device)) return (int)i + 1;
+        rows[i] = {t.const_data_ptr(), t.numel(), kind};
+    } catch (...) { return (int)i + 1; }
+    return 0;
+}
+
+// params: a list of leaves; their pointers and their gradients' into rows.  0; 1 + the place of the first that is not, or whose gradient is not, a
+// contiguous tensor of that type on the device with sizes[i] elements; -1 - the place of the first without a gradient.
+int hf_host_parameters(PyObject* params, int device, int param_type, int grad_type, const int64_t* sizes, hf_adamw_tensor* rows) {
+    const Py_ssize_t n = PyList_GET_SIZE(params);
+    for (Py_ssize_t i = 0; i < n; ++i) try {
+        PyObject* o = PyList_GET_ITEM(params, i);
+        if (!THPVariable_Check(o)) return (int)i + 1;
+        const at::Tensor& p = THPVariable_Unpack(o);
+        const at::Tensor& g = p.grad();
+        if (!g.defined()) return -1 - (int)i;
+        if (kind_of(p) != param_type || kind_of(g) != grad_type || p.numel() != sizes[i] || g.numel() != sizes[i] || !here(p, device) || !here(g, device)) return (int)i + 1;
+        rows[i].p = p.mutable_data_ptr();
+        rows[i].g = g.const_data_ptr();
+    } catch (...) { return (int)i + 1; }
+    return 0;
+}
+
+}  // extern "C"

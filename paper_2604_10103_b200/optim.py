@@ -21,14 +21,12 @@ from .layers import _TYPES, _check, _current, _fail, _here, _lib, _stream
 _F32, _BF16 = torch.float32, torch.bfloat16
 _BLOCK = 256                                                # elements that share a scale; tensors start at multiples of it in the state's buffers
 _STEP = struct.Struct("@3iI3d2P").pack                      # hf_adamw_step
-# (mapped over all tensors: a call of a loop's body takes twice as long)
-_pointer, _numel, _where, _dense = torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.get_device, torch.Tensor.is_contiguous
-_type, _grad, _rate, _of_group = operator.attrgetter("dtype"), operator.attrgetter("grad"), operator.itemgetter("lr"), operator.itemgetter("lr", "weight_decay", "betas", "eps")
+_rate, _of_group = operator.itemgetter("lr"), operator.itemgetter("lr", "weight_decay", "betas", "eps")
 
 
 @functools.lru_cache(maxsize=256)
-def _norm_plan(dev, n):
-    return struct.Struct("@" + "Pqi4x" * n).pack, hf.hf_gradient_norm_workspace(n) // 8
+def _norm_workspace(dev, n):
+    return hf.hf_gradient_norm_workspace(n) // 8
 
 
 def gradient_norm(tensors, max_norm=float("inf")):
@@ -39,22 +37,16 @@ def gradient_norm(tensors, max_norm=float("inf")):
         _fail("no tensors")
     dev = _current("tensors[0]", tensors[0])
     n = len(tensors)
-    kinds, here, dense = list(map(_type, tensors)), list(map(_where, tensors)), list(map(_dense, tensors))
-    if here.count(dev) != n or not all(dense):
-        for i, t in enumerate(tensors):
-            _here(f"tensors[{i}]", t, dev)
-            if not dense[i]:
-                _fail(f"tensors[{i}] has to be contiguous")
-    try:
-        kinds = [_TYPES[kinds[0]]] * n if kinds.count(kinds[0]) == n else [_TYPES[k] for k in kinds]
-    except KeyError as e:
-        _fail(f"a tensor is {e.args[0]}: bfloat16, float16 and float32 are taken")
-    rows = [0] * (3 * n)
-    rows[0::3], rows[1::3], rows[2::3] = map(_pointer, tensors), map(_numel, tensors), kinds
-    pack, doubles = _norm_plan(dev, n)
+    rows = bytearray(24 * n)                                # hf_gradient
+    at = (hf.C.c_char * len(rows)).from_buffer(rows)
+    bad = hf.host().hf_host_gradients(tensors, dev, at)
+    if bad:
+        t = tensors[bad - 1]
+        _here(f"tensors[{bad - 1}]", t, dev)
+        _fail(f"tensors[{bad - 1}] is {t.dtype}{'' if t.is_contiguous() else ', not contiguous'}: contiguous bfloat16, float16 and float32 are taken")
     out = torch.empty(2, dtype=_F32, device=tensors[0].device)
-    ws = torch.empty(doubles, dtype=torch.float64, device=out.device)
-    status = _lib().hf_gradient_norm(pack(*rows), n, max_norm, out.data_ptr(), ws.data_ptr(), _stream())
+    ws = torch.empty(_norm_workspace(dev, n), dtype=torch.float64, device=out.device)
+    status = _lib().hf_gradient_norm(at, n, max_norm, out.data_ptr(), ws.data_ptr(), _stream())
     if status:
         _check(status)
     return out.unbind()
@@ -65,25 +57,17 @@ class _Launch:
 
     def __init__(self, params, sizes, dtype, grad_dtype, device, table, head, counter):
         self.params, self.dtype, self.grad_dtype, self.device, self.table, self.head, self.counter = params, dtype, grad_dtype, device, table, head, counter
-        self.at, self.sizes, self.p, self.g = table.ctypes.data, sizes, None, None
+        self.sizes = np.array(sizes, np.int64)
+        self.at, self.look_over = table.ctypes.data, (device, _TYPES[dtype], _TYPES[grad_dtype], self.sizes.ctypes.data, table.ctypes.data)
 
     def look(self):
-        """The parameters and gradients as they are now, into the table."""
-        params, n = self.params, len(self.params)
-        grads = list(map(_grad, params))
-        g, p = list(map(_pointer, grads)), list(map(_pointer, params))
-        if not (list(map(_numel, params)) == self.sizes == list(map(_numel, grads)) and list(map(_type, grads)).count(self.grad_dtype) == n and all(map(_dense, grads))):
-            self._differs()
-        # (what torch holds equal between a parameter and its gradient, and what does not change where a tensor stays, is looked at where one has moved)
-        if p != self.p or g != self.g:
-            if not (list(map(_type, params)).count(self.dtype) == n and all(map(_dense, params)) and {self.device} == set(map(_where, grads)) == set(map(_where, params))):
-                self._differs()
-            self.table[:, 0] = self.p = p
-            self.table[:, 1] = self.g = g
-
-    def _differs(self):
-        _fail(f"a parameter's or a gradient's size, type, device or layout is not what it was: {self.dtype}, contiguous, on device {self.device}, the gradient of the "
-              "parameter's size, is taken")
+        """The parameters and gradients as they are now, into the table; False where a gradient is missing."""
+        bad = hf.host().hf_host_parameters(self.params, *self.look_over)
+        if bad > 0:
+            p = self.params[bad - 1]
+            _fail(f"a parameter or its gradient is not what it was: {self.dtype} of {self.sizes[bad - 1]} elements, contiguous, on device {self.device}, and such a gradient, "
+                  f"are taken, not {p.dtype} {tuple(p.shape)} on {p.device} with {p.grad.dtype} {tuple(p.grad.shape)} on {p.grad.device}")
+        return not bad
 
 
 class AdamW(torch.optim.Optimizer):
@@ -175,10 +159,12 @@ class AdamW(torch.optim.Optimizer):
         of = {p: (g["betas"], g["eps"]) for g in self.param_groups for p in g["params"]}
         kinds = {}
         for p in params:
+            if p.dtype not in _TYPES or p.grad.dtype not in _TYPES:
+                _fail(f"a parameter is {p.dtype} with a gradient of {p.grad.dtype}: bfloat16 and float32 are taken")
             kinds.setdefault((p.dtype, p.grad.dtype, "master" in self.state[p], *of[p]), []).append(p)
         counter = self.buffers["steps"].data_ptr() + 4 * len(self._params)
-        return [_Launch(some, [self.state[p]["m"].numel() for p in some], dtype, grad_dtype, self._device, self._rows(some), (_TYPES[dtype], _TYPES[grad_dtype], self.state_bits, self.seed, *map(float, betas), float(eps)),
-                        counter) for (dtype, grad_dtype, _, betas, eps), some in kinds.items()]
+        return [_Launch(some, [self.state[p]["m"].numel() for p in some], dtype, grad_dtype, self._device, self._rows(some), (_TYPES[dtype],
+                        _TYPES[grad_dtype], self.state_bits, self.seed, *map(float, betas), float(eps)), counter) for (dtype, grad_dtype, _, betas, eps), some in kinds.items()]
 
     def _settings(self):
         """What the tables were made from, and step for step may change."""
@@ -214,12 +200,8 @@ class AdamW(torch.optim.Optimizer):
         _current("the first parameter", self._params[0])
         settings = self._settings()
         launches = self._plan if settings == self._planned else None
-        if launches is not None:
-            try:
-                for launch in launches:
-                    launch.look()
-            except TypeError:               # a gradient is missing
-                launches = None
+        if launches is not None and not all(launch.look() for launch in launches):
+            launches = None                 # (a gradient is missing)
         if launches is None:
             some = [p for p in self._params if p.grad is not None]
             launches = self._launches(some)

@@ -98,3 +98,22 @@ def test_python_refusals_without_a_device():
         optim.gradient_norm([])
     with pytest.raises(ValueError, match="not on the current CUDA device"):
         optim.gradient_norm([torch.zeros(3)])
+
+
+def test_what_the_look_over_finds():
+    """Without a device: which tensor is refused, and that nothing of it is needed for that."""
+    host = hf.host()
+    rows = (hf.hf_gradient * 3)()
+    assert host.hf_host_gradients([], 0, rows) == 0
+    assert host.hf_host_gradients([torch.zeros(3)], 0, rows) == 1                       # not on the device
+    assert host.hf_host_gradients([1.0], 0, rows) == 1                                  # no tensor
+    assert host.hf_host_gradients([torch.zeros(3).to_sparse()], 0, rows) == 1
+    table = (hf.hf_adamw_tensor * 2)()
+    sizes = (C.c_int64 * 2)(3, 3)
+    p = torch.nn.Parameter(torch.zeros(3))
+    assert host.hf_host_parameters([p], 0, 2, 2, sizes, table) == -1                    # no gradient
+    p.grad = torch.zeros(3)
+    assert host.hf_host_parameters([p], 0, 2, 2, sizes, table) == 1
+    assert host.hf_host_parameters([p, p], 0, 0, 2, sizes, table) == 1
+    assert host.hf_host_parameters([None], 0, 2, 2, sizes, table) == 1
+    assert not table[0].p and not table[0].g
