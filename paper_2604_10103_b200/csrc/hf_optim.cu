@@ -27,14 +27,13 @@ hf_status grid_for(const Device* d, F kernel, int threads, unsigned chunks, unsi
     return HF_OK;
 }
 
-// Elements of a chunk: 2048 (a block of 256 for each warp) where that gives every multiprocessor few of them, up to 8192 (what a chunk takes to look up is
-// then spread over four blocks a warp).
-constexpr int MOST_CHUNK = 8192;
-int adamw_chunk(const Device* d, const hf_adamw_tensor* t, int n) {
+// Elements of a chunk: 2048 (a block of 256 for each warp) where that gives every multiprocessor few of them, up to `most` (what a chunk takes to look up is
+// then spread over many blocks, and in 8 bits there is a next block to ask for; in 32 bits long chunks are no faster).
+int adamw_chunk(const Device* d, const hf_adamw_tensor* t, int n, int most) {
     long long all = 0;
     for (int i = 0; i < n; ++i) all += t[i].n;
     int chunk = 2048;
-    while (chunk < MOST_CHUNK && all / chunk > 16LL * d->sm_count) chunk *= 2;
+    while (chunk < most && all / chunk > 16LL * d->sm_count) chunk *= 2;
     return chunk;
 }
 
@@ -44,7 +43,7 @@ hf_status launch_adamw(const Device* d, const hf_adamw_step* g, const hf_adamw_t
     a.beta1 = (float)g->beta1; a.beta2 = (float)g->beta2; a.rest1 = (float)(1. - g->beta1); a.rest2 = (float)(1. - g->beta2);
     a.ln1 = std::log(g->beta1); a.ln2 = std::log(g->beta2); a.eps = (float)g->eps; a.seed = g->seed; a.factor = g->factor; a.counter = g->counter;
     a.n_tensors = 0; a.chunks = 0;
-    a.chunk = adamw_chunk(d, t, n);
+    a.chunk = adamw_chunk(d, t, n, BITS8 ? 65536 : 8192);
     for (int i = 0; i < n; ++i) {
         if (t[i].n == 0 && !t[i].step) continue;                        // (a tensor of no elements has its step counted)
         OptimTensor& o = a.t[a.n_tensors++];

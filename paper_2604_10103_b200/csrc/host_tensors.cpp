@@ -36,7 +36,8 @@ int hf_host_gradients(PyObject* tensors, int device, hf_gradient* rows) {
 }
 
 // params: a list of leaves; their pointers and their gradients' into rows.  0; 1 + the place of the first that is not, or whose gradient is not, a
-// contiguous tensor of that type on the device with sizes[i] elements; -1 - the place of the first without a gradient.
+// contiguous tensor of that type on the device with sizes[i] elements; -1 - the place of the first without a gradient.  The parameters count as written: a
+// backward pass that has saved one of them raises, as after torch's own steps.
 int hf_host_parameters(PyObject* params, int device, int param_type, int grad_type, const int64_t* sizes, hf_adamw_tensor* rows) {
     const Py_ssize_t n = PyList_GET_SIZE(params);
     for (Py_ssize_t i = 0; i < n; ++i) try {
@@ -46,6 +47,7 @@ int hf_host_parameters(PyObject* params, int device, int param_type, int grad_ty
         const at::Tensor& g = p.grad();
         if (!g.defined()) return -1 - (int)i;
         if (kind_of(p) != param_type || kind_of(g) != grad_type || p.numel() != sizes[i] || g.numel() != sizes[i] || !here(p, device) || !here(g, device)) return (int)i + 1;
+        if (!p.is_inference()) p.unsafeGetTensorImpl()->bump_version();
         rows[i].p = p.mutable_data_ptr();
         rows[i].g = g.const_data_ptr();
     } catch (...) { return (int)i + 1; }

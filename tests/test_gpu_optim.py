@@ -313,6 +313,16 @@ def test_state_goes_out_and_comes_back(bits, tmp_path):
         optim.AdamW(other[:1], state_bits=bits).load_state_dict(saved["opt"])
 
 
+def test_a_backward_pass_over_a_stepped_parameter_raises():
+    from paper_2604_10103_b200 import optim
+    params, _ = make([(50,)], F32)
+    opt = optim.AdamW(params)
+    y = (params[0] * params[0]).sum()
+    opt.step()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+
+
 def test_a_copy_goes_by_the_state():
     import copy
 
