@@ -118,7 +118,17 @@ class AdamW(torch.optim.Optimizer):
             if ma is not None:
                 s["master"] = self.buffers["master"][ma:ma + n].view(p.shape)
         self._device, self._first_block = dev, [a // _BLOCK for a in starts]
-        self._plan, self._planned = None, None
+        self._index, self._plan, self._planned = {p: i for i, p in enumerate(self._params)}, None, None
+        # the library's table (hf_adamw_tensor) without what changes from step to step
+        first, buffers = np.array(starts, np.int64), {k: b.data_ptr() for k, b in self.buffers.items() if b is not None}
+        self._table = np.zeros((len(starts), 12), np.int64)
+        if masters:
+            self._table[:, 2] = [0 if ma is None else buffers["master"] + 4 * ma for ma in master_at]
+        self._table[:, 3], self._table[:, 4] = (buffers[k] + first * (1 if small else 4) for k in ("m", "v"))
+        if small:
+            self._table[:, 5] = buffers["scales"] + first // _BLOCK * 8
+        self._table[:, 6] = buffers["steps"] + 4 * np.arange(len(starts))
+        self._table[:, 8], self._table[:, 9] = [p.numel() for p in self._params], first // _BLOCK
         self.masters_from_parameters()
         self._made = True
 
@@ -133,38 +143,34 @@ class AdamW(torch.optim.Optimizer):
     @torch.no_grad()
     def masters_from_parameters(self):
         """The masters of the parameters as they are now (after weights were loaded)."""
-        for p in self._params:
-            master = self.state[p].get("master")
-            if master is not None:
-                master.copy_(p)
+        pairs = [(self.state[p]["master"], p) for p in self._params if "master" in self.state[p]]
+        if pairs:
+            torch._foreach_copy_(*map(list, zip(*pairs)))
 
     def _rows(self, params):
         """The library's table of these parameters, without their gradients: int64 [n, 12], doubles in the last two columns."""
-        row = {}
+        table = self._table[[self._index[p] for p in params]]
+        rates = {}
         for g in self.param_groups:
             lr = g["lr"]
+            at = (lr.data_ptr(), 0.0) if isinstance(lr, torch.Tensor) else (0, float(lr))
             for p in g["params"]:
-                row[p] = (lr.data_ptr() if isinstance(lr, torch.Tensor) else 0, 0.0 if isinstance(lr, torch.Tensor) else float(lr), float(g["weight_decay"]))
-        table = np.zeros((len(params), 12), np.int64)
-        index = {p: i for i, p in enumerate(self._params)}
-        for r, p in zip(table, params):
-            s = self.state[p]
-            r[2:10] = [s["master"].data_ptr() if "master" in s else 0, s["m"].data_ptr(), s["v"].data_ptr(), s["scales"].data_ptr() if "scales" in s else 0,
-                       s["step"].data_ptr(), row[p][0], s["m"].numel(), self._first_block[index[p]]]
-            r[10:].view(np.float64)[:] = row[p][1:]
+                rates[p] = (*at, float(g["weight_decay"]))
+        table[:, 7] = [rates[p][0] for p in params]
+        table[:, 10:].view(np.float64)[:] = [rates[p][1:] for p in params]
         return table
 
     def _launches(self, params):
         """The calls that a step over these parameters takes: those of one type, with or without masters, with the same betas and eps, together."""
-        of = {p: (g["betas"], g["eps"]) for g in self.param_groups for p in g["params"]}
+        of = {p: (tuple(map(float, g["betas"])), float(g["eps"])) for g in self.param_groups for p in g["params"]}
         kinds = {}
         for p in params:
             if p.dtype not in _TYPES or p.grad.dtype not in _TYPES:
                 _fail(f"a parameter is {p.dtype} with a gradient of {p.grad.dtype}: bfloat16 and float32 are taken")
             kinds.setdefault((p.dtype, p.grad.dtype, "master" in self.state[p], *of[p]), []).append(p)
         counter = self.buffers["steps"].data_ptr() + 4 * len(self._params)
-        return [_Launch(some, [self.state[p]["m"].numel() for p in some], dtype, grad_dtype, self._device, self._rows(some), (_TYPES[dtype],
-                        _TYPES[grad_dtype], self.state_bits, self.seed, *map(float, betas), float(eps)), counter) for (dtype, grad_dtype, _, betas, eps), some in kinds.items()]
+        return [_Launch(some, self._table[[self._index[p] for p in some], 8], dtype, grad_dtype, self._device, self._rows(some), (_TYPES[dtype],
+                        _TYPES[grad_dtype], self.state_bits, self.seed, *betas, eps), counter) for (dtype, grad_dtype, _, betas, eps), some in kinds.items()]
 
     def _settings(self):
         """What the tables were made from, and step for step may change."""
