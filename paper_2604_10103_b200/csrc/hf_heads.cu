@@ -7,7 +7,7 @@ using namespace hf_layers;
 namespace {
 
 // How a token's part is laid out over lanes: see k_heads.cuh.
-struct HeadsPlan { int lanes, warps, teams, per_lane, threads; bool big; };
+struct HeadsPlan { int lanes, warps[3], teams[3], per_lane, threads; bool big; };
 
 hf_status heads_check(const hf_heads_shape* g) {
     if (g == nullptr) return fail(HF_ERR_INVALID_ARG, "shape is null");
@@ -47,20 +47,24 @@ HeadsPlan heads_plan(const hf_heads_shape* g, bool wide) {
     p.lanes = 1;
     while (8 * p.lanes < g->head_dim) p.lanes *= 2;
     const int per_warp = 32 / p.lanes, full = g->type == HF_F32 ? 4 : 6;
-    auto warps = [&](int most) { return (g->heads + per_warp * most - 1) / (per_warp * most); };
-    p.big = !wide || warps(full) > 4;
-    p.per_lane = p.big ? 4 : (warps(2) == 1 ? 2 : full);
-    p.warps = warps(p.per_lane);
-    p.teams = p.warps >= 4 ? 1 : 4 / p.warps;
-    p.threads = 32 * p.warps * p.teams;
+    auto warps = [&](int heads, int most) { return (heads + per_warp * most - 1) / (per_warp * most); };
+    p.big = !wide || warps(g->heads, full) > 4;
+    p.per_lane = p.big ? 4 : (warps(g->heads, 2) == 1 ? 2 : full);
+    const int all = warps(g->heads, p.per_lane), block = all >= 4 ? all : 4 / all * all;       // warps of a thread block
+    for (int i = 0; i < 3; ++i) {               // (shared key heads take fewer, so a thread block takes more tokens of theirs)
+        p.warps[i] = warps(i ? g->kv_heads : g->heads, p.per_lane);
+        p.teams[i] = block / p.warps[i];
+    }
+    p.threads = 32 * block;
     return p;
 }
 // Backward: thread blocks for q, k, v, by the time that they take (a head of v, which is copied, a quarter of one of q; by what they move it would be two
 // thirds: 161 us instead of 144 for 32760 tokens of 12 + 24 heads of 128).
 void heads_blocks(const hf_heads_shape* g, const HeadsPlan& n, int sms, int (&blocks)[3]) {
-    const long long rows = (long long)g->batch * g->tokens, all = (rows + n.teams - 1) / n.teams, total = (long long)sms * ((n.big ? 512 : 256) / n.threads);
+    const long long rows = (long long)g->batch * g->tokens, total = (long long)sms * ((n.big ? 512 : 256) / n.threads);
     const long long part[3] = {4LL * g->heads, 4LL * g->kv_heads, 1LL * g->kv_heads}, sum = part[0] + part[1] + part[2];
     for (int i = 0; i < 3; ++i) {           // (rounded down: one thread block too many would wait for the others' end)
+        const long long all = (rows + n.teams[i] - 1) / n.teams[i];
         long long b = total * part[i] / sum;
         if (b > all) b = all;
         blocks[i] = b < 1 ? 1 : (int)b;
@@ -72,7 +76,7 @@ template <typename T, bool HALVES, bool WIDE, int HB, bool BIG>
 hf_status launch_heads(const Device* d, const HeadsParams& p, const HeadsPlan& n, bool backward, int smem, cudaStream_t st) {
     if (!backward) {
         const long long rows = (long long)p.batch * p.tokens;
-        k_heads<T, HALVES, WIDE, HB, BIG><<<dim3((unsigned)((rows + n.teams - 1) / n.teams), 3), n.threads, 0, st>>>(p);
+        k_heads<T, HALVES, WIDE, HB, BIG><<<dim3((unsigned)((rows + n.teams[0] - 1) / n.teams[0]), 3), n.threads, 0, st>>>(p);
     } else {
         struct Key {};
         const unsigned grid = p.blocks[0] + p.blocks[1] + p.blocks[2];
@@ -110,6 +114,10 @@ hf_status launch_heads(const Device* d, const hf_heads_shape* g, const HeadsPara
     return halves ? launch_heads<float, true>(d, p, n, wide, backward, smem, st) : launch_heads<float, false>(d, p, n, wide, backward, smem, st);
 }
 
+void heads_layout(HeadsParams* p, const HeadsPlan& n) {
+    p->lanes = n.lanes;
+    for (int i = 0; i < 3; ++i) { p->warps[i] = n.warps[i]; p->teams[i] = n.teams[i]; }
+}
 // Parameters of both directions, and whether 16-byte accesses fit everywhere.
 hf_status heads_params(const hf_heads_shape* g, const hf_heads_tensor* t, const void* rows, void* drows, const void* qw, const void* kw,
                        const float* cos_tab, const float* sin_tab, const int32_t* pos, HeadsParams* p, bool* wide) {
@@ -156,7 +164,8 @@ hf_status hf_split_heads_norm_rope(const hf_heads_shape* g, const void* rows, co
     const Device* d;
     HFL_TRY(current_device(&d));
     const HeadsPlan n = heads_plan(g, wide);
-    p.lanes = n.lanes; p.warps = n.warps; p.teams = n.teams; p.dev_status = d->status;
+    heads_layout(&p, n);
+    p.dev_status = d->status;
     return launch_heads(d, g, p, n, wide, false, 0, (cudaStream_t)stream);
 }
 
@@ -196,7 +205,8 @@ hf_status hf_split_heads_norm_rope_backward(const hf_heads_shape* g, const hf_he
     const Device* d;
     HFL_TRY(current_device(&d));
     const HeadsPlan n = heads_plan(g, wide);
-    p.lanes = n.lanes; p.warps = n.warps; p.teams = n.teams; p.dev_status = d->status; p.partials = static_cast<float*>(workspace);
+    heads_layout(&p, n);
+    p.dev_status = d->status; p.partials = static_cast<float*>(workspace);
     heads_blocks(g, n, d->sm_count, p.blocks);
     HFL_TRY(launch_heads(d, g, p, n, wide, true, wq * (int)sizeof(float), st));
     if (!dq_weight && !dk_weight) return HF_OK;

@@ -26,7 +26,7 @@ struct HeadsParams {
     int first[4], pairs[4], extent[4], tab[4];
     int axes, n_pairs;
     int batch, tokens, head_dim, heads[3];
-    int lanes, warps, teams;                // of a unit's heads: L; of a team: W; teams of a thread block
+    int lanes, warps[3], teams[3];          // of a unit's heads: L; for each of the three, warps of a team W and teams of a thread block (warps behind them idle)
     int blocks[3];                          // backward: thread blocks for each of the three
     float* partials;                        // backward: [thread blocks of q and k][row of the weight]
     int* dev_status;
@@ -230,12 +230,13 @@ k_heads(const __grid_constant__ HeadsParams p) {
     __shared__ float s_sum[16];
     __shared__ __align__(16) float s_angles[BIG ? 16 : 4][256];
     const int part = blockIdx.y, heads = p.heads[part];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, team = warp / p.warps, team_warp = warp - team * p.warps;
-    const uint32_t row = blockIdx.x * (uint32_t)p.teams + team, rows = (uint32_t)p.batch * (uint32_t)p.tokens;
-    const bool live = row < rows;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = p.warps[part], team = warp / warps, team_warp = warp - team * warps;
+    const uint32_t row = blockIdx.x * (uint32_t)p.teams[part] + team, rows = (uint32_t)p.batch * (uint32_t)p.tokens;
+    if (blockIdx.x * (uint32_t)p.teams[part] >= rows) return;           // (the grid is for the part of fewest teams)
+    const bool live = row < rows && team < p.teams[part];
     const int b = live ? (int)(row / (uint32_t)p.tokens) : 0, tok = live ? (int)(row - b * p.tokens) : 0;
     const HeadsLane<T, HALVES, WIDE> l(p, lane & (p.lanes - 1));
-    const int per_warp = 32 / p.lanes, slices = p.warps * per_warp, slice = team_warp * per_warp + lane / p.lanes;
+    const int per_warp = 32 / p.lanes, slices = warps * per_warp, slice = team_warp * per_warp + lane / p.lanes;
     const int before = part == 0 ? 0 : (part == 1 ? p.heads[0] : p.heads[0] + p.heads[1]);
     const T* x = static_cast<const T*>(p.rows) + b * p.rows_b + tok * p.rows_t + (before + slice) * p.head_dim;
     T* y = static_cast<T*>(p.t[part].p) + b * p.t[part].b + tok * p.t[part].t + slice * p.t[part].h;
@@ -273,7 +274,7 @@ k_heads(const __grid_constant__ HeadsParams p) {
         all[0] += own[k];
     }
     if (p.over_width) {
-        heads_team_sum(all, team, team_warp, p.warps, s_sum);
+        heads_team_sum(all, team, team_warp, warps, s_sum);
         all[0] = 1.f / sqrtf(all[0] / (float)(heads * p.head_dim) + p.eps);
     }
     __syncwarp();
@@ -314,7 +315,7 @@ __device__ __forceinline__ void heads_weight_sum(const HeadsParams& p, const Hea
         for (int i = 0; i < 8; ++i)
             for (int o = p.lanes; o < 32; o <<= 1) acc[0][i] += __shfl_xor_sync(0xffffffffu, acc[0][i], o);
     }
-    for (int turn_of = 0; turn_of < (p.over_width ? p.teams : (int)blockDim.x / 32); ++turn_of) {
+    for (int turn_of = 0; turn_of < (p.over_width ? p.teams[part] : (int)blockDim.x / 32); ++turn_of) {
         __syncthreads();
         if (turn_of != (p.over_width ? team : warp) || !l.on || (!p.over_width && lane >= p.lanes)) continue;
 #pragma unroll
@@ -341,11 +342,11 @@ k_heads_bwd(const __grid_constant__ HeadsParams p) {
     int part = 0, block = blockIdx.x;
     while (part < 2 && block >= p.blocks[part]) block -= p.blocks[part++];
     const int heads = p.heads[part];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, team = warp / p.warps, team_warp = warp - team * p.warps;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = p.warps[part], teams = p.teams[part], team = warp / warps, team_warp = warp - team * warps;
     const HeadsLane<T, HALVES, WIDE> l(p, lane & (p.lanes - 1));
-    const int per_warp = 32 / p.lanes, slices = p.warps * per_warp, slice = team_warp * per_warp + lane / p.lanes;
+    const int per_warp = 32 / p.lanes, slices = warps * per_warp, slice = team_warp * per_warp + lane / p.lanes;
     const int before = part == 0 ? 0 : (part == 1 ? p.heads[0] : p.heads[0] + p.heads[1]);
-    const long long rows = (long long)p.batch * p.tokens, step = (long long)p.blocks[part] * p.teams;
+    const long long rows = (long long)p.batch * p.tokens, step = (long long)p.blocks[part] * teams;
     const void* w = part < 2 ? p.w[part] : nullptr;
     float acc[HB][8];
 #pragma unroll
@@ -356,8 +357,8 @@ k_heads_bwd(const __grid_constant__ HeadsParams p) {
     if (l.on && !p.over_width) l.weight(p, w, 0, f_w);
     const int turned = heads_turned(p, l.unit);
     int turn = 0;
-    for (long long row0 = (long long)block * p.teams; row0 < rows; row0 += step, turn ^= 1) {       // (the teams walk in step)
-        const long long row = row0 + team;
+    for (long long row0 = (long long)block * teams; row0 < rows; row0 += step, turn ^= 1) {         // (the teams walk in step)
+        const long long row = team < teams ? row0 + team : rows;
         const bool on = row < rows && l.on;
         const int b = row < rows ? (int)((uint32_t)row / (uint32_t)p.tokens) : 0, tok = row < rows ? (int)row - b * p.tokens : 0;
         const T* x = static_cast<const T*>(p.rows) + b * p.rows_b + tok * p.rows_t + (size_t)before * p.head_dim;
@@ -406,7 +407,7 @@ k_heads_bwd(const __grid_constant__ HeadsParams p) {
         }
         float r = 0.f, c = 0.f;
         if (p.over_width) {
-            heads_team_sum(all, team, team_warp, p.warps, s_sum[turn]);
+            heads_team_sum(all, team, team_warp, warps, s_sum[turn]);
             const float n = (float)(heads * p.head_dim);
             r = 1.f / sqrtf(all[0] / n + p.eps);
             c = all[1] * r / n;                 // mean(g w x r)
@@ -465,16 +466,16 @@ k_heads_bwd_ring(const __grid_constant__ HeadsParams p) {
     int part = 0, block = blockIdx.x;
     while (part < 2 && block >= p.blocks[part]) block -= p.blocks[part++];
     const int heads = p.heads[part], units = p.head_dim / 8;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, team = warp / p.warps, team_warp = warp - team * p.warps;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = p.warps[part], teams = p.teams[part], team = warp / warps, team_warp = warp - team * warps;
     const HeadsLane<T, HALVES, true> l(p, lane & (p.lanes - 1));
-    const int per_warp = 32 / p.lanes, slices = p.warps * per_warp, slice = team_warp * per_warp + lane / p.lanes;
+    const int per_warp = 32 / p.lanes, slices = warps * per_warp, slice = team_warp * per_warp + lane / p.lanes;
     const int before = part == 0 ? 0 : (part == 1 ? p.heads[0] : p.heads[0] + p.heads[1]);
-    const uint32_t rows = (uint32_t)p.batch * (uint32_t)p.tokens, step = (uint32_t)p.blocks[part] * (uint32_t)p.teams;
+    const uint32_t rows = (uint32_t)p.batch * (uint32_t)p.tokens, step = (uint32_t)p.blocks[part] * (uint32_t)teams;
     const HeadsTensor dy_of = p.t[part];
     const T* dy = static_cast<const T*>(dy_of.p);
     const T* x = static_cast<const T*>(p.rows) + (size_t)before * p.head_dim;
     T* dx = static_cast<T*>(p.drows) + (size_t)before * p.head_dim;
-    const uint32_t row0 = (uint32_t)block * p.teams + team;
+    const uint32_t row0 = team < teams ? (uint32_t)block * teams + team : rows;
     // a lane's heads, and where the token of a row is: rows come in steps, so without a division
     uint32_t mine = 0;
 #pragma unroll
@@ -620,7 +621,7 @@ k_heads_bwd_ring(const __grid_constant__ HeadsParams p) {
     int set = 0, set_ahead = SETS - 1, turn = 0;
     const float inv = 1.f / (float)(WIDTH ? heads * p.head_dim : p.head_dim);
     // (the teams walk in step: as many rounds for each)
-    for (uint32_t first = (uint32_t)block * p.teams; first < rows; first += step, turn ^= 1) {
+    for (uint32_t first = (uint32_t)block * teams; first < rows; first += step, turn ^= 1) {
         __syncwarp();                           // (the angles of the round before have been read)
         ask(ahead, set_ahead);
         ahead = after(ahead);
@@ -661,7 +662,7 @@ k_heads_bwd_ring(const __grid_constant__ HeadsParams p) {
                 vfma(s2, w, f, s2);
             }
             float all[2] = {vsum(s1), vsum(s2)};
-            heads_team_sum(all, team, team_warp, p.warps, s_sum[turn]);
+            heads_team_sum(all, team, team_warp, warps, s_sum[turn]);
             const float r = 1.f / sqrtf(all[0] * inv + p.eps), c = all[1] * r * inv;
 #pragma unroll
             for (int k = 0; k < HB; ++k, to += x_step) {

@@ -109,6 +109,12 @@ def test_heads_widths_and_types(B, T, H, KV, d, pairs, dtype):
         check(B, T, H, KV, d, dtype, over, pairing, pairs)
 
 
+@pytest.mark.parametrize("H,KV,d,dtype", [(30, 20, 128, BF), (130, 70, 64, F32), (22, 14, 128, HALF), (9, 7, 250, BF)])
+def test_shared_key_heads_that_leave_warps_idle(H, KV, d, dtype):
+    for over, pairing in (("width", "adjacent"), ("head", "halves")):
+        check(2, 45, H, KV, d, dtype, over, pairing, (8, 4, 4))
+
+
 @pytest.mark.parametrize("over", ["head", "width"])
 def test_weights_in_float32_and_none(over):
     check(2, 29, 6, 3, 64, BF, over, "adjacent", (12, 10, 10), wtype=F32)

@@ -373,7 +373,7 @@ def test_a_scheduler_drives_it():
         old = params[0].detach().clone()
         opt.step()
         schedule.step()
-        moves.append(float((params[0] - old).abs().max()))
+        moves.append(float((params[0].detach() - old).abs().max()))
     # (a constant gradient's quotient is 1 in each step, up to eps and float32)
     assert all(abs(m - want) < 1e-4 for m, want in zip(moves, (1.0, 0.5, 0.25)))
 
