@@ -91,7 +91,7 @@ def _rows(name, t):
             _fail(f"{name}: the leading axes have no common stride")
     rows = t.shape[0]
     stride, one = t.stride()
-    if one != 1 and width > 1:
+    if one != 1 and width > 1 and rows:         # (of no rows: whatever it says)
         _fail(f"{name}: the last axis has to be contiguous")
     return rows, width, stride if rows > 1 else width
 
@@ -306,8 +306,8 @@ def split_heads_rope_backward(dq, dk, dv, pos, tables, pairing="adjacent"):
 
 
 def _features_dense(t):
-    """t with the features of a head contiguous; its other axes may lie as they do."""
-    return t if t.stride(-1) == 1 else t.contiguous()
+    """t with the features of a head contiguous; its other axes may lie as they do.  (A copy: `contiguous` keeps an expanded tensor of no elements as it is.)"""
+    return t if t.stride(-1) == 1 else t.clone(memory_format=torch.contiguous_format)
 
 
 class _RopeAxes(torch.autograd.Function):
