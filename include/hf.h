@@ -461,7 +461,7 @@ hf_status hf_linear(const hf_linear_shape* shape, const void* x, const void* wei
 /* dp = dy gate_g act'(pre),  dx = dp W,  dW = dp^T x,  dbias = sum of dp over the rows,  dgate_g = sum of dy act(pre) over the group's rows.  dp is rounded
  * to the type for the two products, and not for the sums (f16: as hf_gated_ff_backward says of dg).  pre: what the forward returned; not read with
  * HF_ACT_NONE and without gate.  dx [rows, width], dweight: the type, contiguous; dbias [out_width], dgate [groups, out_width]: float, contiguous;
- * written, each may be NULL.  (The residual's gradient is dy.) */
+ * written, each may be NULL.  (The residual's gradient is dy.)  Of no rows: zeros; with rows_per_group > 0 there are then no rows of dgate. */
 hf_status hf_linear_backward(const hf_linear_shape* shape, const void* dy, const void* x, const void* weight, const void* pre, const void* gate,
                              void* dx, void* dweight, float* dbias, float* dgate, void* workspace, void* stream);
 

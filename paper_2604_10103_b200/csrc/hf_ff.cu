@@ -491,9 +491,10 @@ hf_status hf_linear_backward(const hf_linear_shape* g, const void* dy, const voi
     const cudaStream_t st = (cudaStream_t)stream;
     const long long M = g->rows, K = g->width, N = g->out_width;
     if (dweight) HFL_TRY(ff_pointer(dweight, "dweight"));
-    if (M == 0) {               // (no groups either)
+    if (M == 0) {               // (no groups of rows either; without groups there is one row of the gate all the same)
         if (dweight) HFL_CUDA(cudaMemsetAsync(dweight, 0, (size_t)N * K * 2, st));
         if (dbias) HFL_CUDA(cudaMemsetAsync(dbias, 0, (size_t)N * sizeof(float), st));
+        if (dgate && g->rows_per_group == 0) HFL_CUDA(cudaMemsetAsync(dgate, 0, (size_t)N * sizeof(float), st));
         return HF_OK;
     }
     if (!dx && !dweight && !dbias && !dgate) return HF_OK;
