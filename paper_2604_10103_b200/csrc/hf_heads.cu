@@ -92,7 +92,8 @@ hf_status launch_heads(const Device* d, const HeadsParams& p, const HeadsPlan& n
                 k_heads_bwd_ring<T, HALVES, HB, false><<<grid, n.threads, smem, st>>>(p);
             }
         } else {
-            if (smem > 48 * 1024) HFL_TRY(allow_shared<Key>(d, k_heads_bwd<T, HALVES, WIDE, HB, BIG>, 16384 * 4));
+            // (asked for whatever the row: beside the kernel's own shared memory one of 12225 features no longer fits in what a launch has unasked)
+            HFL_TRY(allow_shared<Key>(d, k_heads_bwd<T, HALVES, WIDE, HB, BIG>, 16384 * 4));
             k_heads_bwd<T, HALVES, WIDE, HB, BIG><<<grid, n.threads, smem, st>>>(p);
         }
     }
