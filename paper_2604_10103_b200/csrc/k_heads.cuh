@@ -180,9 +180,10 @@ __device__ __forceinline__ float heads_lanes_sum(float v, int n) {
     for (int o = 1; o < n; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
-// Sums over a team's lanes; every thread of the thread block calls it.  s: [2][teams W], one half for each call in turn.
+// Sums over a team's lanes; every thread of the thread block calls it.  s: [2][warps of the thread block], one half for each call in turn.  The warps behind
+// the last team come to the barrier and have no sums to read (there are fewer of them than a team has).
 template <int N>
-__device__ __forceinline__ void heads_team_sum(float (&v)[N], int team, int warp, int warps, float* s) {
+__device__ __forceinline__ void heads_team_sum(float (&v)[N], int team, int teams, int warp, int warps, float* s) {
 #pragma unroll
     for (int n = 0; n < N; ++n) v[n] = heads_lanes_sum(v[n], 32);
     if (warps == 1) return;
@@ -190,6 +191,7 @@ __device__ __forceinline__ void heads_team_sum(float (&v)[N], int team, int warp
 #pragma unroll
         for (int n = 0; n < N; ++n) s[(team * warps + warp) * N + n] = v[n];
     __syncthreads();
+    if (team >= teams) return;
 #pragma unroll
     for (int n = 0; n < N; ++n) v[n] = 0.f;
     for (int w = 0; w < warps; ++w)
@@ -274,7 +276,7 @@ k_heads(const __grid_constant__ HeadsParams p) {
         all[0] += own[k];
     }
     if (p.over_width) {
-        heads_team_sum(all, team, team_warp, warps, s_sum);
+        heads_team_sum(all, team, p.teams[part], team_warp, warps, s_sum);
         all[0] = 1.f / sqrtf(all[0] / (float)(heads * p.head_dim) + p.eps);
     }
     __syncwarp();
@@ -407,7 +409,7 @@ k_heads_bwd(const __grid_constant__ HeadsParams p) {
         }
         float r = 0.f, c = 0.f;
         if (p.over_width) {
-            heads_team_sum(all, team, team_warp, warps, s_sum[turn]);
+            heads_team_sum(all, team, teams, team_warp, warps, s_sum[turn]);
             const float n = (float)(heads * p.head_dim);
             r = 1.f / sqrtf(all[0] / n + p.eps);
             c = all[1] * r / n;                 // mean(g w x r)
@@ -662,7 +664,7 @@ k_heads_bwd_ring(const __grid_constant__ HeadsParams p) {
                 vfma(s2, w, f, s2);
             }
             float all[2] = {vsum(s1), vsum(s2)};
-            heads_team_sum(all, team, team_warp, warps, s_sum[turn]);
+            heads_team_sum(all, team, teams, team_warp, warps, s_sum[turn]);
             const float r = 1.f / sqrtf(all[0] * inv + p.eps), c = all[1] * r * inv;
 #pragma unroll
             for (int k = 0; k < HB; ++k, to += x_step) {
