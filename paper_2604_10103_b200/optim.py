@@ -8,6 +8,7 @@ norm).  As in `layers`: calls of the library (include/hf.h) on the current devic
 """
 from __future__ import annotations
 
+import copy
 import functools
 import operator
 import struct
@@ -224,7 +225,8 @@ class AdamW(torch.optim.Optimizer):
 
     @torch.no_grad()
     def load_state_dict(self, state_dict):
-        """Into the state as it lies: the same parameters, state_bits and masters are taken, and refused before anything is changed otherwise."""
+        """Into the state as it lies: the same parameters, state_bits and masters are taken, and refused before anything is changed otherwise.  A rate that
+        lies on the device takes the saved value where it is."""
         saved = state_dict["param_groups"]
         if [len(g["params"]) for g in saved] != [len(g["params"]) for g in self.param_groups]:
             _fail("the groups' numbers of parameters differ")
@@ -233,9 +235,18 @@ class AdamW(torch.optim.Optimizer):
             mine, theirs = self.state[p], state_dict["state"].get(i, {})
             if mine.keys() != theirs.keys() or any(mine[k].shape != theirs[k].shape or mine[k].dtype != theirs[k].dtype for k in mine):
                 _fail(f"the state of parameter {i} is of another shape, type or kind")
+        for theirs in saved:
+            if isinstance(theirs["lr"], torch.Tensor) and theirs["lr"].numel() != 1:
+                _fail("lr is a number, or a tensor of one element")
         for i, p in zip(ids, self._params):
             for k, t in self.state[p].items():
                 t.copy_(state_dict["state"][i][k])
         for mine, theirs in zip(self.param_groups, saved):
-            mine.update({k: v for k, v in theirs.items() if k != "params"})
+            lr, new = mine["lr"], {k: copy.deepcopy(v) for k, v in theirs.items() if k != "params"}
+            if isinstance(lr, torch.Tensor):        # (where it lies: captured steps read it there)
+                lr.copy_(torch.as_tensor(new["lr"]).reshape(lr.shape))
+                new["lr"] = lr
+            elif isinstance(new["lr"], torch.Tensor):
+                new["lr"] = new["lr"].to(self.buffers["steps"].device, _F32)
+            mine.update(new)
         self._plan = self._planned = None
