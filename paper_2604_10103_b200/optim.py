@@ -227,6 +227,10 @@ class AdamW(torch.optim.Optimizer):
     def load_state_dict(self, state_dict):
         """Into the state as it lies: the same parameters, state_bits and masters are taken, and refused before anything is changed otherwise.  A rate that
         lies on the device takes the saved value where it is."""
+        state_dict = state_dict.copy()
+        for hook in list(self._optimizer_load_state_dict_pre_hooks.values()):           # (torch's own method, which would call them, makes new tensors of the state)
+            changed = hook(self, state_dict)
+            state_dict = state_dict if changed is None else changed
         saved = state_dict["param_groups"]
         if [len(g["params"]) for g in saved] != [len(g["params"]) for g in self.param_groups]:
             _fail("the groups' numbers of parameters differ")
@@ -250,3 +254,5 @@ class AdamW(torch.optim.Optimizer):
                 new["lr"] = new["lr"].to(self.buffers["steps"].device, _F32)
             mine.update(new)
         self._plan = self._planned = None
+        for hook in list(self._optimizer_load_state_dict_post_hooks.values()):
+            hook(self)
