@@ -223,10 +223,14 @@ class AdamW(torch.optim.Optimizer):
                 _check(status)
         return loss
 
+    def state_dict(self):
+        """As torch's optimizers give it, with the seed: a resumed run in 8 bits rounds as one that goes on."""
+        return {**super().state_dict(), "seed": self.seed}
+
     @torch.no_grad()
     def load_state_dict(self, state_dict):
         """Into the state as it lies: the same parameters, state_bits and masters are taken, and refused before anything is changed otherwise.  A rate that
-        lies on the device takes the saved value where it is."""
+        lies on the device takes the saved value where it is.  The seed is the saved one, where there is one (a captured step keeps its own)."""
         state_dict = state_dict.copy()
         for hook in list(self._optimizer_load_state_dict_pre_hooks.values()):           # (torch's own method, which would call them, makes new tensors of the state)
             changed = hook(self, state_dict)
@@ -253,6 +257,7 @@ class AdamW(torch.optim.Optimizer):
             elif isinstance(new["lr"], torch.Tensor):
                 new["lr"] = new["lr"].to(self.buffers["steps"].device, _F32)
             mine.update(new)
+        self.seed = int(state_dict.get("seed", self.seed)) & 0xffffffff
         self._plan = self._planned = None
         for hook in list(self._optimizer_load_state_dict_post_hooks.values()):
             hook(self)
