@@ -12,6 +12,7 @@ import copy
 import functools
 import operator
 import struct
+from itertools import chain
 
 import numpy as np
 import torch
@@ -23,6 +24,7 @@ _F32, _BF16 = torch.float32, torch.bfloat16
 _BLOCK = 256                                                # elements that share a scale; tensors start at multiples of it in the state's buffers
 _STEP = struct.Struct("@3iI3d2P").pack                      # hf_adamw_step
 _rate, _of_group = operator.itemgetter("lr"), operator.itemgetter("lr", "weight_decay", "betas", "eps")
+_betas = operator.itemgetter(2)                             # of those
 
 
 @functools.lru_cache(maxsize=256)
@@ -51,6 +53,14 @@ def gradient_norm(tensors, max_norm=float("inf")):
     if status:
         _check(status)
     return out.unbind()
+
+
+def _kept(settings):
+    """The settings as a copy that changes in place do not reach; None where one of them is an array or a tensor (the tables are then made anew in each step)."""
+    kinds = set(map(type, chain.from_iterable(settings))) | set(map(type, chain.from_iterable(map(_betas, settings))))
+    if not all(issubclass(kind, (int, float, tuple, list, np.number)) for kind in kinds):
+        return None
+    return settings if list not in kinds else [(lr, decay, tuple(betas) if isinstance(betas, tuple) else list(betas), eps) for lr, decay, betas, eps in settings]
 
 
 class _Launch:
@@ -215,7 +225,7 @@ class AdamW(torch.optim.Optimizer):
             for launch in launches:
                 launch.look()
             if len(some) == len(self._params):
-                self._plan, self._planned = launches, settings
+                self._plan, self._planned = launches, _kept(settings)
         stream = _stream()
         for launch in launches:
             status = _lib().hf_adamw(_STEP(*launch.head, factor, launch.counter), launch.at, len(launch.params), stream)
