@@ -72,13 +72,16 @@ class _Launch:
         self.at, self.look_over = table.ctypes.data, (device, _TYPES[dtype], _TYPES[grad_dtype], self.sizes.ctypes.data, table.ctypes.data)
 
     def look(self):
-        """The parameters and gradients as they are now, into the table; False where a gradient is missing."""
-        bad = hf.host().hf_host_parameters(self.params, *self.look_over)
+        """The parameters and gradients as they are now, into the table; otherwise (not 0) where they are not what they were."""
+        return hf.host().hf_host_parameters(self.params, *self.look_over)
+
+    def check(self):
+        """The same; raises where they are not what is taken."""
+        bad = self.look()
         if bad > 0:
             p = self.params[bad - 1]
             _fail(f"a parameter or its gradient is not what it was: {self.dtype} of {self.sizes[bad - 1]} elements, contiguous, on device {self.device}, and such a gradient, "
                   f"are taken, not {p.dtype} {tuple(p.shape)} on {p.device} with {p.grad.dtype} {tuple(p.grad.shape)} on {p.grad.device}")
-        return not bad
 
 
 class AdamW(torch.optim.Optimizer):
@@ -217,13 +220,13 @@ class AdamW(torch.optim.Optimizer):
         _current("the first parameter", self._params[0])
         settings = self._settings()
         launches = self._plan if settings == self._planned else None
-        if launches is not None and not all(launch.look() for launch in launches):
-            launches = None                 # (a gradient is missing)
+        if launches is not None and any(launch.look() for launch in launches):
+            launches = None                 # (a gradient is missing, or of the other type)
         if launches is None:
             some = [p for p in self._params if p.grad is not None]
             launches = self._launches(some)
             for launch in launches:
-                launch.look()
+                launch.check()
             if len(some) == len(self._params):
                 self._plan, self._planned = launches, _kept(settings)
         stream = _stream()
