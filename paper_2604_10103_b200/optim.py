@@ -179,9 +179,12 @@ class AdamW(torch.optim.Optimizer):
         of = {p: (tuple(map(float, g["betas"])), float(g["eps"])) for g in self.param_groups for p in g["params"]}
         kinds = {}
         for p in params:
-            if p.dtype not in _TYPES or p.grad.dtype not in _TYPES:
-                _fail(f"a parameter is {p.dtype} with a gradient of {p.grad.dtype}: bfloat16 and float32 are taken")
+            if p.dtype is not _F32 and p.dtype is not _BF16 or p.grad.dtype is not p.dtype and p.grad.dtype is not _F32:
+                _fail(f"a parameter is {p.dtype} with a gradient of {p.grad.dtype}: bfloat16 and float32 are taken, with a gradient of the same type or float32")
             kinds.setdefault((p.dtype, p.grad.dtype, "master" in self.state[p], *of[p]), []).append(p)
+        for *_, (beta1, beta2), eps in kinds:       # (here, where none of the launches has run)
+            if not (0.0 <= beta1 < 1.0 and 0.0 <= beta2 < 1.0 and 0.0 <= eps <= 3e38):
+                _fail(f"betas {beta1}, {beta2} and eps {eps}: betas in [0, 1) and an eps >= 0, finite, are taken")
         counter = self.buffers["steps"].data_ptr() + 4 * len(self._params)
         return [_Launch(some, self._table[[self._index[p] for p in some], 8], dtype, grad_dtype, self._device, self._rows(some), (_TYPES[dtype],
                         _TYPES[grad_dtype], self.state_bits, self.seed, *betas, eps), counter) for (dtype, grad_dtype, _, betas, eps), some in kinds.items()]
