@@ -192,7 +192,7 @@ class AdamW(torch.optim.Optimizer):
     def _settings(self):
         """What the tables were made from, and step for step may change."""
         groups = self.param_groups
-        if torch.Tensor not in map(type, map(_rate, groups)):
+        if not any(issubclass(kind, torch.Tensor) for kind in set(map(type, map(_rate, groups)))):
             return list(map(_of_group, groups))
         seen = []
         for g in groups:
