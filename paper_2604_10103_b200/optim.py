@@ -103,6 +103,8 @@ class AdamW(torch.optim.Optimizer):
         super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay))
         self.state_bits, self.seed = state_bits, int(seed) & 0xffffffff
         self._params = [p for g in self.param_groups for p in g["params"]]
+        if len(set(self._params)) != len(self._params):         # (two parts of a launch would step it at the same time)
+            _fail("a parameter is given twice")
         dev, starts, at, master_at = None, [], 0, []
         masters = 0
         for i, p in enumerate(self._params):
