@@ -21,11 +21,12 @@ bool here(const at::Tensor& t, int device) { return t.layout() == at::kStrided &
 
 extern "C" {
 
-// tensors: a list; rows: one hf_gradient for each.  0, or 1 + the place of the first that is not a contiguous tensor of a known type on the device.
+// tensors: a list; rows: one hf_gradient for each, of no elements for None.  0, or 1 + the place of the first that is not a contiguous tensor of a known type on the device.
 int hf_host_gradients(PyObject* tensors, int device, hf_gradient* rows) {
     const Py_ssize_t n = PyList_GET_SIZE(tensors);
     for (Py_ssize_t i = 0; i < n; ++i) try {
         PyObject* o = PyList_GET_ITEM(tensors, i);
+        if (o == Py_None) { rows[i] = {nullptr, 0, HF_F32}; continue; }
         if (!THPVariable_Check(o)) return (int)i + 1;
         const at::Tensor& t = THPVariable_Unpack(o);
         const int kind = kind_of(t);

@@ -33,12 +33,13 @@ def _norm_workspace(dev, n):
 
 
 def gradient_norm(tensors, max_norm=float("inf")):
-    """(norm, factor), two float32 scalars on the device: the 2-norm of all tensors together (bf16, f16 or f32, contiguous, on the current device),
-    and min(1, max_norm / norm), which `AdamW.step` takes as its factor; NaN where the norm is not finite."""
+    """(norm, factor), two float32 scalars on the device: the 2-norm of all tensors together (bf16, f16 or f32, contiguous, on the current device; a gradient
+    that is missing, None, is left out), and min(1, max_norm / norm), which `AdamW.step` takes as its factor; NaN where the norm is not finite."""
     tensors = list(tensors)
-    if not tensors:
+    first = next((i for i, t in enumerate(tensors) if t is not None), None)
+    if first is None:
         _fail("no tensors")
-    dev = _current("tensors[0]", tensors[0])
+    dev = _current(f"tensors[{first}]", tensors[first])
     n = len(tensors)
     rows = bytearray(24 * n)                                # hf_gradient
     at = (hf.C.c_char * len(rows)).from_buffer(rows)
@@ -47,7 +48,7 @@ def gradient_norm(tensors, max_norm=float("inf")):
         t = tensors[bad - 1]
         _here(f"tensors[{bad - 1}]", t, dev)
         _fail(f"tensors[{bad - 1}] is {t.dtype}{'' if t.is_contiguous() else ', not contiguous'}: contiguous bfloat16, float16 and float32 are taken")
-    out = torch.empty(2, dtype=_F32, device=tensors[0].device)
+    out = torch.empty(2, dtype=_F32, device=tensors[first].device)
     ws = torch.empty(_norm_workspace(dev, n), dtype=torch.float64, device=out.device)
     status = _lib().hf_gradient_norm(at, n, max_norm, out.data_ptr(), ws.data_ptr(), _stream())
     if status:
