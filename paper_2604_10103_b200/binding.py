@@ -9,6 +9,8 @@ from __future__ import annotations
 import ctypes as C
 import os
 
+from . import build
+
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libhf.so")
 
@@ -180,11 +182,10 @@ _host = None
 
 
 def host() -> C.PyDLL:
-    """Load libhf_host.so (once), which looks over torch tensors for the optimizer's calls.  Raises if it has not been built."""
+    """Load the host library (once), which looks over torch tensors for the optimizer's calls.  Raises if it has not been built for this torch."""
     global _host
     if _host is None:
-        import torch  # noqa: F401  (its libraries come first)
-        path = os.path.join(HERE, "libhf_host.so")
+        path = build.host_lib()                 # (imports torch, whose libraries come first)
         if not os.path.exists(path):
             raise RuntimeError(f"{path} is missing: build it with `python -m paper_2604_10103_b200.build`")
         h = C.PyDLL(path)

@@ -1,4 +1,5 @@
-"""Build libhf.so in-tree with nvcc for sm_100a (cross-compiles without a GPU), and libhf_host.so, which looks over torch tensors for the optimizer, with g++."""
+"""Build libhf.so in-tree with nvcc for sm_100a (cross-compiles without a GPU), and libhf_host-<torch's version>.so, which looks over torch
+tensors for the optimizer, with g++."""
 from __future__ import annotations
 
 import os
@@ -9,7 +10,7 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhf.so")
-HOST_LIB, HOST_SOURCE = os.path.join(HERE, "libhf_host.so"), os.path.join(CSRC, "host_tensors.cpp")
+HOST_SOURCE = os.path.join(CSRC, "host_tensors.cpp")
 HEADER = os.path.join(HERE, "..", "include", "hf.h")
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -29,8 +30,21 @@ def _older(lib, deps) -> bool:
     return not os.path.exists(lib) or any(os.path.getmtime(p) > os.path.getmtime(lib) for p in deps)
 
 
+def host_lib() -> str:
+    """Path of the host library for the torch that is installed: it is built against that one's inlined accessors.  ImportError without torch."""
+    import torch
+    return os.path.join(HERE, f"libhf_host-{torch.__version__}.so")
+
+
+def _host_stale() -> bool:
+    try:
+        return _older(host_lib(), [HOST_SOURCE, HEADER])
+    except ImportError:
+        return False
+
+
 def stale() -> bool:
-    return _older(LIB, _deps()) or _older(HOST_LIB, [HOST_SOURCE, HEADER])
+    return _older(LIB, _deps()) or _host_stale()
 
 
 def _run(cmd):
@@ -45,18 +59,24 @@ def _host_command():
     root = os.path.dirname(torch.__file__)
     include = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"]]
     return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
-            *("-I" + p for p in include), HOST_SOURCE, "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-o", HOST_LIB]
+            *("-I" + p for p in include), HOST_SOURCE, "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-o", host_lib()]
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile every .cu under csrc/ into libhf.so (returns its path), and host_tensors.cpp into libhf_host.so.  Raises on failure."""
-    if force or _older(HOST_LIB, [HOST_SOURCE, HEADER]):
-        _run(_host_command())
+    """Compile every .cu under csrc/ into libhf.so (returns its path), which needs no torch, and then, where torch is installed, host_tensors.cpp into its host
+    library.  Raises on failure."""
     if force or _older(LIB, _deps()):
         nvcc = os.environ.get("NVCC", "nvcc")
         told = _run([nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + sources() + ["-o", LIB])
         if verbose:
             sys.stderr.write(told)
+    try:
+        host = host_lib()
+    except ImportError:
+        sys.stderr.write("torch is not installed: built without the host library, which the optimizer's calls from Python need\n")
+        return LIB
+    if force or _older(host, [HOST_SOURCE, HEADER]):
+        _run(_host_command())
     return LIB
 
 
