@@ -384,6 +384,7 @@ hf_status hf_rope_axes(const hf_rope_shape* shape, const hf_rope_tensor* tensors
  * heads, then k's, then v's.  With r = 1 / sqrt(mean x^2 + eps), the mean over a head (HF_NORM_OVER_HEAD) or over all of q's (of k's) heads of the
  * token (HF_NORM_OVER_WIDTH):   q = R (x r q_weight),  k = R (x r k_weight),  v as it is;   R as hf_rope_axes turns a head (axes, pairs,
  * extent, pairing, tables and positions as there, a position outside its table too).
+ * Squares and their mean are float32: where they overflow (features beyond 1.8e19) results are 0 or not finite.
  *   q_weight  [head_dim], or [heads head_dim] with HF_NORM_OVER_WIDTH (k_weight: kv_heads); NULL: 1
  *   heads     q, k, v [batch, heads or kv_heads, tokens, head_dim], features contiguous, other strides free
  * Pointers are aligned to their element; where all start on 16 bytes, head_dim is a multiple of 8 (and, in halves, the sum of pairs of 4) and
@@ -471,7 +472,7 @@ hf_status hf_linear_backward(const hf_linear_shape* shape, const void* dy, const
 
 /* out[0] = the 2-norm of all tensors together; out[1] = min(1, max_norm / out[0]), the factor that brings it to max_norm at most (1 for a norm of
  * 0; NaN where the norm is not finite, which hf_adamw takes as a step to leave out).  Squares are formed in float32, so a value beyond 1.8e19
- * counts as not finite; they are summed in double, in a fixed order.  Tensors are contiguous.  out: device, two floats. */
+ * counts as not finite, and one below 2e-23 as 0 (below 1e-19 its square has fewer bits); they are summed in double, in a fixed order.  Tensors are contiguous.  out: device, two floats. */
 typedef struct {
     const void* p;
     int64_t n;                   /* elements                */
@@ -488,8 +489,8 @@ hf_status hf_gradient_norm(const hf_gradient* tensors, int n_tensors, float max_
  * scales [ceil(n / 256)][2] float for m and v, rounded up or down at random, up with the probability of what is cut off, by a hash of seed, t
  * and the element's place (256 first_block + its index): give every tensor blocks of its own.  A value that is not finite spoils its block of 256.
  * factor: device float, or NULL (1); where it is not finite the call changes nothing.  lr_at: device float that stands for lr, or NULL, so that a
- * captured step follows a schedule.  Pointers are aligned to their element, scales to 8 bytes; tensors whose pointers are all 16-byte aligned are
- * the fastest.  A tensor is in a call once; two calls on the same tensors or the same counter must not run at the same time. */
+ * captured step follows a schedule.  Pointers are aligned to their element, scales to 8 bytes; a tensor is the fastest where its float32 parts start on
+ * 32 bytes, its bf16 parts on 16 and its states in 8 bits on 8.  A tensor is in a call once; two calls on the same tensors or the same counter must not run at the same time. */
 typedef struct {
     int param_type;              /* HF_BF16 | HF_F32                    */
     int grad_type;               /* the parameters' type, or HF_F32     */

@@ -199,7 +199,7 @@ size_t ff_partial_bytes(const Tiling& t, const Size* s, int n) {
     return tiles * t.splits * 128 * t.cg * t.bn * sizeof(float);
 }
 
-// Up to 16 rows: both products by k_ff_rows (width 1536, hidden 4096: 1 row 10.5 us, 16 rows 13.7; with tiles 23.5; its form for 32 rows took 26).
+// Up to 16 rows: both products by k_ff_rows (width 1536, hidden 4096, weights from memory: 1 row 10.0 us, 16 rows 13.4; with tiles 23.5; its form for 32 rows took 26).
 constexpr int FF_ROWS_MOST = 16;
 template <typename T, int NT, int ACT>
 hf_status launch_rows(const hf_ff_shape* g, const FfRowsParams& first, const FfRowsParams& second, cudaStream_t st) {

@@ -6,8 +6,9 @@
 // The 8 columns of an MMA are 8 rows of x.  The warps of a thread block split the contraction, and their sums meet in shared memory, in
 // order.  Sums are float32; h is rounded once between the products, as the tiled kernels round it.  A contraction index may be permuted if both operands are: lane (g, t) holds the 16 bytes at 32 j + 8 t of row g, and its four words
 // serve as the two k-steps' fragments, so every load is 16 bytes.  The second product's weights are on their way before the first
-// kernel has finished.  Width 1536, hidden 4096 (37.7 MB of weights, 5.8 us at the measured copy rate): one row 10.5 us for both kernels (3.6 TB/s:
-// two launches, and latency at their ends), 8 rows 11.2, 16 rows 13.7.  PAIR, one row of 1536 to 9216 (28 MB, 4.3 us): 6.7 us.
+// kernel has finished.  Width 1536, hidden 4096 (37.7 MB of weights, 5.8 us at the measured copy rate), weights from memory (in L2): one row
+// 10.0 us (7.5) for both kernels (3.8 TB/s: two launches, and latency at their ends), 8 rows 10.8 (8.2), 16 rows 13.4 (11.1).  PAIR, one row of 1536 to 9216
+// (28 MB, 4.3 us): 8.6 us (6.7).
 #pragma once
 #include "k_vec.cuh"
 

@@ -224,8 +224,9 @@ __device__ __forceinline__ void heads_look_up(const HeadsParams& p, int pairs, i
     }
 }
 
-// HB: heads of a lane.  Threads of a thread block: at most 128, or 512 (BIG).  The issue slots bound it with memory (4680 tokens of 12 + 24 heads of 128: 19.0 us): angles
-// looked up by each lane, addresses formed anew for each head and selections for pairs that are not rotated took 21.3.
+// HB: heads of a lane.  Threads of a thread block: at most 128, or 512 (BIG).  4680 tokens of 12 + 24 heads of 128: 18.9 us with the inputs in L2, 23 from memory, where the loads'
+// latency bounds it: a warp loads once, waits, computes and stores, a third of the warps are held, and half of the issue slots are used (13.6 M warp instructions:
+// 12 us of the 592 schedulers).  With angles looked up by each lane, addresses formed anew for each head and selections for pairs that are not rotated 21.3 in L2.
 template <typename T, bool HALVES, bool WIDE, int HB, bool BIG>
 __global__ void __launch_bounds__(BIG ? 512 : 128)
 k_heads(const __grid_constant__ HeadsParams p) {

@@ -98,7 +98,7 @@ template <bool E5> __device__ __forceinline__ void optim_decode(uint2 c, float s
         f[2 * j] = v.x; f[2 * j + 1] = v.y;
     }
 }
-// An invertible mix of 32 bits.
+// An invertible mix of 32 bits: two multiplications between shifts, with the published constants of lowbias32 (C. Wellons, 2018).
 __device__ __forceinline__ uint32_t optim_mix(uint32_t x) {
     x = (x ^ (x >> 16)) * 0x7feb352du;
     x = (x ^ (x >> 15)) * 0x846ca68bu;
@@ -113,7 +113,7 @@ template <int DROP> __device__ __forceinline__ float2 optim_up_or_down(float2 y,
                  make_float2(-off.x, -off.y));
 }
 // Two quotients by a block's scale, no more than the type's largest value: products with its reciprocal, corrected by the residual, which the fused
-// multiply-add forms exactly.
+// multiply-add forms exactly (P. Markstein, IBM Journal of Research and Development 34, 1990).
 __device__ __forceinline__ float2 optim_quotient(float2 v, float scale, float inv, float most) {
     const float2 i2 = make_float2(inv, inv), q = fmul2(v, i2), r = ffma2(make_float2(-q.x, -q.y), make_float2(scale, scale), v), o = ffma2(r, i2, q);
     return make_float2(fminf(o.x, most), fminf(o.y, most));
